@@ -30,6 +30,9 @@
  *     err_count, the "number of corrupted rows" output of Algorithm 1.
  *   - B is symmetric-quantized (zero point 0): the row-offset term
  *     alpha_A beta_B (A_I e_k) e_n^T of Eq. 1 is not part of this library.
+ *
+ * At the end of this header: products with 4-bit weights for a handful of rows
+ * (abft_w4_*), the weight format of a decoding step.  They carry no check.
  */
 #ifndef ABFT_GEMM_H
 #define ABFT_GEMM_H
@@ -338,6 +341,51 @@ int abft_mfma_peak_probe(uint64_t* out, int iters, void* stream);
  * shader cycles and 100 MHz wall ticks before the K loop, after it, and at the
  * end of the kernel.  Process-wide; the product library carries no such code. */
 int abft_clock_trace(uint64_t* buf);
+
+/* ------------------------------------------------------------------------- */
+/* Products with 4-bit weights, for few rows (a decoding step, a short prompt):
+ *     Y[m][n] = sum_k X[m][k] * W[n][k],
+ *     W[n][k] = scale[n][k / group] * code[n][k] + bias[n][k / group],
+ * codes 0..15 (4-bit, two per byte, the even column in the low half, as in the
+ * 4-bit tables of abft_eb.h).  Not part of the paper; no check. */
+
+/* element types of activations, and of what is stored beside codes */
+#define ABFT_TYPE_F32 0
+#define ABFT_TYPE_F16 1
+#define ABFT_TYPE_BF16 2
+
+/* Opaque packed weight.  The library owns its device memory; it belongs to the
+ * device that was current when it was packed (a product with another device
+ * current returns ABFT_EINVAL). */
+typedef struct abft_w4 abft_w4;
+
+/* Lay a weight out once.
+ *   W      codes, N rows of (K + 1) / 2 bytes, ldw (bytes) at least that; the
+ *          high half of the last byte of an odd K is ignored
+ *   scale  N rows of ceil(K / group) values of `scale_type`, lds (values) at least that
+ *   bias   the same shape, or NULL: W = scale * (code - 8)
+ *   group  32, 64 or 128; the last group of a row may be short
+ * The scales are kept in the type that they have.  Allocates with hipMalloc; the
+ * packing kernels are enqueued on `stream`, and the inputs must stay valid until
+ * they have run. */
+int abft_w4_pack(const uint8_t* W, int64_t ldw, const void* scale, const void* bias, int64_t lds, int scale_type, int N, int K,
+                 int group, void* stream, abft_w4** out);
+
+/* N, K, group and the bytes that the weight holds on the device (host out-pointers, any may be NULL). */
+int abft_w4_dims(const abft_w4* Wp, int* N, int* K, int* group, size_t* bytes);
+
+/* Host call.  Frees the handle; the caller has synchronised every stream that used it. */
+void abft_w4_destroy(abft_w4* Wp);
+
+/* Y = X W^T.
+ *   X   M x K of `type`, ldx >= K (elements); Y  M x N of the same type, ldy >= N.
+ *       Any alignment of an element; rows of X that are multiples of 16 bytes are read faster.
+ * The products are exact and are summed in binary32 (16-bit types: X enters the matrix
+ * cores as it is; binary32: as three bfloat16 parts that add up to it), a group's sum is
+ * scaled in binary32, and the result is rounded once, to `type`.  A row of X that holds
+ * an infinity or a NaN gives NaN.  M == 0 is a valid call that does nothing.
+ * No workspace, no host synchronisation, the same bits every time. */
+int abft_w4_gemv(const void* X, int64_t ldx, int type, int M, const abft_w4* Wp, void* Y, int64_t ldy, void* stream);
 
 /* Message for the last non-OK return on this host thread. */
 const char* abft_last_error(void);

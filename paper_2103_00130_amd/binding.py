@@ -33,16 +33,20 @@ EXPORTS = (
     "abft_verify_rows", "abft_row_checksum", "abft_recover_scratch_bytes", "abft_recompute_flagged_rows",
     "abft_recompute_flagged_rows_async",
     "abft_locate_scratch_bytes", "abft_locate_correct", "abft_calib_copy", "abft_clock_probe", "abft_mfma_peak_probe", "abft_clock_trace", "abft_last_error",
+    "abft_w4_pack", "abft_w4_dims", "abft_w4_destroy", "abft_w4_gemv",
 )
 ABFT_LOCATE_CLEAN, ABFT_LOCATE_CORRECTED, ABFT_LOCATE_NOT_ONE_ELEMENT = 0, 1, 2
 EXPORTS_EB = (
     "abft_eb_pack_rowsum", "abft_eb_table_dims", "abft_eb_table_get_rowsums", "abft_eb_table_flip_bit",
     "abft_eb_table_destroy", "abft_eb_u8_checked",
+    "abft_kv_code_bytes", "abft_kv_plan", "abft_kv_append", "abft_kv_read", "abft_kv_attention_workspace_bytes", "abft_kv_attention",
 )
 ABFT_EB_CHECK, ABFT_EB_NOCHECK = 0, 1
 ABFT_EB_VARIANT_BATCH, ABFT_EB_VARIANT_GROUP = 0x100, 0x200
 ABFT_EB_ERR, ABFT_EB_BAD_INDEX = 1, 2
 ABFT_EB_PACK_COMPACT, ABFT_EB_PACK_LINE_ALIGNED, ABFT_EB_PACK_INT4 = 0, 1, 2
+ABFT_TYPE_F32, ABFT_TYPE_F16, ABFT_TYPE_BF16 = 0, 1, 2
+ABFT_KV_NO_BLOCK, ABFT_KV_TABLE_FULL, ABFT_KV_NO_ROW, ABFT_KV_BAD_LENGTH, ABFT_KV_BAD_BLOCK = 1, 2, 4, 8, 16
 
 
 class abft_requant_t(ctypes.Structure):
@@ -52,6 +56,11 @@ class abft_requant_t(ctypes.Structure):
 
 class abft_inject_t(ctypes.Structure):
     _fields_ = [("row", ctypes.c_int32), ("col", ctypes.c_int32), ("xor_mask", ctypes.c_uint32)]
+
+
+class abft_kv_cache_t(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_blocks", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block_tokens", ctypes.c_int32)]
 
 
 class AbftError(RuntimeError):
@@ -107,6 +116,20 @@ def _load() -> ctypes.CDLL:
     L.abft_eb_table_destroy.argtypes = [vp]
     L.abft_eb_table_destroy.restype = None
     L.abft_eb_u8_checked.argtypes = [vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, ctypes.c_double, u32, vp]
+    L.abft_w4_pack.argtypes = [vp, i64, vp, vp, i64, i32, i32, i32, i32, vp, ctypes.POINTER(vp)]
+    L.abft_w4_dims.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(sz)]
+    L.abft_w4_destroy.argtypes = [vp]
+    L.abft_w4_destroy.restype = None
+    L.abft_w4_gemv.argtypes = [vp, i64, i32, i32, vp, vp, i64, vp]
+    kv = ctypes.POINTER(abft_kv_cache_t)
+    L.abft_kv_code_bytes.argtypes = [kv]
+    L.abft_kv_code_bytes.restype = sz
+    L.abft_kv_plan.argtypes = [vp, vp, i32, i32, vp, i64, i32, vp, i32, vp, vp, vp, i64, vp, vp, vp]
+    L.abft_kv_append.argtypes = [kv, vp, i64, i64, vp, i64, i64, i32, vp, i64, vp]
+    L.abft_kv_read.argtypes = [kv, vp, i64, vp, i64, i64, vp, i64, i64, i32, vp]
+    L.abft_kv_attention_workspace_bytes.argtypes = [kv, i32, i32, i32, i32]
+    L.abft_kv_attention_workspace_bytes.restype = sz
+    L.abft_kv_attention.argtypes = [kv, vp, i64, i64, i32, i64, i32, vp, i64, i32, vp, vp, i32, i32, i32, ctypes.c_float, vp, i64, i64, vp, vp, vp, sz, vp]
     return L
 
 
@@ -482,3 +505,201 @@ def abft_eb_u8_checked(Tp: EbTable, indices: torch.Tensor, offsets: torch.Tensor
                                   _ptr(R, torch.float32, "R"), _ld(R, "R"), _ptr(bag_flags, torch.int32, "bag_flags"),
                                   _ptr(rsum, torch.float64, "rsum"), _ptr(csum, torch.float64, "csum"),
                                   float(rel_bound), int(flags), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------------------------
+# Operators of a decoding step: 4-bit weights (abft_gemm.h), the 8-bit key/value cache (abft_eb.h)
+
+_TYPES = {torch.float32: ABFT_TYPE_F32, torch.float16: ABFT_TYPE_F16, torch.bfloat16: ABFT_TYPE_BF16}
+
+
+def _typed(t, name):
+    """(address, ABFT_TYPE_*) of a device tensor of activations."""
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype not in _TYPES:
+        raise TypeError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
+    return t.data_ptr(), _TYPES[t.dtype]
+
+
+def _entries(t, dtype, n, name):
+    """The address of a contiguous device tensor of at least n entries."""
+    if t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with at least {n} entries")
+    return _ptr(t, dtype, name)
+
+
+class W4Weight:
+    """Owner of an abft_w4 handle."""
+
+    def __init__(self, handle: int, N: int, K: int, group: int):
+        self.handle, self.N, self.K, self.group = handle, N, K, group
+
+    def destroy(self):
+        if self.handle:
+            torch.cuda.synchronize()
+            lib.abft_w4_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def abft_w4_pack(W: torch.Tensor, scale: torch.Tensor, bias: torch.Tensor | None = None, K: int | None = None, group: int = 128,
+                 stream=None) -> W4Weight:
+    """W: uint8 device tensor, N x ceil(K / 2) bytes of 4-bit codes (the even column in the low half; K defaults to twice the
+    bytes); scale, bias: N x ceil(K / group), of one type.  The weight is scale * code + bias, or scale * (code - 8) without bias."""
+    ptr = _ptr(W, torch.uint8, "W")
+    ldw = _ld(W, "W")
+    N, row = W.shape
+    if K is None:
+        K = 2 * row
+    if row != (K + 1) // 2:
+        raise ValueError(f"W has rows of {row} bytes, K={K} needs {(K + 1) // 2}")
+    groups = -(-K // group) if group > 0 else 0
+    s_ptr, s_type = _typed(scale, "scale")
+    lds = _ld(scale, "scale")
+    if tuple(scale.shape) != (N, groups):
+        raise ValueError(f"scale must be {N}x{groups}")
+    b_ptr = None
+    if bias is not None:
+        b_ptr, b_type = _typed(bias, "bias")
+        if b_type != s_type or tuple(bias.shape) != (N, groups) or _ld(bias, "bias") != lds:
+            raise ValueError("bias must have the type, shape and strides of scale")
+    out = ctypes.c_void_p()
+    _check(lib.abft_w4_pack(ptr, ldw, s_ptr, b_ptr, lds, s_type, N, K, group, _stream(stream), ctypes.byref(out)))
+    return W4Weight(out.value, N, K, group)
+
+
+def abft_w4_dims(Wp: W4Weight):
+    n, k, g, size = ctypes.c_int(), ctypes.c_int(), ctypes.c_int(), ctypes.c_size_t()
+    _check(lib.abft_w4_dims(Wp.handle, ctypes.byref(n), ctypes.byref(k), ctypes.byref(g), ctypes.byref(size)))
+    return n.value, k.value, g.value, size.value
+
+
+def abft_w4_gemv(X: torch.Tensor, Wp: W4Weight, Y: torch.Tensor, stream=None):
+    """Y = X W^T: X M x K, Y M x N, both float32, float16 or bfloat16."""
+    x_ptr, x_type = _typed(X, "X")
+    y_ptr, y_type = _typed(Y, "Y")
+    ldx, ldy = _ld(X, "X"), _ld(Y, "Y")
+    if X.shape[1] != Wp.K or tuple(Y.shape) != (X.shape[0], Wp.N):
+        raise ValueError(f"X is {tuple(X.shape)} and Y {tuple(Y.shape)}, the weight has K={Wp.K}, N={Wp.N}")
+    if x_type != y_type:
+        raise TypeError("X and Y must have the same type")
+    _check(lib.abft_w4_gemv(x_ptr, ldx, x_type, X.shape[0], Wp.handle, y_ptr, ldy, _stream(stream)))
+
+
+class KvCache:
+    """The buffers of an 8-bit key/value cache (abft_kv_cache_t): k_codes [n_blocks][heads][block_tokens][columns], v_codes
+    [n_blocks][heads][block_tokens / 16][columns][16], k_scale and v_scale [n_blocks][heads]; columns is head_dim rounded up to 64."""
+
+    def __init__(self, n_blocks: int, heads: int, head_dim: int, block_tokens: int = 64, device="cuda"):
+        self.n_blocks, self.heads, self.head_dim, self.block_tokens = int(n_blocks), int(heads), int(head_dim), int(block_tokens)
+        if not lib.abft_kv_code_bytes(ctypes.byref(abft_kv_cache_t(None, None, None, None, *self._sizes()))):
+            raise ValueError(f"no cache of {n_blocks} blocks of {block_tokens} tokens, {heads} heads of {head_dim}: block_tokens must be 16, 32, 64 or 128, "
+                             "head_dim 1..256, and there must be blocks and heads")
+        cols = (self.head_dim + 63) // 64 * 64
+        self.k_codes = torch.zeros((self.n_blocks, self.heads, self.block_tokens, cols), dtype=torch.int8, device=device)
+        self.v_codes = torch.zeros((self.n_blocks, self.heads, self.block_tokens // 16, cols, 16), dtype=torch.int8, device=device)
+        self.k_scale = torch.zeros((self.n_blocks, self.heads), dtype=torch.float32, device=device)
+        self.v_scale = torch.zeros((self.n_blocks, self.heads), dtype=torch.float32, device=device)
+        self.struct = abft_kv_cache_t(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(), *self._sizes())
+        self.ref = ctypes.byref(self.struct)
+
+    def _sizes(self):
+        return self.n_blocks, self.heads, self.head_dim, self.block_tokens
+
+    def load_codes(self, k, v, k_scale, v_scale):
+        """Fill the cache from codes [n_blocks][heads][block_tokens][head_dim] and scales [n_blocks][heads] (a saved cache)."""
+        self.k_codes[..., :self.head_dim] = k
+        self.v_codes[..., :self.head_dim, :] = v.unflatten(2, (self.block_tokens // 16, 16)).transpose(3, 4)
+        self.k_scale.copy_(k_scale)
+        self.v_scale.copy_(v_scale)
+
+    def codes(self):
+        """(k, v): the codes as [n_blocks][heads][block_tokens][head_dim]."""
+        return self.k_codes[..., :self.head_dim], self.v_codes[..., :self.head_dim, :].transpose(3, 4).flatten(2, 3)
+
+
+def abft_kv_plan(ctx_len, new_len, block_tokens: int, table, free_blocks, seq_len, cu_new, slots, req_flags, taken, stream=None):
+    """Block tables and slots of a step; table (int32, requests x blocks) is extended in place, seq_len, cu_new, slots (int64),
+    req_flags and taken are overwritten."""
+    R = ctx_len.numel()
+    if table.dim() != 2 or table.shape[0] != R:
+        raise ValueError("table must be 2-D with a row for each request")
+    ldt = max(_ld(table, "table"), table.shape[1])
+    _check(lib.abft_kv_plan(_entries(ctx_len, torch.int32, R, "ctx_len"), _entries(new_len, torch.int32, R, "new_len"), R, int(block_tokens),
+                            _ptr(table, torch.int32, "table"), ldt, table.shape[1], _entries(free_blocks, torch.int32, 0, "free_blocks"),
+                            free_blocks.numel(), _entries(seq_len, torch.int32, R, "seq_len"), _entries(cu_new, torch.int32, R + 1, "cu_new"),
+                            _entries(slots, torch.int64, 0, "slots"), slots.numel(), _entries(req_flags, torch.int32, R, "req_flags"),
+                            _entries(taken, torch.int32, 1, "taken"), _stream(stream)))
+
+
+def _kv_rows(t, cache, n, name, heads=None):
+    """(address, stride between tokens, stride between heads) of n x heads x head_dim values."""
+    heads = cache.heads if heads is None else heads
+    if tuple(t.shape) != (n, heads, cache.head_dim) or (cache.head_dim > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be {n} x {heads} x {cache.head_dim} with unit column stride, got {tuple(t.shape)}")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def abft_kv_append(cache: KvCache, K, V, slots, stream=None):
+    """Quantizes K and V (tokens x heads x head_dim) into the cache at `slots` (int64, as abft_kv_plan gives them)."""
+    T = slots.numel()
+    _, k_type = _typed(K, "K")
+    _, v_type = _typed(V, "V")
+    if k_type != v_type:
+        raise TypeError("K and V must have the same type")
+    _check(lib.abft_kv_append(cache.ref, *_kv_rows(K, cache, T, "K"), *_kv_rows(V, cache, T, "V"), k_type, _entries(slots, torch.int64, T, "slots"),
+                              T, _stream(stream)))
+
+
+def abft_kv_read(cache: KvCache, slots, K=None, V=None, stream=None):
+    """The tokens at `slots` as values, into K and V (tokens x heads x head_dim); either may be None."""
+    T = slots.numel()
+    types = {_typed(t, name)[1] for t, name in ((K, "K"), (V, "V")) if t is not None}
+    if len(types) > 1:
+        raise TypeError("K and V must have the same type")
+    none = (None, 0, 0)
+    _check(lib.abft_kv_read(cache.ref, _entries(slots, torch.int64, T, "slots"), T, *(none if K is None else _kv_rows(K, cache, T, "K")),
+                            *(none if V is None else _kv_rows(V, cache, T, "V")), types.pop() if types else ABFT_TYPE_F32, _stream(stream)))
+
+
+def abft_kv_attention_workspace_bytes(cache: KvCache, n_req: int, q_heads: int, max_new: int, max_len: int) -> int:
+    return int(lib.abft_kv_attention_workspace_bytes(cache.ref, int(n_req), int(q_heads), int(max_new), int(max_len)))
+
+
+class KvWorkspace:
+    """A workspace tensor for abft_kv_attention on up to n_req requests of up to max_new new tokens and max_len tokens in all (None
+    where none is needed)."""
+
+    def __init__(self, cache: KvCache, n_req: int, q_heads: int, max_new: int, max_len: int):
+        size = abft_kv_attention_workspace_bytes(cache, n_req, q_heads, max_new, max_len)
+        self.tensor = torch.empty(size // 4, dtype=torch.float32, device=cache.k_codes.device) if size else None
+
+
+def abft_kv_attention(cache: KvCache, Q, table, seq_len, cu_new, O, max_new: int, max_len: int, scale: float | None = None, lse=None,
+                      req_flags=None, workspace=None, stream=None):
+    """Attention of the rows of Q (new tokens x query heads x head_dim) over their requests' tokens, into O.  scale: 1 / sqrt(head_dim)
+    unless given."""
+    if Q.dim() != 3 or table.dim() != 2:
+        raise ValueError("Q must be rows x query heads x head_dim and table requests x blocks")
+    n_rows, q_heads = Q.shape[:2]
+    R = seq_len.numel()
+    _, q_type = _typed(Q, "Q")
+    _, o_type = _typed(O, "O")
+    if q_type != o_type:
+        raise TypeError("Q and O must have the same type")
+    if table.shape[0] != R:
+        raise ValueError("table must have a row for each request")
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.abft_kv_attention(
+        cache.ref, *_kv_rows(Q, cache, n_rows, "Q", q_heads), q_type, n_rows, q_heads, _ptr(table, torch.int32, "table"),
+        max(_ld(table, "table"), table.shape[1]), table.shape[1], _entries(seq_len, torch.int32, R, "seq_len"),
+        _entries(cu_new, torch.int32, R + 1, "cu_new"), R, int(max_new), int(max_len), cache.head_dim ** -0.5 if scale is None else float(scale),
+        *_kv_rows(O, cache, n_rows, "O", q_heads), None if lse is None else _entries(lse, torch.float32, n_rows * q_heads, "lse"),
+        None if req_flags is None else _entries(req_flags, torch.int32, R, "req_flags"), None if workspace is None else workspace.data_ptr(),
+        ws_bytes, _stream(stream)))

@@ -1,0 +1,446 @@
+"""The decoding-step operators on the GPU against decode_oracle: whole numbers (tables, slots, codes, scales) equal, the rest within the
+error that the oracle derives for each element."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode_oracle as o
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2103_00130_amd import binding
+    assert torch.cuda.is_available()
+    return binding
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).to("cuda")
+    return t if dtype is None else t.to(dtype)
+
+
+def values(rng, shape, dtype):
+    """Normal values as `dtype` holds them: (device tensor, the same numbers in numpy)."""
+    t = torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(TYPES[dtype])
+    return t.to("cuda"), t.to(torch.float64).numpy()
+
+
+def f64(t):
+    return t.cpu().to(torch.float64).numpy()
+
+
+def within(got, want, tol, what):
+    off = np.abs(got - want) > tol
+    assert not (off | ~np.isfinite(got)).any(), f"{what}: {off.sum()} of {got.size} beyond the bound, worst {np.max(np.abs(got - want) / np.maximum(tol, 1e-300)):.3g} times"
+
+
+# -------------------------------------------------------------------------------------------------------------- weights
+def weight(rng, N, K, group, dtype, bias):
+    W = rng.integers(0, 256, (N, (K + 1) // 2), dtype=np.uint8)
+    G = -(-K // group)
+    scale = torch.from_numpy((np.exp(rng.standard_normal((N, G)) * 0.5) * 0.05).astype(np.float32)).to(TYPES[dtype])
+    shift = torch.from_numpy((rng.standard_normal((N, G)) * 0.5).astype(np.float32)).to(TYPES[dtype]) if bias else None
+    return W, scale, shift
+
+
+@pytest.mark.parametrize("dtype,scale_dtype", [("bf16", "bf16"), ("f16", "f16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "f16"), ("f16", "bf16")])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_w4_products(b, dtype, scale_dtype, group):
+    sizes = [(1, 1, 1), (1, 16, 128), (2, 17, 31), (1, 100, 129), (16, 48, 257), (17, 33, 640), (5, 15, 33), (33, 70, 1000), (1, 5, 4099), (70, 20, 96)]
+    for case, (M, N, K) in enumerate(sizes):
+        rng = np.random.default_rng(1000 * group + case)
+        bias = case % 2 == 1
+        W, scale, shift = weight(rng, N, K, group, scale_dtype, bias)
+        # rows of X and Y further apart than they are long, and X off any wide alignment
+        xs, _ = values(rng, (M, K + 3), dtype)
+        x = xs[:, 1:K + 1] if case % 3 else xs[:, :K].contiguous()
+        y = torch.full((M, N + 2), 7.0, dtype=TYPES[dtype], device="cuda")
+        Wp = b.abft_w4_pack(dev(W), scale.cuda(), None if shift is None else shift.cuda(), K=K, group=group)
+        assert b.abft_w4_dims(Wp)[:3] == (N, K, group)
+        b.abft_w4_gemv(x, Wp, y[:, :N])
+        want, tol = o.w4_product(f64(x), W, f64(scale), None if shift is None else f64(shift), group, dtype)
+        within(f64(y[:, :N]), want, tol, f"{M}x{N}x{K} group {group}")
+        assert (y[:, N:] == 7.0).all()
+
+
+def test_w4_same_bits_any_batch_and_stream(b):
+    """A row's result does not depend on the rows beside it, nor on the stream or the call."""
+    rng = np.random.default_rng(5)
+    W, scale, shift = weight(rng, 130, 700, 64, "bf16", True)
+    Wp = b.abft_w4_pack(dev(W), scale.cuda(), shift.cuda(), K=700, group=64)
+    x, _ = values(rng, (16, 700), "bf16")
+    y = torch.empty((16, 130), dtype=torch.bfloat16, device="cuda")
+    b.abft_w4_gemv(x, Wp, y)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for m in (1, 7, 16):
+        z = torch.empty((m, 130), dtype=torch.bfloat16, device="cuda")
+        with torch.cuda.stream(s):
+            b.abft_w4_gemv(x[:m], Wp, z)
+        s.synchronize()
+        assert torch.equal(z.view(torch.int16), y[:m].view(torch.int16))
+    e = torch.empty((0, 130), dtype=torch.bfloat16, device="cuda")
+    b.abft_w4_gemv(x[:0], Wp, e)   # no rows
+
+
+def test_w4_infinities_stay_in_their_row(b):
+    rng = np.random.default_rng(6)
+    W, scale, _ = weight(rng, 40, 256, 128, "f32", False)
+    Wp = b.abft_w4_pack(dev(W), scale.cuda(), K=256)
+    x, xn = values(rng, (4, 256), "f32")
+    x[1, 7], x[2, 200] = float("inf"), float("nan")
+    y = torch.empty((4, 40), device="cuda")
+    b.abft_w4_gemv(x, Wp, y)
+    want, tol = o.w4_product(xn, W, f64(scale), None, 128, "f32")
+    got = f64(y)
+    within(got[[0, 3]], want[[0, 3]], tol[[0, 3]], "rows without infinities")
+    assert not np.isfinite(got[1:3]).any()
+
+
+def test_w4_refuses_what_does_not_fit(b):
+    W = torch.zeros((8, 64), dtype=torch.uint8, device="cuda")
+    s = torch.ones((8, 1), dtype=torch.bfloat16, device="cuda")
+    Wp = b.abft_w4_pack(W, s)
+    x, y = torch.zeros((2, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, 8), dtype=torch.bfloat16, device="cuda")
+    for bad in (lambda: b.abft_w4_gemv(x[:, :127], Wp, y), lambda: b.abft_w4_gemv(x, Wp, y[:1]), lambda: b.abft_w4_pack(W, s, K=125),
+                lambda: b.abft_w4_pack(W, s, K=128, group=64), lambda: b.abft_w4_pack(W, s, bias=s.float())):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: b.abft_w4_gemv(x.float(), Wp, y), lambda: b.abft_w4_gemv(x.int(), Wp, y), lambda: b.abft_w4_gemv(x.cpu(), Wp, y)):
+        with pytest.raises(TypeError):
+            bad()
+    with pytest.raises(b.AbftError):
+        b.abft_w4_pack(W, torch.ones((8, 3), dtype=torch.bfloat16, device="cuda"), group=48)
+
+
+# ------------------------------------------------------------------------------------------------------- tables and slots
+def run_plan(b, ctx, new, block, table, free, n_slots, pad=0):
+    R, width = table.shape
+    wide = np.full((R, width + pad), -5, np.int32)
+    wide[:, :width] = table
+    t = dev(wide)
+    i32 = lambda n: torch.full((n,), -77, dtype=torch.int32, device="cuda")
+    seq, cu, flags, taken = i32(R), i32(R + 1), i32(R), i32(1)
+    slots = torch.full((n_slots,), -77, dtype=torch.int64, device="cuda")
+    for _ in range(2):   # twice: the same again
+        b.abft_kv_plan(dev(np.asarray(ctx, np.int32)), dev(np.asarray(new, np.int32)), block, t[:, :width], dev(np.asarray(free, np.int32)), seq, cu, slots, flags, taken)
+    got = t.cpu().numpy()
+    assert (got[:, width:] == -5).all()
+    return got[:, :width], seq.cpu().numpy(), cu.cpu().numpy(), slots.cpu().numpy(), flags.cpu().numpy(), int(taken.item())
+
+
+@pytest.mark.parametrize("R,longest,new,block,width,short,slots_short", [
+    (1, 0, 1, 16, 4, 0, 0), (1, 100, 40, 16, 20, 0, 0), (3, 50, 70, 1, 130, 0, 0), (64, 4000, 1, 64, 64, 0, 0), (256, 100, 30, 16, 9, 0, 0),
+    (257, 300, 60, 32, 12, 0, 5), (700, 90, 9, 7, 15, 40, 0), (1500, 60, 20, 16, 5, 300, 700), (5000, 40, 4, 16, 4, 0, 0), (16384, 30, 2, 128, 1, 2000, 0)])
+def test_plan(b, R, longest, new, block, width, short, slots_short):
+    rng = np.random.default_rng(R + block)
+    ctx, fresh = rng.integers(0, longest + 1, R), rng.integers(0, new + 1, R)
+    if R > 100:
+        ctx[rng.integers(0, R, 3)] = -4
+        fresh[rng.integers(0, R, 3)] = -1
+    table = np.full((R, width), -1, np.int64)
+    ids = rng.permutation(R * width)
+    for r in range(R):
+        n = -(-max(int(ctx[r]), 0) // block)
+        table[r, :min(n, width)] = ids[r * width:r * width + min(n, width)]
+    c, f = np.maximum(ctx, 0), np.maximum(fresh, 0)
+    need = int((-(-(c + f) // block) + c // -block).sum())
+    free = 10 ** 6 + rng.permutation(max(0, need - short) + (0 if short else 3))
+    n_slots = max(0, int(f.sum()) - slots_short + (0 if slots_short else 4))
+    want_table = table.copy()
+    seq, cu, slots, flags, taken = o.plan(ctx, fresh, block, want_table, free, n_slots)
+    got = run_plan(b, ctx, fresh, block, table, free, n_slots, pad=R % 3)
+    for name, x, y in (("table", got[0], want_table), ("seq_len", got[1], seq), ("cu_new", got[2], cu), ("slots", got[3], slots), ("flags", got[4], flags)):
+        assert np.array_equal(x, y), name
+    assert got[5] == taken
+
+
+def test_plan_of_nothing_and_of_lengths_past_32_bits(b):
+    empty = torch.empty(0, dtype=torch.int32, device="cuda")
+    cu, taken = torch.full((1,), 5, dtype=torch.int32, device="cuda"), torch.full((1,), 5, dtype=torch.int32, device="cuda")
+    slots = torch.zeros(3, dtype=torch.int64, device="cuda")
+    b.abft_kv_plan(empty, empty, 16, empty.reshape(0, 4), empty, empty, cu, slots, empty, taken)
+    assert cu.tolist() == [0] and taken.tolist() == [0] and slots.tolist() == [-1] * 3
+    big = 2 ** 31 - 1
+    table = np.full((3, 2), -1)
+    want = o.plan([big, 0, 3], [big, 5, 2], 16, table.copy(), [8, 9], 0)      # (rows past 32 bits: every request is refused)
+    got = run_plan(b, [big, 0, 3], [big, 5, 2], 16, table, [8, 9], 0)
+    assert np.array_equal(got[1], want[0]) and np.array_equal(got[4], want[3]) and got[5] == 0 and (got[2] == 0).all()
+
+
+# ------------------------------------------------------------------------------------------------------------------ cache
+def make_cache(b, rng, n_blocks, heads, dim, block, small=1.0):
+    k, v = (np.clip(np.rint(rng.standard_normal((n_blocks, heads, block, dim)) * 40), -127, 127).astype(np.int8) for _ in range(2))
+    ks, vs = ((np.exp(rng.standard_normal((n_blocks, heads)) * 0.4) * 0.03 * small).astype(np.float32) for _ in range(2))
+    c = b.KvCache(n_blocks, heads, dim, block)
+    # whatever was never written may hold anything
+    c.k_codes.fill_(-128)
+    c.v_codes.fill_(77)
+    c.load_codes(dev(k), dev(v), dev(ks), dev(vs))
+    return c, k, v, ks, vs
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("heads,dim,block,fused", [(1, 64, 16, False), (2, 128, 64, True), (3, 80, 32, False), (2, 33, 128, True), (1, 256, 64, False), (5, 8, 16, True), (2, 1, 16, False)])
+def test_append_and_read(b, dtype, heads, dim, block, fused):
+    rng = np.random.default_rng(heads * 1000 + dim + block)
+    n_blocks = 9
+    c, k, v, ks, vs = make_cache(b, rng, n_blocks, heads, dim, block, small=0.02)
+    # runs of every kind, blocks out of order: a whole block, one token, the end of a block and the beginning of another, padding
+    runs = [(4, 0, block), (7, 3, 1), (2, block - 2, 2), (5, 0, 3), (0, 1, block - 1), (8, block - 1, 1), (1, 0, 1)]
+    slots = []
+    for i, (blk, first, n) in enumerate(runs):
+        slots += list(range(blk * block + first, blk * block + first + n))
+        if i % 2:
+            slots += [-1]
+    slots += [n_blocks * block, -7, 2 ** 40, 3 * block]
+    slots = np.array(slots, np.int64)
+    T = len(slots)
+    if fused:
+        rows, _ = values(rng, (T, 3 * heads * dim + 5), dtype)
+        kx = rows[:, heads * dim:2 * heads * dim].unflatten(1, (heads, dim))
+        vx = rows[:, 2 * heads * dim + 5:].unflatten(1, (heads, dim))
+    else:
+        kx, vx = (values(rng, (T, heads, dim), dtype)[0] for _ in range(2))
+    vx[min(5, T - 1), heads - 1, 0] = 100.0    # one value far above the others of its block
+    before = [x.copy() for x in (k, v)]
+    for codes, scale, x in ((k, ks, kx), (v, vs, vx)):
+        o.append(codes, scale, x.float().cpu().numpy(), slots)
+    for _ in range(2):    # the second time changes nothing
+        b.abft_kv_append(c, kx, vx, dev(slots))
+        gk, gv = (x.cpu().numpy() for x in c.codes())
+        assert np.array_equal(c.k_scale.cpu().numpy(), ks) and np.array_equal(c.v_scale.cpu().numpy(), vs)
+        # tokens behind a run are nobody's: all that lie before a run's end, and all blocks without one
+        for got, want, old in ((gk, k, before[0]), (gv, v, before[1])):
+            end = {blk: first + n for blk, first, n in runs + [(3, 0, 1)]}
+            for blk in range(n_blocks):
+                n = end.get(blk, block)
+                assert np.array_equal(got[blk, :, :n], want[blk, :, :n]), f"block {blk}"
+                if blk not in end:
+                    assert np.array_equal(want[blk], old[blk])
+    back = rng.permutation(np.concatenate([np.arange(n_blocks * block)[: 5 * block], [-1, n_blocks * block, 2 ** 45]])).astype(np.int64)
+    wide = torch.full((len(back), heads, dim + 3), 5.0, dtype=TYPES[dtype], device="cuda")
+    kb, vb = wide[:, :, :dim], torch.full((len(back), heads, dim), 5.0, dtype=TYPES[dtype], device="cuda")
+    b.abft_kv_read(c, dev(back), kb, vb)
+    for got, codes, scale in ((kb, gk, ks), (vb, gv, vs)):
+        want = torch.from_numpy(o.read(codes, scale, back).astype(np.float32)).to(TYPES[dtype])   # (code * scale is rounded to 32 bits first)
+        assert torch.equal(got.cpu(), want)
+    assert (wide[:, :, dim:] == 5.0).all()
+    only = torch.zeros_like(vb)
+    b.abft_kv_read(c, dev(back), None, only)
+    assert torch.equal(only, vb)
+
+
+def test_append_of_zeros_infinities_and_nan(b):
+    c = b.KvCache(3, 1, 64, 16)
+    k = np.zeros((3, 1, 16, 64), np.int8)
+    ks = np.zeros((3, 1), np.float32)
+    x = np.zeros((5, 1, 64), np.float32)
+    x[1, 0, :4] = [np.inf, -np.inf, np.nan, 2.0]
+    x[3, 0, 0] = 1e-44                         # a block whose largest value is far below the smallest scale
+    x[4, 0, :2] = [np.nan, np.inf]             # a block without a finite value other than zero
+    slots = np.array([0, 1, 2, 16, 32], np.int64)
+    o.append(k, ks, x, slots)
+    b.abft_kv_append(c, dev(x), dev(x), dev(slots))
+    gk, gv = c.codes()
+    assert np.array_equal(c.k_scale.cpu().numpy(), ks) and np.array_equal(c.v_scale.cpu().numpy(), ks)
+    for got in (gk.cpu().numpy(), gv.cpu().numpy()):
+        assert np.array_equal(got[0, :, :3], k[0, :, :3]) and np.array_equal(got[1, :, :1], k[1, :, :1]) and np.array_equal(got[2, :, :1], k[2, :, :1])
+    assert k[0, 0, 1, :4].tolist() == [127, -127, 0, 127] and ks[1, 0] == 2.0 ** -126
+
+
+def test_append_token_by_token_against_the_whole(b):
+    """A block filled token by token holds what the values are worth within one step of its scale for each time the scale grew."""
+    rng = np.random.default_rng(11)
+    heads, dim, block = 2, 64, 32
+    x, xn = values(rng, (block, heads, dim), "bf16")
+    one, all_at_once = b.KvCache(2, heads, dim, block), b.KvCache(2, heads, dim, block)
+    b.abft_kv_append(all_at_once, x, x, torch.arange(block, 2 * block, device="cuda"))
+    for t in range(block):
+        b.abft_kv_append(one, x[t:t + 1], x[t:t + 1], torch.tensor([block + t], device="cuda"))
+    assert torch.equal(one.k_scale, all_at_once.k_scale) and torch.equal(one.v_scale[1], all_at_once.v_scale[1])
+    grew = np.ones((heads,))
+    peak = np.abs(xn).max(2)
+    for h in range(heads):
+        grew[h] += (np.diff(np.maximum.accumulate(peak[:, h])) > 0).sum()
+    scale = one.k_scale[1].cpu().numpy().astype(np.float64)
+    for got in one.codes():
+        off = np.abs(got[1].cpu().numpy() * scale[:, None, None] - xn.transpose(1, 0, 2))
+        assert (off <= (0.5 + 0.5 * grew[:, None, None]) * scale[:, None, None] * (1 + 1e-6)).all()
+
+
+# -------------------------------------------------------------------------------------------------------------- attention
+def build(b, rng, lengths, fresh, q_heads, heads, dim, block, dtype, strided=False):
+    n = [-(-int(x) // block) for x in lengths]
+    n_blocks = sum(n) + 3
+    c, k, v, ks, vs = make_cache(b, rng, n_blocks, heads, dim, block)
+    ids = rng.permutation(n_blocks)
+    table = np.full((len(lengths), max(n) + 1), -1, np.int32)
+    at = 0
+    for r, m in enumerate(n):
+        table[r, :m] = ids[at:at + m]
+        at += m
+    cu = np.concatenate([[0], np.cumsum(fresh)]).astype(np.int32)
+    rows = int(cu[-1])
+    if strided:
+        wide, _ = values(rng, (rows, q_heads * dim + 3), dtype)
+        q = wide[:, 3:].unflatten(1, (q_heads, dim)) if rows else wide[:, 3:].reshape(0, q_heads, dim)
+    else:
+        q, _ = values(rng, (rows, q_heads, dim), dtype)
+    return c, (k, v, ks, vs), table, cu, q * 2
+
+
+def check(b, c, parts, table, lengths, cu, q, dtype, max_new, max_len, ws=True, scale=None, strided=False):
+    rows, q_heads, dim = q.shape
+    out = torch.full((rows, q_heads, dim + (3 if strided else 0)), 9.0, dtype=TYPES[dtype], device="cuda")
+    lse = torch.full((rows, q_heads), 9.0, device="cuda")
+    flags = torch.full((len(lengths),), 99, dtype=torch.int32, device="cuda")
+    work = b.KvWorkspace(c, len(lengths), q_heads, max_new, max_len).tensor if ws else None
+    if work is not None:
+        work.fill_(float("nan"))
+    b.abft_kv_attention(c, q, dev(table), dev(np.asarray(lengths, np.int32)), dev(cu), out[:, :, :dim], max_new, max_len, scale=scale, lse=lse, req_flags=flags, workspace=work)
+    want, tol, want_lse, lse_tol = o.attention(f64(q), *parts, table, lengths, cu, dim ** -0.5 if scale is None else scale, dtype)
+    got = f64(out[:, :, :dim])
+    within(got, want, tol, "attention")
+    assert (out[:, :, dim:] == 9.0).all()
+    none = np.isneginf(want_lse)
+    got_lse = f64(lse)
+    assert np.array_equal(np.isneginf(got_lse), none) and not got[none].any()
+    within(got_lse[~none], want_lse[~none], lse_tol[~none], "lse")
+    return out, flags.cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("dim,block", [(64, 16), (64, 64), (128, 64), (128, 32), (80, 16), (96, 128), (192, 64), (256, 32), (33, 64), (1, 16), (256, 128)])
+def test_attention_single_tokens(b, dtype, dim, block):
+    for heads, group in ((1, 1), (2, 4), (1, 16), (2, 7), (1, 20), (1, 40)):
+        rng = np.random.default_rng(dim + block + group)
+        lengths = [1, 0, 15, 16, 17, 63, 64, 65, 200, 257] if group == 4 else [3, 130, 66]
+        fresh = [1] * len(lengths)
+        c, parts, table, cu, q = build(b, rng, lengths, fresh, heads * group, heads, dim, block, dtype, strided=group == 7)
+        _, flags = check(b, c, parts, table, lengths, cu, q, dtype, 1, max(lengths), strided=group == 7)
+        assert not flags.any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,block,group", [(64, 32, 1), (128, 64, 4), (128, 16, 2), (192, 128, 3), (256, 16, 1)])
+def test_attention_several_new_tokens(b, dtype, dim, block, group):
+    for fresh, lengths in (([1, 3, 0, 5], [20, 3, 70, 140]), ([37, 1, 20, 2], [100, 64, 20, 1]), ([70, 0], [70, 5])):
+        # (one request has more new tokens than tokens: its first row sees nothing)
+        rng = np.random.default_rng(dim + group + len(fresh))
+        c, parts, table, cu, q = build(b, rng, lengths, fresh, 2 * group, 2, dim, block, dtype)
+        check(b, c, parts, table, lengths, cu, q, dtype, max(fresh), max(lengths))
+
+
+@pytest.mark.parametrize("block", [16, 64])
+def test_attention_in_parts_with_any_workspace_and_any_hint(b, block):
+    """Long requests are cut; sizes that are only hints, and too small a workspace, change the cut and not the result."""
+    rng = np.random.default_rng(block)
+    lengths, fresh = [1500, 3, 700, 0, 1025], [1, 1, 2, 1, 1]
+    c, parts, table, cu, q = build(b, rng, lengths, fresh, 8, 2, 128, block, "bf16")
+    assert b.abft_kv_attention_workspace_bytes(c, 5, 8, 2, 1500) > 0
+    for max_new, max_len, ws in ((2, 1500, True), (2, 1500, False), (1, 300, True), (1, 1, False), (9, 40000, True), (300, 1500, True)):
+        check(b, c, parts, table, lengths, cu, q, "bf16", max_new, max_len, ws)
+    small = torch.empty(abs(b.abft_kv_attention_workspace_bytes(c, 5, 8, 2, 1500)) // 4 // 2, device="cuda")
+    out = torch.empty_like(q)
+    b.abft_kv_attention(c, q, dev(table), dev(np.asarray(lengths, np.int32)), dev(cu), out, 2, 1500, workspace=small)
+    want, tol, _, _ = o.attention(f64(q), *parts, table, lengths, cu, 128 ** -0.5, "bf16")
+    within(f64(out), want, tol, "half a workspace")
+
+
+def test_attention_same_bits_every_time_and_on_another_stream(b):
+    rng = np.random.default_rng(8)
+    lengths = [900, 40, 2000]
+    c, parts, table, cu, q = build(b, rng, lengths, [1, 1, 1], 8, 2, 64, 64, "f16")
+    first, _ = check(b, c, parts, table, lengths, cu, q, "f16", 1, 2000)
+    s = torch.cuda.Stream()
+    t, n, u = dev(table), dev(np.asarray(lengths, np.int32)), dev(cu)
+    ws = b.KvWorkspace(c, 3, 8, 1, 2000).tensor
+    s.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        out = torch.zeros_like(q)
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            b.abft_kv_attention(c, q, t, n, u, out, 1, 2000, workspace=ws)
+        s.synchronize()
+        assert torch.equal(out.view(torch.int16), first.view(torch.int16))
+
+
+@pytest.mark.parametrize("block", [16, 128])
+def test_attention_leaves_out_blocks_that_do_not_exist(b, block):
+    rng = np.random.default_rng(9)
+    lengths = [300, 300, 100]
+    c, parts, table, cu, q = build(b, rng, lengths, [1, 1, 1], 4, 2, 64, block, "f32")
+    table[0, 1], table[2, :] = c.n_blocks + 5, -1
+    _, flags = check(b, c, parts, table, lengths, cu, q, "f32", 1, 300)
+    assert flags.tolist() == [b.ABFT_KV_BAD_BLOCK, 0, b.ABFT_KV_BAD_BLOCK]
+
+
+@pytest.mark.parametrize("block", [16, 64])
+def test_attention_takes_nothing_from_what_it_does_not_see(b, block):
+    """Scales of blocks that no row of a request sees are NaN, and codes past the lengths are at their lowest."""
+    rng = np.random.default_rng(10)
+    lengths, fresh = [70, 33], [40, 1]
+    c, parts, table, cu, q = build(b, rng, lengths, fresh, 4, 2, 64, block, "f32")
+    used = set()
+    for r, n in enumerate(lengths):
+        used |= {int(x) for x in table[r, : -(-n // block)]}
+    free = [x for x in range(c.n_blocks) if x not in used]
+    for t in (c.k_scale, c.v_scale):
+        t[torch.tensor(free, device="cuda")] = float("nan")
+    table[0, -1] = free[0]
+    check(b, c, parts, table, lengths, cu, q, "f32", 40, 70)
+    # a row with an infinity or a NaN in its query gives NaN, the others what they did
+    q[3, 1, 5], q[7, 0, 0] = float("inf"), float("nan")
+    out = torch.empty_like(q)
+    b.abft_kv_attention(c, q, dev(table), dev(np.asarray(lengths, np.int32)), dev(cu), out, 40, 70)
+    got = f64(out)
+    bad = np.zeros(got.shape[:2], bool)
+    bad[3, 1] = bad[7, 0] = True
+    assert np.isnan(got[bad]).all() and np.isfinite(got[~bad]).all()
+    # a NaN scale of the second block: the rows that see none of it stay
+    if block == 64:
+        c.v_scale[int(table[0, 1])] = float("nan")
+        b.abft_kv_attention(c, q, dev(table), dev(np.asarray(lengths, np.int32)), dev(cu), out, 40, 70)
+        again = f64(out)
+        assert np.array_equal(again[:34][~bad[:34]], got[:34][~bad[:34]]) and np.isnan(again[34:40]).all()
+
+
+def test_attention_large_and_small_scales(b):
+    """Scores that leave one token standing, blocks whose values differ by ten orders of magnitude, blocks of zeros."""
+    rng = np.random.default_rng(12)
+    for block in (16, 64):
+        lengths = [200, 150]
+        c, parts, table, cu, q = build(b, rng, lengths, [1, 2], 4, 1, 64, block, "f32")
+        k, v, ks, vs = parts
+        vs[int(table[0, 0])], vs[int(table[0, 1])], vs[int(table[1, 1])], ks[int(table[1, 0])] = 1e6, 1e-6, 0.0, 0.0
+        c.load_codes(dev(k), dev(v), dev(ks), dev(vs))
+        for scale in (None, 5.0, -0.3, 1e-6):
+            check(b, c, parts, table, lengths, cu, q, "f32", 2, 200, scale=scale)
+
+
+def test_attention_refuses_what_does_not_fit(b):
+    c = b.KvCache(4, 2, 64, 16)
+    q = torch.zeros((1, 4, 64), dtype=torch.bfloat16, device="cuda")
+    t, n, u = (torch.zeros(s, dtype=torch.int32, device="cuda") for s in ((1, 4), (1,), (2,)))
+    call = lambda **kw: b.abft_kv_attention(**{**dict(cache=c, Q=q, table=t, seq_len=n, cu_new=u, O=torch.zeros_like(q), max_new=1, max_len=64), **kw})
+    for bad in (dict(Q=q[:, :, :63]), dict(O=torch.zeros_like(q)[:, :2]), dict(table=t.expand(2, 4)), dict(cu_new=u[:1]), dict(lse=torch.zeros(3, device="cuda"))):
+        with pytest.raises(ValueError):
+            call(**bad)
+    for bad in (dict(Q=q.float()), dict(Q=q.cpu()), dict(table=t.long())):
+        with pytest.raises(TypeError):
+            call(**bad)
+    for bad in (dict(Q=q[:, :3], O=torch.zeros_like(q)[:, :3]), dict(max_new=0), dict(scale=float("nan"))):
+        with pytest.raises(b.AbftError):
+            call(**bad)
+    with pytest.raises(ValueError):
+        b.KvCache(4, 2, 64, 24)
+    with pytest.raises(ValueError):
+        b.abft_kv_append(c, q, q, torch.zeros(1, dtype=torch.int64, device="cuda"))
+    with pytest.raises(TypeError):
+        b.abft_kv_append(c, q[:, :2], q[:, :2].float(), torch.zeros(1, dtype=torch.int64, device="cuda"))
+    call()   # a request of no tokens and no rows
