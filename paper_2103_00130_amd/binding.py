@@ -3,9 +3,9 @@
 Argument marshalling only.  torch tensors supply device memory and the current
 stream; every step of the method runs in the HIP kernels behind the C ABI.
 Importing this module fails loudly when the library has not been built
-(`python -m paper_2103_00130_amd.build`): there is no fallback path.  The two calls
-of a serving loop, the checked GEMM and the checked lookup, are marshalled natively
-(csrc/fastcall.cpp); operands that it does not take - and so every wrong one - go
+(`python -m paper_2103_00130_amd.build`): there is no fallback path.  The calls
+of a serving loop, the checked GEMM, the checked lookup and those of a decoding step, are
+marshalled natively (csrc/fastcall.cpp); operands that it does not take - and so every wrong one - go
 through the Python code that follows, which says what is wrong with them.
 """
 from __future__ import annotations
@@ -139,7 +139,8 @@ try:
     from . import _fastcall
 except ImportError as e:
     raise ImportError(f"{e}: build it with `python -m paper_2103_00130_amd.build`") from e
-_fastcall.bind(ctypes.cast(lib.abft_gemm_u8s8s32_checked, ctypes.c_void_p).value, ctypes.cast(lib.abft_eb_u8_checked, ctypes.c_void_p).value,
+_fastcall.bind([ctypes.cast(f, ctypes.c_void_p).value for f in (lib.abft_gemm_u8s8s32_checked, lib.abft_eb_u8_checked, lib.abft_w4_gemv, lib.abft_kv_plan,
+                                                                 lib.abft_kv_append, lib.abft_kv_read, lib.abft_kv_attention)],
                torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
 
 
@@ -582,6 +583,11 @@ def abft_w4_dims(Wp: W4Weight):
 
 def abft_w4_gemv(X: torch.Tensor, Wp: W4Weight, Y: torch.Tensor, stream=None):
     """Y = X W^T: X M x K, Y M x N, both float32, float16 or bfloat16."""
+    rc = _fastcall.w4(X, Wp.handle, Wp.N, Wp.K, Y, stream)
+    if rc is not None:
+        if rc != ABFT_OK:
+            _check(rc)
+        return
     x_ptr, x_type = _typed(X, "X")
     y_ptr, y_type = _typed(Y, "Y")
     ldx, ldy = _ld(X, "X"), _ld(Y, "Y")
@@ -608,6 +614,7 @@ class KvCache:
         self.v_scale = torch.zeros((self.n_blocks, self.heads), dtype=torch.float32, device=device)
         self.struct = abft_kv_cache_t(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(), *self._sizes())
         self.ref = ctypes.byref(self.struct)
+        self.address = ctypes.addressof(self.struct)
 
     def _sizes(self):
         return self.n_blocks, self.heads, self.head_dim, self.block_tokens
@@ -627,6 +634,11 @@ class KvCache:
 def abft_kv_plan(ctx_len, new_len, block_tokens: int, table, free_blocks, seq_len, cu_new, slots, req_flags, taken, stream=None):
     """Block tables and slots of a step; table (int32, requests x blocks) is extended in place, seq_len, cu_new, slots (int64),
     req_flags and taken are overwritten."""
+    rc = _fastcall.plan(ctx_len, new_len, block_tokens, table, free_blocks, seq_len, cu_new, slots, req_flags, taken, stream)
+    if rc is not None:
+        if rc != ABFT_OK:
+            _check(rc)
+        return
     R = ctx_len.numel()
     if table.dim() != 2 or table.shape[0] != R:
         raise ValueError("table must be 2-D with a row for each request")
@@ -648,6 +660,11 @@ def _kv_rows(t, cache, n, name, heads=None):
 
 def abft_kv_append(cache: KvCache, K, V, slots, stream=None):
     """Quantizes K and V (tokens x heads x head_dim) into the cache at `slots` (int64, as abft_kv_plan gives them)."""
+    rc = _fastcall.append(cache.address, cache.heads, cache.head_dim, K, V, slots, stream)
+    if rc is not None:
+        if rc != ABFT_OK:
+            _check(rc)
+        return
     T = slots.numel()
     _, k_type = _typed(K, "K")
     _, v_type = _typed(V, "V")
@@ -659,6 +676,11 @@ def abft_kv_append(cache: KvCache, K, V, slots, stream=None):
 
 def abft_kv_read(cache: KvCache, slots, K=None, V=None, stream=None):
     """The tokens at `slots` as values, into K and V (tokens x heads x head_dim); either may be None."""
+    rc = _fastcall.read(cache.address, cache.heads, cache.head_dim, slots, K, V, stream)
+    if rc is not None:
+        if rc != ABFT_OK:
+            _check(rc)
+        return
     T = slots.numel()
     types = {_typed(t, name)[1] for t, name in ((K, "K"), (V, "V")) if t is not None}
     if len(types) > 1:
@@ -685,6 +707,13 @@ def abft_kv_attention(cache: KvCache, Q, table, seq_len, cu_new, O, max_new: int
                       req_flags=None, workspace=None, stream=None):
     """Attention of the rows of Q (new tokens x query heads x head_dim) over their requests' tokens, into O.  scale: 1 / sqrt(head_dim)
     unless given."""
+    if scale is None:
+        scale = cache.head_dim ** -0.5
+    rc = _fastcall.attention(cache.address, cache.head_dim, Q, table, seq_len, cu_new, O, max_new, max_len, scale, lse, req_flags, workspace, stream)
+    if rc is not None:
+        if rc != ABFT_OK:
+            _check(rc)
+        return
     if Q.dim() != 3 or table.dim() != 2:
         raise ValueError("Q must be rows x query heads x head_dim and table requests x blocks")
     n_rows, q_heads = Q.shape[:2]
@@ -699,7 +728,7 @@ def abft_kv_attention(cache: KvCache, Q, table, seq_len, cu_new, O, max_new: int
     _check(lib.abft_kv_attention(
         cache.ref, *_kv_rows(Q, cache, n_rows, "Q", q_heads), q_type, n_rows, q_heads, _ptr(table, torch.int32, "table"),
         max(_ld(table, "table"), table.shape[1]), table.shape[1], _entries(seq_len, torch.int32, R, "seq_len"),
-        _entries(cu_new, torch.int32, R + 1, "cu_new"), R, int(max_new), int(max_len), cache.head_dim ** -0.5 if scale is None else float(scale),
+        _entries(cu_new, torch.int32, R + 1, "cu_new"), R, int(max_new), int(max_len), float(scale),
         *_kv_rows(O, cache, n_rows, "O", q_heads), None if lse is None else _entries(lse, torch.float32, n_rows * q_heads, "lse"),
         None if req_flags is None else _entries(req_flags, torch.int32, R, "req_flags"), None if workspace is None else workspace.data_ptr(),
         ws_bytes, _stream(stream)))

@@ -14,7 +14,7 @@ SOURCES = ["api.hip", "pack.hip", "gemm_tile.hip", "gemm_tile_a256.hip", "gemm_t
            "gemm_tile_a128.hip", "gemm_tile_a64.hip", "gemm_tile_a64r4.hip", "gemm_tile_a64s.hip", "gemm_tile_g64.hip", "gemm_smallm.hip",
            "gemm_tile_wk32x32w4.hip", "gemm_tile_wk32x32w8.hip", "gemm_tile_wk32x32w8s.hip", "gemm_tile_wk32x64w4.hip", "gemm_tile_wk32x64w8.hip", "gemm_tile_wk64x64w4.hip",
            "rowops.hip", "locate.hip", "eb.hip",
-           "w4.hip", "kv_plan.hip", "kv_cache.hip", "kv_attention.hip", "kv_attention_f32.hip", "kv_attention_f16.hip", "kv_attention_bf16.hip"]
+           "w4.hip", "w4_f32.hip", "w4_f16.hip", "w4_bf16.hip", "kv_plan.hip", "kv_cache.hip", "kv_attention.hip", "kv_attention_f32.hip", "kv_attention_f16.hip", "kv_attention_bf16.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Wno-inline-asm",
@@ -63,7 +63,7 @@ def _build(force, verbose, build_dir, lib, extra) -> str:
 
 
 def build_fastcall(force: bool = True) -> str:
-    """_fastcall.so: the native marshalling that binding.py uses for the two calls of a serving loop (host code only)."""
+    """_fastcall.so: the native marshalling that binding.py uses for the calls of a serving loop (host code only)."""
     import sysconfig
 
     import torch

@@ -19,7 +19,13 @@
 //  * A request longer than a part (params.chunk) is cut into parts, each a workgroup; a second kernel joins them.
 //
 // Scales of a block: that of the keys multiplies the scores.  That of the values multiplies what a tile adds to the sums; where a
-// block is smaller than a tile, the numerators instead, before they become digits.
+// block is smaller than a tile, it is part of the factor that makes numerators digits (the numerators of a lane are of 16
+// neighbouring tokens, so of one block), which are then relative to the largest numerator times scale.
+//
+// The vector instructions that are left for each score: two to make it a float, one for the maximum, one multiply-add and an exp2,
+// one for the sum, 2.75 to make it digits; for each sum of values two to make it a float and one multiply-add.  The sums are
+// relative to a maximum that is only moved when a row's largest score has grown by more than 2^kSlack, which spares their
+// multiplication for nearly every tile.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -46,17 +52,21 @@ struct AttnParams {
     int n_blocks, heads, q_heads, group, dim, block_shift, width, n_req;
     int parts, chunk;   // a part is `chunk` tokens, a multiple of 256; the last takes what is left
     float scale2;       // the scale of the scores, times log2(e)
-    bool q_wide;        // rows of Q in pieces of 16 bytes
+    bool q_wide;        // rows of Q are whole aligned pieces of 16 bytes
 };
 
 // which kernel (one for each of them and each type, number of columns and kind of block)
 enum AttnShape {
     kAttnTokens1,   // up to 16 rows, tokens split among the wavefronts
-    kAttnTokens2,   // up to 32, up to 128 columns (beyond, a wavefront's sums do not fit its registers)
+    kAttnTokens2,   // up to 32, where a wavefront holds that many
     kAttnRows       // rows split among the wavefronts
 };
-// rows of a tile's wavefront x 16 that kAttnRows takes
-constexpr int attn_rows_tiles(int cols) { return cols <= 128 ? 2 : 1; }
+// Most rows of a wavefront, in sixteens.  More do not fit its registers, and a kernel that spills is not to be had: the compiler has put
+// the copy of a spilled register before the end of a divergent branch, where not every lane made it.
+constexpr int attn_rows_tiles(int digits, int cols) { return cols <= (digits == 2 ? 128 : 64) ? 2 : 1; }
+// Wavefronts that are to share a SIMD's registers.
+constexpr int attn_waves(int digits, int cols) { return cols <= (digits == 2 ? 128 : 64) ? 2 : 1; }
+constexpr int attn_digits(int type_size) { return type_size == 4 ? 3 : 2; }
 
 hipError_t launch_attention_f32(AttnShape shape, int cols, bool small_blocks, const AttnParams& p, dim3 grid, hipStream_t s);
 hipError_t launch_attention_f16(AttnShape shape, int cols, bool small_blocks, const AttnParams& p, dim3 grid, hipStream_t s);
@@ -69,6 +79,7 @@ typedef uint32_t attn_v4u __attribute__((ext_vector_type(4)));
 typedef float attn_v4f __attribute__((ext_vector_type(4)));
 
 constexpr int kAttnTile = kKvTile;
+constexpr float kSlack = 12.0f;   // (a sum of 2^31 numerators of 2^12 is far from binary32's end)
 
 // over the lanes l % 16, + 16, + 32, + 48
 __device__ inline float max_of_four(float v) {
@@ -82,6 +93,13 @@ __device__ inline float sum_of_four(float v) {
     v = __builtin_bit_cast(float, (uint32_t)a[0]) + __builtin_bit_cast(float, (uint32_t)a[1]);
     const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
     return __builtin_bit_cast(float, (uint32_t)b[0]) + __builtin_bit_cast(float, (uint32_t)b[1]);
+}
+
+// The same number, of which the compiler knows nothing: what depends on it is computed where it is used, not ahead of a loop in
+// which it would hold registers.
+__device__ inline int here_only(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
 }
 
 // The byte `which` (0, 1, 2) of four words, side by side.
@@ -128,15 +146,18 @@ __device__ inline float meet(const v4i (&acc)[ND], int i) {
 }
 
 template <typename T, int COLS, int RT, bool SMALL, bool BY_ROWS>
-__global__ __launch_bounds__(256) void kv_attention_kernel(const AttnParams p) {
-    constexpr int ND = sizeof(T) == 4 ? 3 : 2;
+__global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), RT * COLS)) void kv_attention_kernel(const AttnParams p) {
+    constexpr int ND = attn_digits(sizeof(T));
     constexpr int KC = COLS / 64, VT = COLS / 16;
     constexpr int kRows = RT * 16 * (BY_ROWS ? 4 : 1);         // rows of a workgroup
     constexpr int kStep = kAttnTile * (BY_ROWS ? 1 : 4);       // tokens that it takes at a time
     constexpr int kPitch = COLS + 4;
+    __shared__ v4i s_q[kRows / 16][KC][ND][64];                // digits of the rows, as the lanes of a product take them
+    __shared__ float s_q_scale[kRows];
+    __shared__ int s_token[kRows], s_head[kRows], s_limit[kRows];   // of a row: new token (-1: no such row), query head, last position it sees
     __shared__ float s_o[BY_ROWS ? 1 : 4 * 16 * kPitch];
     __shared__ float s_m[4][16], s_l[4][16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lq = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15, lq = lane >> 4;
     const int head = blockIdx.y, req = blockIdx.z, part = blockIdx.x % p.parts, first_group = blockIdx.x / p.parts, groups = gridDim.x / p.parts;
     const int block_tokens = 1 << p.block_shift;
 
@@ -145,7 +166,7 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnParams p) {
     const int len = (int)len64;
     const int64_t c0 = min((int64_t)max(p.cu_new[req], 0), p.n_rows), c1 = min(max((int64_t)p.cu_new[req + 1], c0), p.n_rows);
     const int fresh = (int)(c1 - c0);
-    const int64_t rows = (int64_t)fresh * p.group;
+    const int rows = fresh * p.group;   // (n_rows * q_heads is below 2^31)
     const int32_t* const table = p.table + (int64_t)req * p.ldt;
     // parts that this request has: what lies past the last one's chunk is the last one's too
     const int mine = len <= 0 ? 1 : min(p.parts, (len + p.chunk - 1) / p.chunk);
@@ -153,57 +174,80 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnParams p) {
     bool bad_block = false;
 
     for (int64_t row0 = (int64_t)first_group * kRows; row0 < rows; row0 += (int64_t)groups * kRows) {
-        // ---- this wavefront's rows: where each may look, and its query as digits
-        int limit[RT];
-        int64_t q_row[RT];   // token * q_heads + query head, or -1
-        float q_scale[RT];
-        v4i qd[RT][KC][ND];
-        int last = -1;       // the last position that any of them sees
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const int64_t row = row0 + (BY_ROWS ? wave * RT * 16 : 0) + rt * 16 + lr;
+        // ---- the rows, once for the workgroup: sixteen threads a row, sixteen columns a thread
+        __syncthreads();
+#pragma unroll 1
+        for (int tile = 0; tile < kRows / 16; ++tile) {
+            const int tid = here_only(threadIdx.x), row16 = tid >> 4, at = tile * 16 + row16, pc = tid & 15, d = 16 * pc;
+            const int64_t row = row0 + at;
             const bool real = row < rows;
-            const int i = real ? (int)(row / p.group) : 0, qh = head * p.group + (real ? (int)(row - (int64_t)i * p.group) : 0);
-            q_row[rt] = real ? (c0 + i) * p.q_heads + qh : -1;
-            limit[rt] = real ? len - fresh + i : len - 1;
-            if (real) last = max(last, limit[rt]);
+            const int i = real ? (int)((uint32_t)row / (uint32_t)p.group) : 0, qh = head * p.group + (real ? (int)row - i * p.group : 0);
             const T* const q = static_cast<const T*>(p.Q) + (c0 + i) * p.q_token + qh * p.q_head;
-            float x[KC][16], most = 0.0f;
-            bool finite = true;
+            // (every thread loads, from columns that exist, whatever its own are)
+            float x[16];
+            if (p.q_wide) {
+                constexpr int PER = 16 / sizeof(T);
+                typedef T piece __attribute__((ext_vector_type(PER)));
 #pragma unroll
-            for (int c = 0; c < KC; ++c) {
-                const int d = 64 * c + 16 * lq;
-                if (d + 16 <= p.dim) {
-                    load_values<T, 16>(x[c], q + d, p.q_wide);
-                } else {
+                for (int k = 0; k < 16 / PER; ++k) {
+                    const piece v = *reinterpret_cast<const piece*>(q + min(d + PER * k, p.dim - PER));
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) x[c][j] = d + j < p.dim ? to_f32(q[d + j]) : 0.0f;
+                    for (int j = 0; j < PER; ++j) x[PER * k + j] = d + PER * k < p.dim ? to_f32((T)v[j]) : 0.0f;
                 }
+            } else {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const float a = fabsf(x[c][j]);
-                    most = fmaxf(most, a);
-                    finite = finite && a < INFINITY;
+                    const float v = to_f32(q[min(d + j, p.dim - 1)]);
+                    x[j] = d + j < p.dim ? v : 0.0f;
                 }
             }
-            most = max_of_four(finite ? most : INFINITY);   // (an infinity or a NaN makes the row's scores NaN)
-            const float one = Fixed<ND, true>::kOne;
-            const bool some = most >= 0x1p-100f && most < INFINITY;
-            const float inv = some ? one / most : 0.0f;
-            q_scale[rt] = most < INFINITY ? most / one * p.scale2 : NAN;
+            float most = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float a = fabsf(x[j]);
+                most = a < INFINITY ? fmaxf(most, a) : INFINITY;   // (an infinity or a NaN makes the row's scores NaN)
+                x[j] = a < INFINITY ? x[j] : 0.0f;
+            }
+#pragma unroll
+            for (int m = 1; m < 16; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+            constexpr float one = Fixed<ND, true>::kOne;
+            const float inv = most >= 0x1p-100f && most < INFINITY ? __builtin_copysignf(one / most, p.scale2) : 0.0f;   // (a score's factor is not negative)
+            v4i digits[ND];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t digit[ND];
+                four_digits<ND, true>(x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3], inv, digit);
+#pragma unroll
+                for (int t = 0; t < ND; ++t) digits[t][w] = (int)digit[t];
+            }
+            if (d < COLS)
+#pragma unroll
+                for (int t = 0; t < ND; ++t) s_q[tile][pc / 4][t][pc % 4 * 16 + row16] = digits[t];
+            if (pc == 0) {
+                s_q_scale[at] = most < INFINITY ? most / one * fabsf(p.scale2) : NAN;
+                s_token[at] = real ? (int)(c0 + i) : -1;
+                s_head[at] = qh;
+                s_limit[at] = real ? len - fresh + i : len - 1;
+            }
+        }
+        __syncthreads();
+        // ---- this wavefront's rows
+        const int wave_rows = BY_ROWS ? wave * RT * 16 : 0;
+        int limit[RT];
+        float q_scale[RT];
+        v4i qd[RT][KC][ND];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            limit[rt] = s_limit[wave_rows + rt * 16 + lr];
+            q_scale[rt] = s_q_scale[wave_rows + rt * 16 + lr];
 #pragma unroll
             for (int c = 0; c < KC; ++c)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    uint32_t digit[ND];
-                    four_digits<ND, true>(some ? x[c][4 * w] : 0.0f, some ? x[c][4 * w + 1] : 0.0f, some ? x[c][4 * w + 2] : 0.0f, some ? x[c][4 * w + 3] : 0.0f, inv, digit);
-#pragma unroll
-                    for (int t = 0; t < ND; ++t) qd[rt][c][t][w] = (int)digit[t];
-                }
+                for (int t = 0; t < ND; ++t) qd[rt][c][t] = s_q[wave_rows / 16 + rt][c][t][lane];
         }
-        // (rows count up with positions: the last lane's last row sees most; all lanes of a wavefront agree)
-#pragma unroll
-        for (int m = 1; m < 16; m *= 2) last = max(last, __shfl_xor(last, m));
+        // the last position that any of them sees: that of the last row
+        const int64_t past = min(row0 + wave_rows + RT * 16, (int64_t)rows);
+        const int last = past > row0 + wave_rows ? len - fresh + (int)((uint32_t)(past - 1) / (uint32_t)p.group) : -1;
 
         float top[RT], sum[RT];
         attn_v4f o[RT][VT];
@@ -216,47 +260,58 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnParams p) {
         }
 
         const int begin = part * p.chunk, end = min(part == mine - 1 ? len : begin + p.chunk, last + 1);
-        // Blocks of a tile: where a tile lies within one block, that one; else those of its groups of 16 tokens as the lane needs
-        // them, for K those of group lr / 4, else of group lq.
-        constexpr int kApart = SMALL ? 16 : 0;
-        auto block_of = [&](int t) __attribute__((always_inline)) {
-            return t < len ? table[t >> p.block_shift] : -1;
+        // Blocks of a tile: where a tile lies within one block, that one (in scalar registers); else those of its groups of 16 tokens
+        // as the lane needs them, for K those of group lr / 4, else of group lq.
+        struct Blocks {
+            int k, v;
         };
-        int t0 = begin + (BY_ROWS ? 0 : wave * kAttnTile);
-        int id_k = -1, id_v = -1;
+        auto block_of = [&](int t) __attribute__((always_inline)) { return t < len ? table[t >> p.block_shift] : -1; };
+        auto blocks_of = [&](int t) __attribute__((always_inline)) {
+            Blocks x;
+            if constexpr (SMALL) {
+                x.k = block_of(t + 16 * (lr >> 2));
+                x.v = block_of(t + 16 * lq);
+            } else {
+                x.k = x.v = __builtin_amdgcn_readfirstlane(block_of(t));
+            }
+            return x;
+        };
+        auto exists = [&](int id) __attribute__((always_inline)) { return (uint32_t)id < (uint32_t)p.n_blocks; };
+        const int64_t block_bytes = (int64_t)COLS << p.block_shift;   // of one head
+        const int k_lane = (SMALL ? (lr & 3) : 16 * (lr >> 2) + (lr & 3)) * COLS + 16 * lq;
+        const int v_lane = (SMALL ? 0 : lq * COLS * kKvGroup) + lr * 16;
         v4i kf[4][KC];
         auto load_k = [&](int id, int t) __attribute__((always_inline)) {
-            const int64_t b = (uint32_t)id < (uint32_t)p.n_blocks ? id : 0;
-            const int off = ((t + 16 * (lr >> 2)) & (block_tokens - 1)) + (lr & 3);
-            const int8_t* const at = p.k_codes + ((b * p.heads + head) * block_tokens + off) * COLS + 16 * lq;
+            const int64_t b = exists(id) ? id : 0;
+            const int off = (SMALL ? t + 16 * (lr >> 2) : t) & (block_tokens - 1);
+            const int8_t* const at = p.k_codes + (b * p.heads + head) * block_bytes + off * COLS;
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll
-                for (int c = 0; c < KC; ++c) kf[s][c] = *reinterpret_cast<const v4i*>(at + 4 * s * COLS + 64 * c);
+                for (int c = 0; c < KC; ++c) kf[s][c] = *reinterpret_cast<const v4i*>(at + k_lane + (4 * s * COLS + 64 * c));
         };
+        int t0 = begin + (BY_ROWS ? 0 : wave * kAttnTile);
+        Blocks now = {-1, -1};
         if (t0 < end) {
-            id_k = block_of(t0 + kApart * (lr >> 2));
-            id_v = block_of(t0 + kApart * lq);
-            load_k(id_k, t0);
+            now = blocks_of(t0);
+            load_k(now.k, t0);
         }
         for (; t0 < end; t0 += kStep) {
-            const bool here = (uint32_t)id_v < (uint32_t)p.n_blocks;
-            if (!here && t0 + kApart * lq < len) bad_block = true;
-            const int64_t bv = here ? id_v : 0;
-            const int64_t block_head = bv * p.heads + head;
-            const float ks = here ? p.k_scale[block_head] : 0.0f, vs = here ? p.v_scale[block_head] : 0.0f;
+            const bool here = exists(now.v);
+            if (!here && t0 + (SMALL ? 16 * lq : 0) < len) bad_block = true;
+            const int64_t block_head = (int64_t)(here ? now.v : 0) * p.heads + head;
+            const float ks = p.k_scale[block_head], vs = p.v_scale[block_head];   // (of block 0 where there is none: nothing is seen of it)
             v4i vf[VT];
             {
-                const int g = ((t0 + 16 * lq) & (block_tokens - 1)) / kKvGroup;
-                const int8_t* const at = p.v_codes + (block_head * (block_tokens / kKvGroup) + g) * (COLS * kKvGroup) + lr * 16;
+                const int off = (SMALL ? t0 + 16 * lq : t0) & (block_tokens - 1);
+                const int8_t* const at = p.v_codes + block_head * block_bytes + off * COLS;
 #pragma unroll
-                for (int t = 0; t < VT; ++t) vf[t] = *reinterpret_cast<const v4i*>(at + t * 256);
+                for (int t = 0; t < VT; ++t) vf[t] = *reinterpret_cast<const v4i*>(at + v_lane + t * 256);
             }
-            // ---- scores, base 2
+            // ---- scores, as sums of digit products
             float z[RT][16];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const float f = q_scale[rt] * ks;
+            for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     v4i acc[ND];
@@ -267,48 +322,51 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnParams p) {
                         for (int c = 0; c < KC; ++c) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[s][c], qd[rt][c][t], acc[t], 0, 0, 0);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z[rt][4 * s + i] = meet<ND>(acc, i) * f;
+                    for (int i = 0; i < 4; ++i) z[rt][4 * s + i] = meet<ND>(acc, i);
                 }
-            }
             // ---- the next tile's keys are on their way from here on
             const int tn = t0 + kStep;
             if (tn < end) {
-                id_k = block_of(tn + kApart * (lr >> 2));
-                id_v = block_of(tn + kApart * lq);
-                load_k(id_k, tn);
+                now = blocks_of(tn);
+                load_k(now.k, tn);
             }
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
+                float f = q_scale[rt] * ks;   // makes a score of a sum, base 2
                 if (!__all(here && t0 + kAttnTile - 1 <= limit[rt])) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) z[rt][j] = here && t0 + 16 * lq + j <= limit[rt] ? z[rt][j] : -INFINITY;
+                    for (int j = 0; j < 16; ++j) z[rt][j] = here && t0 + 16 * lq + j <= limit[rt] ? z[rt][j] * f : -INFINITY;
+                    f = 1.0f;
                 }
-                float most = z[rt][0];
+                float mine_most = z[rt][0];
 #pragma unroll
-                for (int j = 1; j < 16; ++j) most = fmaxf(most, z[rt][j]);
-                most = max_of_four(most);
-                const float ref = most == -INFINITY ? 0.0f : most;
+                for (int j = 1; j < 16; ++j) mine_most = fmaxf(mine_most, z[rt][j]);
+                mine_most *= f;
+                const float most = max_of_four(mine_most), ref = most == -INFINITY ? 0.0f : most;
                 float part_sum = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    z[rt][j] = __builtin_amdgcn_exp2f(z[rt][j] - ref);
+                    z[rt][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[rt][j], f, -ref));
                     part_sum += z[rt][j];
                 }
-                const float up = fmaxf(top[rt], most), up_ref = up == -INFINITY ? 0.0f : up;
-                const float keep = __builtin_amdgcn_exp2f(top[rt] - up_ref), add = __builtin_amdgcn_exp2f(most - up_ref);
-                top[rt] = up;
-                sum[rt] = __builtin_fmaf(sum[rt], keep, part_sum * add);
-                constexpr float one = Fixed<ND, false>::kOne;
-                float to_one = one, worth;   // numerators become digits relative to `one`; what one is worth
-                if constexpr (SMALL) {
-                    float big = 0.0f;
+                if (__any(most > top[rt] + kSlack)) {   // (the first tile's too)
+                    const float up = fmaxf(top[rt], most), keep = up == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[rt] - up);
+                    top[rt] = up;
+                    sum[rt] *= keep;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        z[rt][j] = z[rt][j] > 0.0f ? z[rt][j] * vs : z[rt][j] * 0.0f;
-                        big = fmaxf(big, z[rt][j]);
-                    }
-                    big = max_of_four(big);
-                    to_one = big >= 0x1p-100f ? one / big : 0.0f;
+                    for (int v = 0; v < VT; ++v)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[rt][v][i] *= keep;
+                }
+                const float add = most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(most - top[rt]);
+                sum[rt] = __builtin_fmaf(part_sum, add, sum[rt]);
+                constexpr float one = Fixed<ND, false>::kOne;
+                float to_one = one, worth;   // what makes a numerator a fixed-point number, and what a step of that is worth
+                if constexpr (SMALL) {
+                    // (a lane that sees nothing has no say, whatever its block's scale is)
+                    const float own = mine_most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine_most - ref) * vs;
+                    const float big = max_of_four(own);
+                    to_one = big >= 0x1p-100f && mine_most != -INFINITY ? one / big * vs : 0.0f;
                     worth = add * big * (1.0f / one);
                 } else {
                     worth = add > 0.0f ? add * vs * (1.0f / one) : add * 0.0f;
@@ -321,13 +379,25 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnParams p) {
 #pragma unroll
                     for (int t = 0; t < ND; ++t) pd[t][s] = (int)digit[t];
                 }
+                // (a few products ahead of the sums that take them: all at once would be more registers than there are)
+                constexpr int kAhead = 2;
+                v4i acc[2][kAhead][ND];
+                auto products = [&](int v, v4i (&a)[kAhead][ND]) __attribute__((always_inline)) {
 #pragma unroll
-                for (int v = 0; v < VT; ++v) {
-                    v4i acc[ND];
+                    for (int k = 0; k < kAhead; ++k)
 #pragma unroll
-                    for (int t = 0; t < ND; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[v], pd[t], v4i{0, 0, 0, 0}, 0, 0, 0);
+                        for (int t = 0; t < ND; ++t) a[k][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[v + k], pd[t], v4i{0, 0, 0, 0}, 0, 0, 0);
+                };
+                products(0, acc[0]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[rt][v][i] = __builtin_fmaf(meet<ND>(acc, i), worth, o[rt][v][i] * keep);
+                for (int v = 0; v < VT; v += kAhead) {
+                    if (v + kAhead < VT) products(v + kAhead, acc[(v / kAhead & 1) ^ 1]);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[rt][v + k][i] = __builtin_fmaf(meet<ND>(acc[v / kAhead & 1][k], i), worth, o[rt][v + k][i]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
@@ -338,27 +408,28 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnParams p) {
         for (int rt = 0; rt < RT; ++rt) {
             sum[rt] = sum_of_four(sum[rt]);
             if constexpr (BY_ROWS) {
-                if (q_row[rt] < 0) continue;
+                const int token = s_token[wave_rows + rt * 16 + lr], qh = s_head[wave_rows + rt * 16 + lr];
+                const int64_t at = (int64_t)token * p.q_heads + qh;
+                if (token < 0) continue;
                 if (p.parts > 1) {
-                    float* const po = p.part_o + ((int64_t)part * all_rows + q_row[rt]) * COLS;
+                    float* const po = p.part_o + ((int64_t)part * all_rows + at) * COLS;
 #pragma unroll
                     for (int v = 0; v < VT; ++v) *reinterpret_cast<attn_v4f*>(po + 16 * v + 4 * lq) = o[rt][v];
                     if (lq == 0) {
-                        float* const ml = p.part_ml + ((int64_t)part * all_rows + q_row[rt]) * 2;
+                        float* const ml = p.part_ml + ((int64_t)part * all_rows + at) * 2;
                         ml[0] = top[rt];
                         ml[1] = sum[rt];
                     }
                 } else {
-                    const int64_t token = q_row[rt] / p.q_heads;
-                    const int qh = (int)(q_row[rt] - token * p.q_heads);
-                    T* const out = static_cast<T*>(p.O) + token * p.o_token + qh * p.o_head;
+                    const int first = here_only(4 * lq);
+                    T* const out = static_cast<T*>(p.O) + token * p.o_token + qh * p.o_head + first;
                     const float inv = sum[rt] == 0.0f ? 0.0f : 1.0f / sum[rt];
 #pragma unroll
                     for (int v = 0; v < VT; ++v)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if (16 * v + 4 * lq + i < p.dim) out[16 * v + 4 * lq + i] = from_f32<T>(o[rt][v][i] * inv);
-                    if (p.lse && lq == 0) p.lse[q_row[rt]] = sum[rt] == 0.0f ? -INFINITY : (top[rt] + __builtin_amdgcn_logf(sum[rt])) * 0.69314718f;
+                            if (first < p.dim - (16 * v + i)) out[16 * v + i] = from_f32<T>(o[rt][v][i] * inv);
+                    if (p.lse && lq == 0) p.lse[at] = sum[rt] == 0.0f ? -INFINITY : (top[rt] + __builtin_amdgcn_logf(sum[rt])) * 0.69314718f;
                 }
             } else {
                 __syncthreads();
@@ -369,11 +440,10 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnParams p) {
 #pragma unroll
                 for (int v = 0; v < VT; ++v) *reinterpret_cast<attn_v4f*>(&s_o[(wave * 16 + lr) * kPitch + 16 * v + 4 * lq]) = o[rt][v];
                 __syncthreads();
-                for (int e = threadIdx.x; e < 16 * COLS; e += 256) {
-                    const int r = e / COLS, d = e % COLS;
-                    const int64_t row = row0 + rt * 16 + r;
-                    if (row >= rows) break;
-                    const int i = (int)(row / p.group), qh = head * p.group + (int)(row - (int64_t)i * p.group);
+#pragma unroll 1
+                for (int e = here_only(threadIdx.x); e < 16 * COLS; e += 256) {
+                    const int r = e / COLS, d = e % COLS, token = s_token[rt * 16 + r], qh = s_head[rt * 16 + r];
+                    if (token < 0) break;   // (rows that exist come first)
                     float m = s_m[0][r];
 #pragma unroll
                     for (int w = 1; w < 4; ++w) m = fmaxf(m, s_m[w][r]);
@@ -385,7 +455,7 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnParams p) {
                         l = __builtin_fmaf(s_l[w][r], f, l);
                         x = __builtin_fmaf(s_o[(w * 16 + r) * kPitch + d], f, x);
                     }
-                    const int64_t at = (c0 + i) * p.q_heads + qh;
+                    const int64_t at = (int64_t)token * p.q_heads + qh;
                     if (p.parts > 1) {
                         p.part_o[((int64_t)part * all_rows + at) * COLS + d] = x;
                         if (d == 0) {
@@ -394,7 +464,7 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnParams p) {
                             ml[1] = l;
                         }
                     } else {
-                        if (d < p.dim) static_cast<T*>(p.O)[(c0 + i) * p.o_token + qh * p.o_head + d] = from_f32<T>(l == 0.0f ? 0.0f : x / l);
+                        if (d < p.dim) static_cast<T*>(p.O)[token * p.o_token + qh * p.o_head + d] = from_f32<T>(l == 0.0f ? 0.0f : x / l);
                         if (p.lse && d == 0) p.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718f;
                     }
                 }
@@ -404,32 +474,49 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(const AttnParams p) {
     if (p.req_flags && __any(bad_block) && lane == 0) atomicOr(p.req_flags + req, ABFT_KV_BAD_BLOCK);
 }
 
-// Joins the parts of a request's rows: one wavefront a row.
-template <typename T, int COLS>
+// Joins the parts of a request's rows: NW wavefronts a row, which take parts in turn, lanes own columns.
+template <typename T, int COLS, int NW>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(const AttnParams p) {
-    constexpr int PER = COLS / 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, req = blockIdx.y;
+    constexpr int PER = COLS / 64, kRows = 4 / NW;
+    __shared__ float s_x[NW > 1 ? NW : 1][NW > 1 ? COLS : 1], s_l[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine_first = wave % NW, req = blockIdx.y;
     const int64_t room = (int64_t)p.width << p.block_shift;
     const int len = (int)min((int64_t)max(p.seq_len[req], 0), room);
     const int64_t c0 = min((int64_t)max(p.cu_new[req], 0), p.n_rows), c1 = min(max((int64_t)p.cu_new[req + 1], c0), p.n_rows);
-    const int mine = len <= 0 ? 1 : min(p.parts, (len + p.chunk - 1) / p.chunk);
+    const int parts = len <= 0 ? 1 : min(p.parts, (len + p.chunk - 1) / p.chunk);
     const int64_t all_rows = p.n_rows * p.q_heads;
-    for (int64_t r = c0 * p.q_heads + blockIdx.x * 4 + wave; r < c1 * p.q_heads; r += (int64_t)gridDim.x * 4) {
+    // (with several wavefronts a row, all of a workgroup are at the same row)
+    for (int64_t r = c0 * p.q_heads + (int64_t)blockIdx.x * kRows + wave / NW; r < c1 * p.q_heads; r += (int64_t)gridDim.x * kRows) {
         float m = -INFINITY;
-        for (int s = lane; s < mine; s += 64) m = fmaxf(m, p.part_ml[(s * all_rows + r) * 2]);
+        for (int s = lane; s < parts; s += 64) m = fmaxf(m, p.part_ml[(s * all_rows + r) * 2]);
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
         const float ref = m == -INFINITY ? 0.0f : m;
         float l = 0.0f, x[PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i) x[i] = 0.0f;
-        for (int s = 0; s < mine; ++s) {
+#pragma unroll 4
+        for (int s = mine_first; s < parts; s += NW) {
             const float* const ml = p.part_ml + (s * all_rows + r) * 2;
+            const float* const po = p.part_o + (s * all_rows + r) * COLS + lane * PER;
             const float f = __builtin_amdgcn_exp2f(ml[0] - ref);
             l = __builtin_fmaf(ml[1], f, l);
-            const float* const po = p.part_o + (s * all_rows + r) * COLS + lane * PER;
 #pragma unroll
             for (int i = 0; i < PER; ++i) x[i] = __builtin_fmaf(po[i], f, x[i]);
+        }
+        if constexpr (NW > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < PER; ++i) s_x[wave][lane * PER + i] = x[i];
+            if (lane == 0) s_l[wave] = l;
+            __syncthreads();
+            if (wave > 0) continue;
+#pragma unroll
+            for (int w = 1; w < NW; ++w) {
+                l += s_l[w];
+#pragma unroll
+                for (int i = 0; i < PER; ++i) x[i] += s_x[w][lane * PER + i];
+            }
         }
         const int64_t token = r / p.q_heads;
         const int qh = (int)(r - token * p.q_heads);
@@ -443,18 +530,21 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(const AttnParams
 
 template <typename T, int COLS, bool SMALL>
 hipError_t launch_attention_block(AttnShape shape, const AttnParams& p, dim3 grid, hipStream_t s) {
+    constexpr int kMost = attn_rows_tiles(attn_digits(sizeof(T)), COLS);
     const dim3 threads(256);
-    if (shape == kAttnTokens1) kv_attention_kernel<T, COLS, 1, SMALL, false><<<grid, threads, 0, s>>>(p);
-    else if (COLS <= 128 && shape == kAttnTokens2) kv_attention_kernel<T, COLS <= 128 ? COLS : 128, 2, SMALL, false><<<grid, threads, 0, s>>>(p);
-    else kv_attention_kernel<T, COLS, attn_rows_tiles(COLS), SMALL, true><<<grid, threads, 0, s>>>(p);
+    if (shape == kAttnRows) kv_attention_kernel<T, COLS, kMost, SMALL, true><<<grid, threads, 0, s>>>(p);
+    else if (shape == kAttnTokens2) kv_attention_kernel<T, COLS, kMost, SMALL, false><<<grid, threads, 0, s>>>(p);
+    else kv_attention_kernel<T, COLS, 1, SMALL, false><<<grid, threads, 0, s>>>(p);
     return hipGetLastError();
 }
 template <typename T, int COLS>
 hipError_t launch_attention_cols(AttnShape shape, bool small_blocks, const AttnParams& p, dim3 grid, hipStream_t s) {
     const hipError_t e = small_blocks ? launch_attention_block<T, COLS, true>(shape, p, grid, s) : launch_attention_block<T, COLS, false>(shape, p, grid, s);
     if (e != hipSuccess || p.parts <= 1) return e;
+    // many parts, few rows: the wavefronts of a workgroup share a row's
     const int64_t rows = (p.n_rows + p.n_req - 1) / p.n_req * p.q_heads;
-    kv_attention_join_kernel<T, COLS><<<dim3((unsigned)((rows + 3) / 4 < 1024 ? (rows + 3) / 4 : 1024), (unsigned)p.n_req), dim3(256), 0, s>>>(p);
+    if (p.parts > 8) kv_attention_join_kernel<T, COLS, 4><<<dim3((unsigned)(rows < 4096 ? rows : 4096), (unsigned)p.n_req), dim3(256), 0, s>>>(p);
+    else kv_attention_join_kernel<T, COLS, 1><<<dim3((unsigned)((rows + 3) / 4 < 1024 ? (rows + 3) / 4 : 1024), (unsigned)p.n_req), dim3(256), 0, s>>>(p);
     return hipGetLastError();
 }
 template <typename T>

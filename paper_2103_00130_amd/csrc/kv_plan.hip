@@ -168,10 +168,9 @@ extern "C" int abft_kv_plan(const int32_t* ctx_len, const int32_t* new_len, int 
     const unsigned grid = (unsigned)(groups < 1 ? 1 : groups > 256 ? 256 : groups);
     if (nt == 256) abft::kv_plan_kernel<256><<<dim3(grid), dim3(256), lds, (hipStream_t)stream>>>(p);
     else {
-        if (lds > 48 * 1024) {
-            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(abft::kv_plan_kernel<1024>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)(abft::kMaxRequests * 8));
-            if (e != hipSuccess) return abft::set_error(ABFT_EHIP, "%s: %s", fn, hipGetErrorString(e));
-        }
+        static std::atomic<uint64_t> done{0};
+        const hipError_t e = abft::allow_dynamic_lds(reinterpret_cast<const void*>(abft::kv_plan_kernel<1024>), abft::kMaxRequests * 8, done);
+        if (e != hipSuccess) return abft::set_error(ABFT_EHIP, "%s: %s", fn, hipGetErrorString(e));
         abft::kv_plan_kernel<1024><<<dim3(grid), dim3(1024), lds, (hipStream_t)stream>>>(p);
     }
     const hipError_t e = hipGetLastError();

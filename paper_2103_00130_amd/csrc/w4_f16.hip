@@ -1,0 +1,8 @@
+// Products with 4-bit weights, activations of type f16.
+#include "w4.h"
+
+namespace abft {
+hipError_t launch_w4_f16(bool wide, bool bias, int group, W4Shape shape, const W4Params& p, hipStream_t s) {
+    return launch_w4<f16>(wide, bias, group, shape, p, s);
+}
+}  // namespace abft
