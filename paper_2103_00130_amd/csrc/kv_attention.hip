@@ -6,24 +6,24 @@
 namespace abft {
 namespace {
 
-// How a call is cut, by what the host knows of it.
+// How a call is cut, by what the host knows of it.  most: rows of a wavefront, in sixteens.
 struct AttnCut {
     AttnShape shape;
     int groups;   // workgroups for the rows of a request and head
     int parts, chunk;
 };
 constexpr int kWanted = 2048;   // workgroups: eight for each compute unit, of which up to four run at a time
-AttnCut cut(int cols, int n_req, int heads, int group, int max_new, int max_len) {
+AttnCut cut(int most, int n_req, int heads, int group, int max_new, int max_len) {
     AttnCut c;
     const int64_t rows = (int64_t)max_new * group;
-    c.shape = rows <= 16 ? kAttnTokens1 : rows <= 32 && cols <= 128 ? kAttnTokens2 : kAttnRows;
-    const int64_t per = c.shape == kAttnTokens1 ? 16 : c.shape == kAttnTokens2 ? 32 : 64 * attn_rows_tiles(cols);
+    c.shape = rows <= 16 ? kAttnTokens1 : rows <= 16 * most ? kAttnTokens2 : kAttnRows;
+    const int64_t per = c.shape == kAttnTokens1 ? 16 : c.shape == kAttnTokens2 ? 16 * most : 64 * most;
     const int64_t groups = (rows + per - 1) / per;
     c.groups = (int)(groups < 1 ? 1 : groups > 65535 ? 65535 : groups);
     const int64_t whole = (int64_t)n_req * heads * c.groups;
     int64_t parts = whole >= kWanted ? 1 : kWanted / whole;
-    const int64_t most = ((int64_t)max_len + 255) / 256;
-    parts = parts > most ? most : parts;
+    const int64_t longest = ((int64_t)max_len + 255) / 256;
+    parts = parts > longest ? longest : parts;
     parts = parts < 1 ? 1 : parts;
     c.chunk = (int)((((int64_t)max_len + parts - 1) / parts + 255) / 256 * 256);
     if (c.chunk < 256) c.chunk = 256;
@@ -46,8 +46,13 @@ extern "C" {
 size_t abft_kv_attention_workspace_bytes(const abft_kv_cache_t* cache, int n_req, int q_heads, int max_new, int max_len) {
     if (abft::kv_wrong_sizes(cache) || n_req < 1 || q_heads < 1 || q_heads % cache->heads != 0 || max_new < 1 || max_len < 1 || max_len > 0x7ffffe00) return 0;
     const int cols = abft::kv_columns(cache->head_dim);
-    const abft::AttnCut c = abft::cut(cols, n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
-    return c.parts <= 1 ? 0 : c.parts * abft::part_bytes((int64_t)n_req * max_new * q_heads, cols);
+    size_t bytes = 0;
+    for (const int digits : {2, 3}) {   // (whatever the type)
+        const abft::AttnCut c = abft::cut(abft::attn_rows_tiles(digits, cols), n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
+        const size_t need = c.parts <= 1 ? 0 : c.parts * abft::part_bytes((int64_t)n_req * max_new * q_heads, cols);
+        bytes = need > bytes ? need : bytes;
+    }
+    return bytes;
 }
 
 int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_token_stride, int64_t q_head_stride, int type,
@@ -73,7 +78,7 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
     if (n_rows > 0x7fffffffll / q_heads) return abft::set_error(ABFT_EUNSUPPORTED, "%s: n_rows=%lld too large for one launch", fn, (long long)n_rows);
 
     const int cols = abft::kv_columns(cache->head_dim);
-    abft::AttnCut c = abft::cut(cols, n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
+    abft::AttnCut c = abft::cut(abft::attn_rows_tiles(abft::attn_digits(abft::type_size(type)), cols), n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
     const size_t each = abft::part_bytes(n_rows * q_heads, cols);
     if (c.parts > 1 && (!workspace || workspace_bytes / each < (size_t)c.parts)) {
         const size_t fit = workspace ? workspace_bytes / each : 0;
@@ -112,7 +117,7 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
     p.parts = c.parts;
     p.chunk = c.chunk;
     p.scale2 = scale * 1.44269504f;
-    p.q_wide = ((reinterpret_cast<uintptr_t>(Q) | (uintptr_t)(q_token_stride * (int64_t)es) | (uintptr_t)(q_head_stride * (int64_t)es)) & 15) == 0;
+    p.q_wide = ((reinterpret_cast<uintptr_t>(Q) | (uintptr_t)(q_token_stride * (int64_t)es) | (uintptr_t)(q_head_stride * (int64_t)es) | (uintptr_t)(cache->head_dim * (int64_t)es)) & 15) == 0;
     hipStream_t s = (hipStream_t)stream;
     hipError_t e = hipSuccess;
     if (req_flags) {
