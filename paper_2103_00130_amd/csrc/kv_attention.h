@@ -29,6 +29,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "kv_cache.h"
 #include "values.h"
 
@@ -50,27 +52,29 @@ struct AttnParams {
     float* part_ml;   // [part][row][2]: maximum (base 2), sum of numerators
     int64_t q_token, q_head, o_token, o_head, ldt, n_rows;
     int n_blocks, heads, q_heads, group, dim, block_shift, width, n_req;
+    int groups;         // workgroups for the rows of a head and request
     int parts, chunk;   // a part is `chunk` tokens, a multiple of 256; the last takes what is left
+    int stride;
     float scale2;       // the scale of the scores, times log2(e)
     bool q_wide;        // rows of Q are whole aligned pieces of 16 bytes
 };
 
 // which kernel (one for each of them and each type, number of columns and kind of block)
 enum AttnShape {
-    kAttnTokens1,   // up to 16 rows, tokens split among the wavefronts
-    kAttnTokens2,   // up to 32, where a wavefront holds that many
+    kAttnTokens1,   // 16 rows, tokens split among the wavefronts
+    kAttnTokens2,   // 32, where a wavefront holds that many
     kAttnRows       // rows split among the wavefronts
 };
 // Most rows of a wavefront, in sixteens.  More do not fit its registers, and a kernel that spills is not to be had: the compiler has put
 // the copy of a spilled register before the end of a divergent branch, where not every lane made it.
-constexpr int attn_rows_tiles(int digits, int cols) { return cols <= (digits == 2 ? 128 : 64) ? 2 : 1; }
-// Wavefronts that are to share a SIMD's registers.
-constexpr int attn_waves(int digits, int cols) { return cols <= (digits == 2 ? 128 : 64) ? 2 : 1; }
+constexpr int attn_rows_tiles(int cols) { return cols <= 64 ? 2 : 1; }
+// Wavefronts that are to share a SIMD's registers (512): what the kernels fit without spilling.
+constexpr int attn_waves(int digits, int cols, int row_tiles) { return cols == 256 ? 1 : digits == 2 && cols <= 128 && row_tiles == 1 ? 3 : 2; }
 constexpr int attn_digits(int type_size) { return type_size == 4 ? 3 : 2; }
 
-hipError_t launch_attention_f32(AttnShape shape, int cols, bool small_blocks, const AttnParams& p, dim3 grid, hipStream_t s);
-hipError_t launch_attention_f16(AttnShape shape, int cols, bool small_blocks, const AttnParams& p, dim3 grid, hipStream_t s);
-hipError_t launch_attention_bf16(AttnShape shape, int cols, bool small_blocks, const AttnParams& p, dim3 grid, hipStream_t s);
+hipError_t launch_attention_f32(AttnShape shape, int cols, bool small_blocks, const AttnParams& p, unsigned grid, hipStream_t s);
+hipError_t launch_attention_f16(AttnShape shape, int cols, bool small_blocks, const AttnParams& p, unsigned grid, hipStream_t s);
+hipError_t launch_attention_bf16(AttnShape shape, int cols, bool small_blocks, const AttnParams& p, unsigned grid, hipStream_t s);
 
 #ifdef __HIPCC__
 
@@ -146,7 +150,7 @@ __device__ inline float meet(const v4i (&acc)[ND], int i) {
 }
 
 template <typename T, int COLS, int RT, bool SMALL, bool BY_ROWS>
-__global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), RT * COLS)) void kv_attention_kernel(const AttnParams p) {
+__global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), COLS, RT)) void kv_attention_kernel(const AttnParams p) {
     constexpr int ND = attn_digits(sizeof(T));
     constexpr int KC = COLS / 64, VT = COLS / 16;
     constexpr int kRows = RT * 16 * (BY_ROWS ? 4 : 1);         // rows of a workgroup
@@ -158,7 +162,16 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), RT * COLS))
     __shared__ float s_o[BY_ROWS ? 1 : 4 * 16 * kPitch];
     __shared__ float s_m[4][16], s_l[4][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15, lq = lane >> 4;
-    const int head = blockIdx.y, req = blockIdx.z, part = blockIdx.x % p.parts, first_group = blockIdx.x / p.parts, groups = gridDim.x / p.parts;
+    // Which part and group of rows (`late`: the last ones, of which only long requests have any and which see most, come first) of which
+    // head of which request.  Neighbouring workgroups run in different eighths of the chip, and those 256 apart on one compute unit.
+    // Rows split: what a head and request has stands together, since it reads the same codes.  Tokens split: every head and request of one
+    // part ahead of the next part's, and from part to part they move on by p.stride, so that neither an eighth nor a compute unit has
+    // much of one long request (64 requests of uneven lengths up to 8000 in four parts: 97 us, 127 with the parts of a request next
+    // to each other, where an eighth had the first parts of all).
+    const uint32_t many = (uint32_t)(p.groups * p.parts), pairs = (uint32_t)(p.heads * p.n_req);
+    const uint32_t turn = BY_ROWS ? blockIdx.x % many : blockIdx.x / pairs, late = many - 1 - turn;
+    const int part = (int)(late / (uint32_t)p.groups), first_group = (int)(late % (uint32_t)p.groups), groups = p.groups;
+    const int pair = (int)(BY_ROWS ? blockIdx.x / many : (blockIdx.x % pairs + turn * (uint64_t)p.stride) % pairs), req = pair / p.heads, head = pair - req * p.heads;
     const int block_tokens = 1 << p.block_shift;
 
     const int64_t room = (int64_t)p.width << p.block_shift;
@@ -174,6 +187,59 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), RT * COLS))
     bool bad_block = false;
 
     for (int64_t row0 = (int64_t)first_group * kRows; row0 < rows; row0 += (int64_t)groups * kRows) {
+        const int wave_rows = BY_ROWS ? wave * RT * 16 : 0;   // this wavefront's first row
+        // the last position that any of its rows sees: that of the last row
+        const int64_t past = min(row0 + wave_rows + RT * 16, (int64_t)rows);
+        const int last = past > row0 + wave_rows ? len - fresh + (int)((uint32_t)(past - 1) / (uint32_t)p.group) : -1;
+
+        const int begin = part * p.chunk, end = min(part == mine - 1 ? len : begin + p.chunk, last + 1);
+        // Blocks of a tile: where a tile lies within one block, that one (in scalar registers); else those of its groups of 16 tokens
+        // as the lane needs them, for K those of group lr / 4, else of group lq.
+        struct Blocks {
+            int k, v;
+        };
+        auto block_of = [&](int t) __attribute__((always_inline)) { return t < len ? table[t >> p.block_shift] : -1; };
+        auto blocks_of = [&](int t) __attribute__((always_inline)) {
+            Blocks x;
+            if constexpr (SMALL) {
+                x.k = block_of(t + 16 * (lr >> 2));
+                x.v = block_of(t + 16 * lq);
+            } else {
+                x.k = x.v = __builtin_amdgcn_readfirstlane(block_of(t));
+            }
+            return x;
+        };
+        auto exists = [&](int id) __attribute__((always_inline)) { return (uint32_t)id < (uint32_t)p.n_blocks; };
+        const int64_t block_bytes = (int64_t)COLS << p.block_shift;   // of one head
+        const int k_lane = (SMALL ? (lr & 3) : 16 * (lr >> 2) + (lr & 3)) * COLS + 16 * lq;
+        const int v_lane = (SMALL ? 0 : lq * COLS * kKvGroup) + lr * 16;
+        v4i kf[4][KC];
+        auto load_k = [&](int id, int t) __attribute__((always_inline)) {
+            const int64_t b = exists(id) ? id : 0;
+            const int off = (SMALL ? t + 16 * (lr >> 2) : t) & (block_tokens - 1);
+            const int8_t* const at = p.k_codes + (b * p.heads + head) * block_bytes + off * COLS;
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int c = 0; c < KC; ++c) kf[s][c] = *reinterpret_cast<const v4i*>(at + k_lane + (4 * s * COLS + 64 * c));
+        };
+        v4i vf[VT];
+        float ks = 0.0f, vs = 0.0f;   // (of block 0 where there is none: nothing is seen of it)
+        auto load_v = [&](int id, int t) __attribute__((always_inline)) {
+            const int64_t block_head = (int64_t)(exists(id) ? id : 0) * p.heads + head;
+            const int off = (SMALL ? t + 16 * lq : t) & (block_tokens - 1);
+            const int8_t* const at = p.v_codes + block_head * block_bytes + off * COLS;
+#pragma unroll
+            for (int v = 0; v < VT; ++v) vf[v] = *reinterpret_cast<const v4i*>(at + v_lane + v * 256);
+            ks = p.k_scale[block_head];
+            vs = p.v_scale[block_head];
+        };
+        int t0 = begin + (BY_ROWS ? 0 : wave * kAttnTile);
+        Blocks now = {-1, -1};
+        if (t0 < end) {
+            now = blocks_of(t0);
+            load_k(now.k, t0);
+        }
         // ---- the rows, once for the workgroup: sixteen threads a row, sixteen columns a thread
         __syncthreads();
 #pragma unroll 1
@@ -232,23 +298,13 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), RT * COLS))
         }
         __syncthreads();
         // ---- this wavefront's rows
-        const int wave_rows = BY_ROWS ? wave * RT * 16 : 0;
         int limit[RT];
         float q_scale[RT];
-        v4i qd[RT][KC][ND];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             limit[rt] = s_limit[wave_rows + rt * 16 + lr];
             q_scale[rt] = s_q_scale[wave_rows + rt * 16 + lr];
-#pragma unroll
-            for (int c = 0; c < KC; ++c)
-#pragma unroll
-                for (int t = 0; t < ND; ++t) qd[rt][c][t] = s_q[wave_rows / 16 + rt][c][t][lane];
         }
-        // the last position that any of them sees: that of the last row
-        const int64_t past = min(row0 + wave_rows + RT * 16, (int64_t)rows);
-        const int last = past > row0 + wave_rows ? len - fresh + (int)((uint32_t)(past - 1) / (uint32_t)p.group) : -1;
-
         float top[RT], sum[RT];
         attn_v4f o[RT][VT];
 #pragma unroll
@@ -259,59 +315,22 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), RT * COLS))
             for (int t = 0; t < VT; ++t) o[rt][t] = attn_v4f{0, 0, 0, 0};
         }
 
-        const int begin = part * p.chunk, end = min(part == mine - 1 ? len : begin + p.chunk, last + 1);
-        // Blocks of a tile: where a tile lies within one block, that one (in scalar registers); else those of its groups of 16 tokens
-        // as the lane needs them, for K those of group lr / 4, else of group lq.
-        struct Blocks {
-            int k, v;
-        };
-        auto block_of = [&](int t) __attribute__((always_inline)) { return t < len ? table[t >> p.block_shift] : -1; };
-        auto blocks_of = [&](int t) __attribute__((always_inline)) {
-            Blocks x;
-            if constexpr (SMALL) {
-                x.k = block_of(t + 16 * (lr >> 2));
-                x.v = block_of(t + 16 * lq);
-            } else {
-                x.k = x.v = __builtin_amdgcn_readfirstlane(block_of(t));
-            }
-            return x;
-        };
-        auto exists = [&](int id) __attribute__((always_inline)) { return (uint32_t)id < (uint32_t)p.n_blocks; };
-        const int64_t block_bytes = (int64_t)COLS << p.block_shift;   // of one head
-        const int k_lane = (SMALL ? (lr & 3) : 16 * (lr >> 2) + (lr & 3)) * COLS + 16 * lq;
-        const int v_lane = (SMALL ? 0 : lq * COLS * kKvGroup) + lr * 16;
-        v4i kf[4][KC];
-        auto load_k = [&](int id, int t) __attribute__((always_inline)) {
-            const int64_t b = exists(id) ? id : 0;
-            const int off = (SMALL ? t + 16 * (lr >> 2) : t) & (block_tokens - 1);
-            const int8_t* const at = p.k_codes + (b * p.heads + head) * block_bytes + off * COLS;
-#pragma unroll
-            for (int s = 0; s < 4; ++s)
-#pragma unroll
-                for (int c = 0; c < KC; ++c) kf[s][c] = *reinterpret_cast<const v4i*>(at + k_lane + (4 * s * COLS + 64 * c));
-        };
-        int t0 = begin + (BY_ROWS ? 0 : wave * kAttnTile);
-        Blocks now = {-1, -1};
-        if (t0 < end) {
-            now = blocks_of(t0);
-            load_k(now.k, t0);
-        }
-        for (; t0 < end; t0 += kStep) {
+        // one tile; `more`: there is another, which is fetched while this one is worked on
+        auto tile_at = [&](int t0, auto more) __attribute__((always_inline)) {
+            load_v(now.v, t0);
             const bool here = exists(now.v);
             if (!here && t0 + (SMALL ? 16 * lq : 0) < len) bad_block = true;
-            const int64_t block_head = (int64_t)(here ? now.v : 0) * p.heads + head;
-            const float ks = p.k_scale[block_head], vs = p.v_scale[block_head];   // (of block 0 where there is none: nothing is seen of it)
-            v4i vf[VT];
-            {
-                const int off = (SMALL ? t0 + 16 * lq : t0) & (block_tokens - 1);
-                const int8_t* const at = p.v_codes + block_head * block_bytes + off * COLS;
+            const int at_lane = here_only(lane);   // (the rows' digits stay in LDS: their registers are worth a wavefront more)
+            const int tn = t0 + kStep;
 #pragma unroll
-                for (int t = 0; t < VT; ++t) vf[t] = *reinterpret_cast<const v4i*>(at + v_lane + t * 256);
-            }
-            // ---- scores, as sums of digit products
-            float z[RT][16];
+            for (int rt = 0; rt < RT; ++rt) {
+                // ---- scores, as sums of digit products
+                float z[16];
+                v4i qd[KC][ND];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+                for (int c = 0; c < KC; ++c)
+#pragma unroll
+                    for (int t = 0; t < ND; ++t) qd[c][t] = s_q[wave_rows / 16 + rt][c][t][at_lane];
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     v4i acc[ND];
@@ -319,35 +338,32 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), RT * COLS))
                     for (int t = 0; t < ND; ++t) {
                         acc[t] = v4i{0, 0, 0, 0};
 #pragma unroll
-                        for (int c = 0; c < KC; ++c) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[s][c], qd[rt][c][t], acc[t], 0, 0, 0);
+                        for (int c = 0; c < KC; ++c) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[s][c], qd[c][t], acc[t], 0, 0, 0);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z[rt][4 * s + i] = meet<ND>(acc, i);
+                    for (int i = 0; i < 4; ++i) z[4 * s + i] = meet<ND>(acc, i);
                 }
-            // ---- the next tile's keys are on their way from here on
-            const int tn = t0 + kStep;
-            if (tn < end) {
-                now = blocks_of(tn);
-                load_k(now.k, tn);
-            }
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
+                // ---- the next tile's keys are on their way from here on
+                if (decltype(more)::value && rt == RT - 1) {
+                    now = blocks_of(tn);
+                    load_k(now.k, tn);
+                }
                 float f = q_scale[rt] * ks;   // makes a score of a sum, base 2
                 if (!__all(here && t0 + kAttnTile - 1 <= limit[rt])) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) z[rt][j] = here && t0 + 16 * lq + j <= limit[rt] ? z[rt][j] * f : -INFINITY;
+                    for (int j = 0; j < 16; ++j) z[j] = here && t0 + 16 * lq + j <= limit[rt] ? z[j] * f : -INFINITY;
                     f = 1.0f;
                 }
-                float mine_most = z[rt][0];
+                float mine_most = z[0];
 #pragma unroll
-                for (int j = 1; j < 16; ++j) mine_most = fmaxf(mine_most, z[rt][j]);
+                for (int j = 1; j < 16; ++j) mine_most = fmaxf(mine_most, z[j]);
                 mine_most *= f;
                 const float most = max_of_four(mine_most), ref = most == -INFINITY ? 0.0f : most;
                 float part_sum = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    z[rt][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[rt][j], f, -ref));
-                    part_sum += z[rt][j];
+                    z[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], f, -ref));
+                    part_sum += z[j];
                 }
                 if (__any(most > top[rt] + kSlack)) {   // (the first tile's too)
                     const float up = fmaxf(top[rt], most), keep = up == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[rt] - up);
@@ -375,7 +391,7 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), RT * COLS))
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     uint32_t digit[ND];
-                    four_digits<ND, false>(z[rt][4 * s], z[rt][4 * s + 1], z[rt][4 * s + 2], z[rt][4 * s + 3], to_one, digit);
+                    four_digits<ND, false>(z[4 * s], z[4 * s + 1], z[4 * s + 2], z[4 * s + 3], to_one, digit);
 #pragma unroll
                     for (int t = 0; t < ND; ++t) pd[t][s] = (int)digit[t];
                 }
@@ -400,7 +416,9 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), RT * COLS))
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-        }
+        };
+        for (; t0 + kStep < end; t0 += kStep) tile_at(t0, std::true_type{});
+        if (t0 < end) tile_at(t0, std::false_type{});
 
         // ---- out: column 16 v + 4 lq + i of row lr
         const int64_t all_rows = p.n_rows * p.q_heads;
@@ -529,16 +547,15 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(const AttnParams
 }
 
 template <typename T, int COLS, bool SMALL>
-hipError_t launch_attention_block(AttnShape shape, const AttnParams& p, dim3 grid, hipStream_t s) {
-    constexpr int kMost = attn_rows_tiles(attn_digits(sizeof(T)), COLS);
-    const dim3 threads(256);
-    if (shape == kAttnRows) kv_attention_kernel<T, COLS, kMost, SMALL, true><<<grid, threads, 0, s>>>(p);
-    else if (shape == kAttnTokens2) kv_attention_kernel<T, COLS, kMost, SMALL, false><<<grid, threads, 0, s>>>(p);
-    else kv_attention_kernel<T, COLS, 1, SMALL, false><<<grid, threads, 0, s>>>(p);
+hipError_t launch_attention_block(AttnShape shape, const AttnParams& p, unsigned grid, hipStream_t s) {
+    constexpr int kMost = attn_rows_tiles(COLS);
+    if (shape == kAttnRows) kv_attention_kernel<T, COLS, kMost, SMALL, true><<<dim3(grid), dim3(256), 0, s>>>(p);
+    else if (shape == kAttnTokens2) kv_attention_kernel<T, COLS, kMost, SMALL, false><<<dim3(grid), dim3(256), 0, s>>>(p);
+    else kv_attention_kernel<T, COLS, 1, SMALL, false><<<dim3(grid), dim3(256), 0, s>>>(p);
     return hipGetLastError();
 }
 template <typename T, int COLS>
-hipError_t launch_attention_cols(AttnShape shape, bool small_blocks, const AttnParams& p, dim3 grid, hipStream_t s) {
+hipError_t launch_attention_cols(AttnShape shape, bool small_blocks, const AttnParams& p, unsigned grid, hipStream_t s) {
     const hipError_t e = small_blocks ? launch_attention_block<T, COLS, true>(shape, p, grid, s) : launch_attention_block<T, COLS, false>(shape, p, grid, s);
     if (e != hipSuccess || p.parts <= 1) return e;
     // many parts, few rows: the wavefronts of a workgroup share a row's
@@ -548,7 +565,7 @@ hipError_t launch_attention_cols(AttnShape shape, bool small_blocks, const AttnP
     return hipGetLastError();
 }
 template <typename T>
-hipError_t launch_attention(AttnShape shape, int cols, bool small_blocks, const AttnParams& p, dim3 grid, hipStream_t s) {
+hipError_t launch_attention(AttnShape shape, int cols, bool small_blocks, const AttnParams& p, unsigned grid, hipStream_t s) {
     switch (cols) {
         case 64: return launch_attention_cols<T, 64>(shape, small_blocks, p, grid, s);
         case 128: return launch_attention_cols<T, 128>(shape, small_blocks, p, grid, s);

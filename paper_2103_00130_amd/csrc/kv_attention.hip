@@ -6,25 +6,31 @@
 namespace abft {
 namespace {
 
-// How a call is cut, by what the host knows of it.  most: rows of a wavefront, in sixteens.
+// How a call is cut, by what the host knows of it.
 struct AttnCut {
     AttnShape shape;
     int groups;   // workgroups for the rows of a request and head
     int parts, chunk;
 };
-constexpr int kWanted = 2048;   // workgroups: eight for each compute unit, of which up to four run at a time
-AttnCut cut(int most, int n_req, int heads, int group, int max_new, int max_len) {
+AttnCut cut(int cols, int n_req, int heads, int group, int max_new, int max_len) {
     AttnCut c;
     const int64_t rows = (int64_t)max_new * group;
-    c.shape = rows <= 16 ? kAttnTokens1 : rows <= 16 * most ? kAttnTokens2 : kAttnRows;
-    const int64_t per = c.shape == kAttnTokens1 ? 16 : c.shape == kAttnTokens2 ? 16 * most : 64 * most;
+    const int most = attn_rows_tiles(cols);
+    c.shape = rows <= 16 ? kAttnTokens1 : rows <= 32 ? (most > 1 ? kAttnTokens2 : kAttnTokens1) : kAttnRows;
+    const int64_t per = c.shape == kAttnTokens1 ? 16 : c.shape == kAttnTokens2 ? 32 : 64 * most;
     const int64_t groups = (rows + per - 1) / per;
-    c.groups = (int)(groups < 1 ? 1 : groups > 65535 ? 65535 : groups);
+    c.groups = (int)(groups < 1 ? 1 : groups > 4096 ? 4096 : groups);   // (they take rows in turn)
     const int64_t whole = (int64_t)n_req * heads * c.groups;
-    int64_t parts = whole >= kWanted ? 1 : kWanted / whole;
-    const int64_t longest = ((int64_t)max_len + 255) / 256;
-    parts = parts > longest ? longest : parts;
-    parts = parts < 1 ? 1 : parts;
+    int64_t parts = 1;
+    auto limited = [](int64_t x, int64_t most) { return x < most ? x : most; };
+    if (c.shape == kAttnRows) {
+        if (whole < 400) parts = limited(1024 / whole, (max_len + 511) / 512);
+    } else {
+        const int64_t least = max_len > 16384 ? 512 : 256;
+        const int64_t fill = limited((512 + whole / 2) / whole, (max_len + least - 1) / least), even = limited(2048 / whole, max_len / 2048);
+        parts = fill > even ? fill : even;
+    }
+    if (parts < 1) parts = 1;
     c.chunk = (int)((((int64_t)max_len + parts - 1) / parts + 255) / 256 * 256);
     if (c.chunk < 256) c.chunk = 256;
     c.parts = (int)(((int64_t)max_len + c.chunk - 1) / c.chunk);
@@ -46,13 +52,8 @@ extern "C" {
 size_t abft_kv_attention_workspace_bytes(const abft_kv_cache_t* cache, int n_req, int q_heads, int max_new, int max_len) {
     if (abft::kv_wrong_sizes(cache) || n_req < 1 || q_heads < 1 || q_heads % cache->heads != 0 || max_new < 1 || max_len < 1 || max_len > 0x7ffffe00) return 0;
     const int cols = abft::kv_columns(cache->head_dim);
-    size_t bytes = 0;
-    for (const int digits : {2, 3}) {   // (whatever the type)
-        const abft::AttnCut c = abft::cut(abft::attn_rows_tiles(digits, cols), n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
-        const size_t need = c.parts <= 1 ? 0 : c.parts * abft::part_bytes((int64_t)n_req * max_new * q_heads, cols);
-        bytes = need > bytes ? need : bytes;
-    }
-    return bytes;
+    const abft::AttnCut c = abft::cut(cols, n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
+    return c.parts <= 1 ? 0 : c.parts * abft::part_bytes((int64_t)n_req * max_new * q_heads, cols);
 }
 
 int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_token_stride, int64_t q_head_stride, int type,
@@ -78,7 +79,7 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
     if (n_rows > 0x7fffffffll / q_heads) return abft::set_error(ABFT_EUNSUPPORTED, "%s: n_rows=%lld too large for one launch", fn, (long long)n_rows);
 
     const int cols = abft::kv_columns(cache->head_dim);
-    abft::AttnCut c = abft::cut(abft::attn_rows_tiles(abft::attn_digits(abft::type_size(type)), cols), n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
+    abft::AttnCut c = abft::cut(cols, n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
     const size_t each = abft::part_bytes(n_rows * q_heads, cols);
     if (c.parts > 1 && (!workspace || workspace_bytes / each < (size_t)c.parts)) {
         const size_t fit = workspace ? workspace_bytes / each : 0;
@@ -86,6 +87,8 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
         c.chunk = (int)((((int64_t)max_len + parts - 1) / parts + 255) / 256 * 256);
         c.parts = (int)(((int64_t)max_len + c.chunk - 1) / c.chunk);
     }
+    const int64_t pairs = (int64_t)n_req * cache->heads, workgroups = pairs * c.groups * c.parts;
+    if (workgroups > 0xffffff) return abft::set_error(ABFT_EUNSUPPORTED, "%s: n_req=%d requests of %d heads and %d new tokens are too many for one launch", fn, n_req, cache->heads, max_new);
     abft::AttnParams p;
     p.k_codes = cache->k_codes;
     p.v_codes = cache->v_codes;
@@ -114,7 +117,9 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
     p.block_shift = cache->block_tokens == 16 ? 4 : cache->block_tokens == 32 ? 5 : cache->block_tokens == 64 ? 6 : 7;
     p.width = width;
     p.n_req = n_req;
+    p.groups = c.groups;
     p.parts = c.parts;
+    p.stride = (int)(pairs * 382 / 1000 / 8 * 8 + 1);   // (far, by no simple fraction, and on to the next eighth)
     p.chunk = c.chunk;
     p.scale2 = scale * 1.44269504f;
     p.q_wide = ((reinterpret_cast<uintptr_t>(Q) | (uintptr_t)(q_token_stride * (int64_t)es) | (uintptr_t)(q_head_stride * (int64_t)es) | (uintptr_t)(cache->head_dim * (int64_t)es)) & 15) == 0;
@@ -124,12 +129,11 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
         abft::kv_clear_flags_kernel<<<dim3((unsigned)((n_req + 255) / 256)), dim3(256), 0, s>>>(req_flags, n_req);
         e = hipGetLastError();
     }
-    const dim3 grid((unsigned)c.groups * (unsigned)c.parts, (unsigned)cache->heads, (unsigned)n_req);
     const bool small_blocks = cache->block_tokens < abft::kKvTile;
     if (e == hipSuccess)
-        e = type == ABFT_TYPE_F32 ? abft::launch_attention_f32(c.shape, cols, small_blocks, p, grid, s)
-            : type == ABFT_TYPE_F16 ? abft::launch_attention_f16(c.shape, cols, small_blocks, p, grid, s)
-                                    : abft::launch_attention_bf16(c.shape, cols, small_blocks, p, grid, s);
+        e = type == ABFT_TYPE_F32 ? abft::launch_attention_f32(c.shape, cols, small_blocks, p, (unsigned)workgroups, s)
+            : type == ABFT_TYPE_F16 ? abft::launch_attention_f16(c.shape, cols, small_blocks, p, (unsigned)workgroups, s)
+                                    : abft::launch_attention_bf16(c.shape, cols, small_blocks, p, (unsigned)workgroups, s);
     if (e != hipSuccess) return abft::set_error(ABFT_EHIP, "%s: %s", fn, hipGetErrorString(e));
     return ABFT_OK;
 }

@@ -2,7 +2,7 @@
 #include "kv_attention.h"
 
 namespace abft {
-hipError_t launch_attention_bf16(AttnShape shape, int cols, bool small_blocks, const AttnParams& p, dim3 grid, hipStream_t s) {
+hipError_t launch_attention_bf16(AttnShape shape, int cols, bool small_blocks, const AttnParams& p, unsigned grid, hipStream_t s) {
     return launch_attention<bf16>(shape, cols, small_blocks, p, grid, s);
 }
 }  // namespace abft
