@@ -1,11 +1,12 @@
 // The 8-bit key/value cache: new tokens quantized into it, and tokens read back as values (abft_kv_append and abft_kv_read in
 // include/abft_eb.h).
 //
-// A block and head has one scale, so one workgroup owns a run of tokens of one block for one head, keys or values: it takes the
-// largest value of the run, settles the scale, brings the codes that the block held before to it if it grew, and writes the run's.
-// Keys are written in pieces of a token's columns; values in pieces of 16 tokens of a column, as they stand (a lane gathers them
-// from 16 rows, neighbouring lanes neighbouring columns).  Bound by memory for prompts, by three dependent trips to it (slot, values,
-// scale) for single tokens.
+// A block and head has one scale, so a run of tokens of one block is one wavefront's for each head, and for keys and values: it takes the
+// largest value of the run, settles the scale, brings the codes that the block held before to it if it grew, and writes the
+// run's.  A workgroup looks for runs among some tokens and deals two heads of each to its four wavefronts.  Long runs: a lane has 16 tokens of 8 columns, 16 loads of 16 bytes under way at once, kept in registers from
+// their one read to their codes; what it writes are 8 bytes of 16 rows of keys, or 128 bytes of values as they stand.  Few
+// tokens: a lane has 8 columns of one.  Bound by memory for prompts, by two dependent trips to it (slots, then values and scale) for
+// single tokens.
 #include <hip/hip_runtime.h>
 
 #include "kv_cache.h"
@@ -23,33 +24,66 @@ struct Side {   // keys or values
     const void* x;
     void* out;
     int64_t token_stride, head_stride;
-    bool wide;   // pieces of 8 columns of x (or out) are 16-byte aligned
+    bool wide;   // rows of x (or out) are whole pieces of 8 columns, 16-byte aligned
 };
 struct CacheParams {
     Side side[2];
     const int64_t* slots;
     int64_t n_tokens, limit;   // limit: slots of the cache
-    int heads, dim, cols, block;
-    int window;                // tokens in which a workgroup looks for the beginning of runs
+    int heads, dim, cols, block, shift;   // shift: of a slot to its block
+    int window;                // append: tokens in which a workgroup looks for the beginning of runs; read: heads of a workgroup
 };
 
 constexpr int kNT = 256;
 constexpr int kMaxWindow = 16, kMaxBlock = 128;
 
-// eight columns from `d` on; those past the head are zero
+// Eight columns of a token, as they are stored.
 template <typename T>
-__device__ inline void load_eight(float (&v)[8], const T* row, int d, int dim, bool wide) {
-    if (d + 8 <= dim) {
-        load_values<T, 8>(v, row + d, wide);
+struct Eight {
+    static constexpr int kWords = 2 * sizeof(T);
+    uint32_t w[kWords];
+};
+// From column d on; those past the head are zero.  WIDE: rows are whole aligned pieces of 8 columns.
+template <typename T, bool WIDE>
+__device__ inline void load_eight(Eight<T>& e, const T* row, int d, int dim) {
+    constexpr int PER = 4 / sizeof(T);
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int h = 0; h < Eight<T>::kWords / 4; ++h) {
+            const v4u v = reinterpret_cast<const v4u*>(row + d)[h];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e.w[4 * h + i] = v[i];
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = d + i < dim ? to_f32(row[d + i]) : 0.0f;
+        for (int h = 0; h < Eight<T>::kWords; ++h) {
+            e.w[h] = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int c = d + h * PER + i;
+                const T x = row[min(c, dim - 1)];
+                if constexpr (sizeof(T) == 4) e.w[h] = c < dim ? __builtin_bit_cast(uint32_t, x) : 0u;
+                else e.w[h] |= (c < dim ? (uint32_t)__builtin_bit_cast(uint16_t, x) : 0u) << (16 * i);
+            }
+        }
     }
 }
+template <typename T>
+__device__ inline float value_of(const Eight<T>& e, int i) {
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, e.w[i]);
+    else return to_f32(__builtin_bit_cast(T, (uint16_t)(e.w[i / 2] >> (16 * (i % 2)))));
+}
 
-__device__ inline int code_of(float x, float inv) {
-    const float y = __builtin_rintf(x * inv);
-    return (int)(y != y ? 0.0f : __builtin_amdgcn_fmed3f(y, -127.0f, 127.0f));
+// rne(x * inv) in the low byte of what comes back: what is added leaves a whole number, rounded to nearest even.  A finite x is no
+// larger than 127 scales (and a rounding); of others an infinity becomes 127 and a NaN 0.
+template <bool FINITE>
+__device__ inline uint32_t code_of(float x, float inv) {
+    float y = x * inv;
+    if (!FINITE) y = __builtin_amdgcn_fmed3f(y == y ? y : 0.0f, -127.0f, 127.0f);
+    return __builtin_bit_cast(uint32_t, y + 12582912.0f);
+}
+__device__ inline uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
 __device__ inline uint32_t rescale_word(uint32_t w, float ratio) {
     uint32_t r = 0;
@@ -61,113 +95,203 @@ __device__ inline uint32_t rescale_word(uint32_t w, float ratio) {
     return r;
 }
 
-// tokens t .. t + n - 1 have the slots from `slot` on, all in one block
-template <typename T, bool VALUES>
-__device__ inline void append_run(const CacheParams& p, const Side& s, int head, int64_t t, int n, int64_t slot, float* s_peak) {
-    const int tid = threadIdx.x;
-    const int64_t block = slot / p.block;
-    const int first = (int)(slot % p.block);
-    const T* const x = static_cast<const T*>(s.x) + t * s.token_stride + head * s.head_stride;
-    int8_t* const codes = s.codes + (block * p.heads + head) * p.block * p.cols;
-    float* const scale_at = s.scale + block * p.heads + head;
-
-    const int pieces = (p.dim + 7) / 8;
-    float peak = 0.0f;
-    for (int u = tid; u < n * pieces; u += kNT) {
-        float v[8];
-        load_eight(v, x + (int64_t)(u / pieces) * s.token_stride, u % pieces * 8, p.dim, s.wide);
+__device__ inline float wave_max(float v) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float a = fabsf(v[i]);
-            peak = a < INFINITY ? fmaxf(peak, a) : peak;
-        }
+    for (int m = 1; m < 64; m *= 2) v = fmaxf(v, __shfl_xor(v, m));
+    return v;
+}
+// The largest |x|, as bits that order like the numbers: two halves at a time for 16-bit types.
+template <typename T>
+__device__ inline uint32_t max_bits(uint32_t most, const Eight<T>& e) {
+    typedef uint16_t half2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int h = 0; h < Eight<T>::kWords; ++h) {
+        if constexpr (sizeof(T) == 4) most = max(most, e.w[h] & 0x7fffffffu);
+        else most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(half2, most), __builtin_bit_cast(half2, e.w[h] & 0x7fff7fffu)));
     }
+    return most;
+}
+template <typename T>
+__device__ inline float from_bits(uint32_t most) {
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, most);
+    else return to_f32(__builtin_bit_cast(T, (uint16_t)max(most & 0xffffu, most >> 16)));
+}
+// the largest finite one
+template <typename T>
+__device__ inline float finite_max(float peak, const Eight<T>& e) {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) peak = fmaxf(peak, __shfl_xor(peak, d));
-    if ((tid & 63) == 0) s_peak[tid >> 6] = peak;
-    const float old = first > 0 ? *scale_at : 0.0f;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kNT / 64; ++w) peak = fmaxf(peak, s_peak[w]);
-    const float scale = fmaxf(old, peak > 0.0f ? fmaxf(peak / 127.0f, 0x1p-126f) : 0.0f);
-    const float inv = scale > 0.0f ? 1.0f / scale : 0.0f;
-    const bool grew = first > 0 && scale > old;
-    const float ratio = grew ? old / scale : 1.0f;
-    if (tid == 0) *scale_at = scale;
+    for (int i = 0; i < 8; ++i) {
+        const float a = fabsf(value_of(e, i));
+        peak = a < INFINITY ? fmaxf(peak, a) : peak;
+    }
+    return peak;
+}
+// the run's scale, from the largest value and what the block had
+struct Settled {
+    float scale, inv, ratio;
+    bool grew;
+};
+__device__ inline Settled settle(float peak, float old, int first) {
+    Settled r;
+    r.scale = fmaxf(old, peak > 0.0f ? fmaxf(peak / 127.0f, 0x1p-126f) : 0.0f);
+    r.inv = r.scale > 0.0f ? 1.0f / r.scale : 0.0f;
+    r.grew = first > 0 && r.scale > old;
+    r.ratio = r.grew ? old / r.scale : 1.0f;
+    return r;
+}
 
+// Codes of a run's 16 tokens of 8 columns (those of the group that are the run's), to where they stand.
+template <typename T, bool VALUES, bool FINITE>
+__device__ inline void store_unit(const CacheParams& p, const Eight<T> (&v)[kKvGroup], int8_t* codes, int o, int d, int first, int n, const Settled& r) {
+    const bool whole = o >= first && o + kKvGroup <= first + n;
     if constexpr (!VALUES) {
-        if (grew) {
-            v4u* const held = reinterpret_cast<v4u*>(codes);
-            for (int u = tid; u < first * p.cols / 16; u += kNT) {
-                v4u w = held[u];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = rescale_word(w[i], ratio);
-                held[u] = w;
-            }
-        }
-        for (int u = tid; u < n * pieces; u += kNT) {
-            const int i = u / pieces, d = u % pieces * 8;
-            float v[8];
-            load_eight(v, x + (int64_t)i * s.token_stride, d, p.dim, s.wide);
-            v2u w;
+        for (int j = 0; j < kKvGroup; ++j) {
+            uint32_t c[8];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                w[h] = 0;
-#pragma unroll
-                for (int b = 0; b < 4; ++b) w[h] |= ((uint32_t)code_of(v[4 * h + b], inv) & 255u) << (8 * b);
-            }
-            *reinterpret_cast<v2u*>(codes + (first + i) * p.cols + d) = w;
-        }
-    } else if (!grew && n < kKvGroup) {
-        for (int u = tid; u < n * p.dim; u += kNT) {
-            const int i = u / p.dim, d = u % p.dim, o = first + i;
-            codes[(o / kKvGroup * p.cols + d) * kKvGroup + o % kKvGroup] = (int8_t)code_of(to_f32(x[i * s.token_stride + d]), inv);
+            for (int k = 0; k < 8; ++k) c[k] = code_of<FINITE>(value_of(v[j], k), r.inv);
+            if (o + j >= first && o + j < first + n)
+                *reinterpret_cast<v2u*>(codes + (o + j) * p.cols + d) = v2u{low_bytes(c[0], c[1], c[2], c[3]), low_bytes(c[4], c[5], c[6], c[7])};
         }
     } else {
-        // groups of 16 tokens: from the block's first one if what it held has to be rescaled
-        const int g0 = grew ? 0 : first / kKvGroup, g1 = (first + n - 1) / kKvGroup + 1;
-        for (int u = tid; u < (g1 - g0) * p.dim; u += kNT) {
-            const int g = g0 + u / p.dim, d = u % p.dim, o = g * kKvGroup;
-            v4u* const at = reinterpret_cast<v4u*>(codes + ((int64_t)g * p.cols + d) * kKvGroup);
-            v4u w = {0, 0, 0, 0};
-            if (o < first || o + kKvGroup > first + n) {
-                w = *at;
-                // (what stands past the run is of no token; it may be rescaled with the rest)
-                if (grew)
+        v4u* const group = reinterpret_cast<v4u*>(codes + ((int64_t)o / kKvGroup * p.cols + d) * kKvGroup);
+        v4u mask = {0, 0, 0, 0};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = rescale_word(w[i], ratio);
-            }
+        for (int j = 0; j < kKvGroup; ++j) mask[j / 4] |= o + j >= first && o + j < first + n ? 255u << (8 * (j % 4)) : 0u;
 #pragma unroll
-            for (int j = 0; j < kKvGroup; ++j) {
-                const int i = o + j - first;
-                if (i >= 0 && i < n) {
-                    const uint32_t c = (uint32_t)code_of(to_f32(x[i * s.token_stride + d]), inv) & 255u;
-                    w[j / 4] = (w[j / 4] & ~(255u << (8 * (j % 4)))) | c << (8 * (j % 4));
-                }
+        for (int k = 0; k < 8; ++k) {
+            v4u w;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                w[q] = low_bytes(code_of<FINITE>(value_of(v[4 * q], k), r.inv), code_of<FINITE>(value_of(v[4 * q + 1], k), r.inv),
+                                 code_of<FINITE>(value_of(v[4 * q + 2], k), r.inv), code_of<FINITE>(value_of(v[4 * q + 3], k), r.inv));
+            if (!whole) {   // (what else stands there: tokens before the run, already at its scale, and what is past it, of no token)
+                const v4u was = group[k];
+                w = (w & mask) | (was & ~mask);
             }
-            *at = w;
+            group[k] = w;
         }
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kNT) void kv_append_kernel(const CacheParams p) {
+// A run of n tokens from x on, whose slots begin at token `first` of a block, by one wavefront.  codes: of the block and head.
+template <typename T, bool VALUES, bool WIDE>
+__device__ inline void append_run(const CacheParams& p, const T* x, int64_t stride, int8_t* codes, float* scale_at, int first, int n) {
+    const int lane = threadIdx.x & 63, pieces = (p.dim + 7) / 8, items = n * pieces;
+    const float old = first > 0 ? *scale_at : 0.0f;
+    const bool few = !WIDE || items <= 64;
+    // Few tokens (and rows that are read by elements): a lane has 8 columns of a token, as often as it takes.  Else it has units of 16
+    // tokens of a group and 8 columns, mostly one.
+    const int units = p.block / kKvGroup * pieces;
+    Eight<T> e, v[WIDE ? kKvGroup : 1];
+    // (every token of a group is loaded, from rows that exist, so that the loads go out together)
+    auto load = [&](int o, int d) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < (WIDE ? kKvGroup : 1); ++j) load_eight<T, WIDE>(v[j], x + (int64_t)min(max(o + j - first, 0), n - 1) * stride, d, p.dim);
+    };
+    uint32_t most = 0;
+    if (few) {
+#pragma unroll 1
+        for (int u = lane; u < items; u += 64) {
+            load_eight<T, WIDE>(e, x + (int64_t)(u / pieces) * stride, u % pieces * 8, p.dim);
+            most = max_bits(most, e);
+        }
+    } else if constexpr (WIDE) {
+#pragma unroll 1
+        for (int u = lane; u < units; u += 64) {
+            const int o = u / pieces * kKvGroup, d = u % pieces * 8;
+            if (o + kKvGroup <= first || o >= first + n) continue;
+            load(o, d);
+#pragma unroll
+            for (int j = 0; j < kKvGroup; ++j) most = max_bits(most, v[j]);
+        }
+    }
+    // (as bits: those of an infinity or a NaN are above all others, where a maximum of floats would pass a NaN by)
+    most = __builtin_bit_cast(uint32_t, from_bits<T>(most));
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, m));
+    float peak = __builtin_bit_cast(float, most);
+    const bool finite = most < 0x7f800000u;
+    if (!finite) {
+        peak = 0.0f;
+#pragma unroll 1
+        for (int u = lane; u < items; u += 64) {
+            load_eight<T, WIDE>(e, x + (int64_t)(u / pieces) * stride, u % pieces * 8, p.dim);
+            peak = finite_max(peak, e);
+        }
+        peak = wave_max(peak);
+    }
+    const Settled r = settle(peak, old, first);
+    if (lane == 0) *scale_at = r.scale;
+    if (r.grew) {
+        // all rows of keys before the run, all groups of values that hold any: what stands past them is of no token, or the run's and
+        // written below
+        const int words = VALUES ? (first + kKvGroup - 1) / kKvGroup * p.cols : first * p.cols / 16;
+#pragma unroll 1
+        for (int u = lane; u < words; u += 64) {
+            v4u w = reinterpret_cast<v4u*>(codes)[u];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = rescale_word(w[k], r.ratio);
+            reinterpret_cast<v4u*>(codes)[u] = w;
+        }
+        // (other lanes read and write those groups: their stores are done first)
+        __builtin_amdgcn_s_waitcnt(0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    }
+    if (few) {
+#pragma unroll 1
+        for (int u = lane; u < items; u += 64) {
+            const int o = first + u / pieces, d = u % pieces * 8;
+            if (items > 64 || !finite) load_eight<T, WIDE>(e, x + (int64_t)(u / pieces) * stride, d, p.dim);   // (else it is there)
+            uint32_t c[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) c[k] = code_of<false>(value_of(e, k), r.inv);
+            if constexpr (!VALUES) {
+                *reinterpret_cast<v2u*>(codes + o * p.cols + d) = v2u{low_bytes(c[0], c[1], c[2], c[3]), low_bytes(c[4], c[5], c[6], c[7])};
+            } else {
+                int8_t* const at = codes + (o / kKvGroup * p.cols + d) * kKvGroup + o % kKvGroup;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) at[k * kKvGroup] = (int8_t)c[k];   // (columns are padded to 64)
+            }
+        }
+    } else if constexpr (WIDE) {
+#pragma unroll 1
+        for (int u = lane; u < units; u += 64) {
+            const int o = u / pieces * kKvGroup, d = u % pieces * 8;
+            if (o + kKvGroup <= first || o >= first + n) continue;
+            if (units > 64) load(o, d);   // (with one unit to a lane it is there)
+            if (finite) store_unit<T, VALUES, true>(p, v, codes, o, d, first, n, r);
+            else store_unit<T, VALUES, false>(p, v, codes, o, d, first, n, r);
+        }
+    }
+}
+
+constexpr int kAppendHeads = 2, kAppendWaves = 2 * kAppendHeads;
+template <typename T, bool WIDE>
+__global__ __launch_bounds__(kAppendWaves * 64) void kv_append_kernel(const CacheParams p) {
     __shared__ int64_t s_slot[kMaxWindow + kMaxBlock + 1];   // of the token before the window, the window, and what a run can reach
-    __shared__ float s_peak[kNT / 64];
-    const int tid = threadIdx.x, lane = tid & 63, head = blockIdx.y;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t t0 = (int64_t)blockIdx.x * p.window;
     const int ahead = p.window + p.block + 1;
-    for (int i = tid; i < ahead; i += kNT) {
+    for (int i = threadIdx.x; i < ahead; i += kAppendWaves * 64) {
         const int64_t t = t0 - 1 + i;
         const int64_t v = t >= 0 && t < p.n_tokens ? p.slots[t] : -1;
         s_slot[i] = v >= 0 && v < p.limit ? v : -1;
     }
     __syncthreads();
-    for (int w = 0; w < p.window; ++w) {
-        const int64_t slot = s_slot[w + 1];
-        if (slot < 0) continue;
-        const int first = (int)(slot % p.block);
-        if (first > 0 && s_slot[w] == slot - 1) continue;   // inside a run that began before
+    // the tokens of the window that begin a run: those that do not continue the slot before them within its block
+    bool begins = false;
+    if (lane < p.window) {
+        const int64_t slot = s_slot[lane + 1];
+        begins = slot >= 0 && (((int)slot & (p.block - 1)) == 0 || s_slot[lane] != slot - 1);
+    }
+    unsigned long long left = __ballot(begins);
+    const int side = wave & 1, head = blockIdx.y * kAppendHeads + (wave >> 1);
+    if (head >= p.heads) return;
+    for (; left; left &= left - 1) {
+        const int w = __builtin_ctzll(left);
+        const int64_t slot = s_slot[w + 1], block = slot >> p.shift;
+        const int first = (int)slot & (p.block - 1);
         // the run's length: how many slots count up from here without leaving the block
         int n = 0;
 #pragma unroll
@@ -177,66 +301,111 @@ __global__ __launch_bounds__(kNT) void kv_append_kernel(const CacheParams p) {
             const unsigned long long b = __ballot(on);
             if (n == h * 64) n += b == ~0ull ? 64 : __builtin_ctzll(~b);
         }
-        if (blockIdx.z == 0) append_run<T, false>(p, p.side[0], head, t0 + w, n, slot, s_peak);
-        else append_run<T, true>(p, p.side[1], head, t0 + w, n, slot, s_peak);
-        __syncthreads();   // (s_peak is used again)
+        const Side& s = p.side[side];
+        const T* const x = static_cast<const T*>(s.x) + (t0 + w) * s.token_stride + head * s.head_stride;
+        int8_t* const codes = s.codes + (block * p.heads + head) * p.block * p.cols;
+        float* const scale_at = s.scale + block * p.heads + head;
+        if (side == 0) append_run<T, false, WIDE>(p, x, s.token_stride, codes, scale_at, first, n);
+        else append_run<T, true, WIDE>(p, x, s.token_stride, codes, scale_at, first, n);
     }
 }
 
+// Reading: a workgroup has 16 tokens and p.window of their heads.  Where their slots are a whole group of a block, a thread has 8 of them and 8
+// columns, 8 loads under way at once; else a token's 8 columns, a byte at a time from values.
 constexpr int kReadTokens = 16;
 template <typename T>
+__device__ inline void store_eight(T* out, const float (&f)[8], float scale, int columns, bool wide) {
+    T v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = from_f32<T>(f[i] * scale);
+    if (wide) {
+        constexpr int PER = 16 / sizeof(T);
+        typedef T piece __attribute__((ext_vector_type(PER)));
+#pragma unroll
+        for (int i = 0; i < 8 / PER; ++i) {
+            piece q;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) q[j] = v[i * PER + j];
+            reinterpret_cast<piece*>(out)[i] = q;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < columns) out[i] = v[i];
+    }
+}
+__device__ inline float byte_of(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
+
+template <typename T>
 __global__ __launch_bounds__(kNT) void kv_read_kernel(const CacheParams p, int side0) {
-    const int head = blockIdx.y, which = side0 + blockIdx.z;
+    __shared__ int64_t s_slot[kReadTokens];
+    const int which = side0 + blockIdx.y, tid = threadIdx.x, head0 = blockIdx.z * p.window, heads = min(p.window, p.heads - head0);
     const Side& s = p.side[which];
     const int64_t t0 = (int64_t)blockIdx.x * kReadTokens;
-    const int pieces = (p.dim + 7) / 8;
-    for (int u = threadIdx.x; u < kReadTokens * pieces; u += kNT) {
-        const int64_t t = t0 + u / pieces;
-        if (t >= p.n_tokens) break;
-        const int d = u % pieces * 8;
-        const int64_t slot = p.slots[t];
-        const bool held = slot >= 0 && slot < p.limit;
-        const int64_t block = held ? slot / p.block : 0;
-        const int o = held ? (int)(slot % p.block) : 0;
-        const int8_t* const codes = s.codes + (block * p.heads + head) * p.block * p.cols;
-        const float scale = held ? s.scale[block * p.heads + head] : 0.0f;
-        uint32_t w[2] = {0, 0};
-        if (held) {
+    const int tokens = (int)min(p.n_tokens - t0, (int64_t)kReadTokens), pieces = (p.dim + 7) / 8, per_head = p.block * p.cols;
+    if (tid < kReadTokens) s_slot[tid] = tid < tokens ? p.slots[t0 + tid] : -1;
+    __syncthreads();
+    const int64_t slot0 = s_slot[0];
+    const bool group = __all(s_slot[tid & 15] == slot0 + (tid & 15)) && slot0 >= 0 && slot0 < p.limit && (slot0 & 15) == 0;
+    if (group) {
+        const int64_t block = slot0 >> p.shift;
+        const int o = (int)slot0 & (p.block - 1), units = heads * pieces * 2;
+        for (int u = tid; u < units; u += kNT) {
+            // (neighbouring threads: neighbouring columns)
+            const int half = u / (pieces * heads), rest = u - half * (pieces * heads), h = rest / pieces, head = head0 + h, d = (rest - h * pieces) * 8;
+            const int8_t* const codes = s.codes + (block * p.heads + head) * per_head;
+            v2u w[8];
+            if (which == 0) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const v2u*>(codes + (o + 8 * half + j) * p.cols + d);
+            } else {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) w[c] = *reinterpret_cast<const v2u*>(codes + (o / kKvGroup * p.cols + d + c) * kKvGroup + 8 * half);   // (columns are padded to 64)
+            }
+            const float scale = s.scale[block * p.heads + head];
+            T* const out = static_cast<T*>(s.out) + (t0 + 8 * half) * s.token_stride + head * s.head_stride + d;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float f[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) f[c] = which == 0 ? byte_of(w[j][c / 4], c % 4) : byte_of(w[c][j / 4], j % 4);
+                store_eight<T>(out + j * s.token_stride, f, scale, p.dim - d, s.wide);
+            }
+        }
+    } else {
+        const int units = tokens * heads * pieces;
+        for (int u = tid; u < units; u += kNT) {
+            const int row = u / pieces, t = row / heads, head = head0 + (row - t * heads), d = (u - row * pieces) * 8;
+            const int64_t slot = s_slot[t];
+            const bool held = slot >= 0 && slot < p.limit;
+            const int64_t block = held ? slot >> p.shift : 0;
+            const int o = held ? (int)slot & (p.block - 1) : 0;
+            const int8_t* const codes = s.codes + (block * p.heads + head) * per_head;
+            const float scale = s.scale[block * p.heads + head];
+            uint32_t w[2];
             if (which == 0) {
                 const v2u v = *reinterpret_cast<const v2u*>(codes + o * p.cols + d);
                 w[0] = v[0];
                 w[1] = v[1];
             } else {
-                const int8_t* const at = codes + (o / kKvGroup * p.cols + d) * kKvGroup + o % kKvGroup;
+                const uint8_t* const at = reinterpret_cast<const uint8_t*>(codes) + (o / kKvGroup * p.cols + d) * kKvGroup + o % kKvGroup;
+                uint32_t b[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i / 4] |= (uint32_t)(uint8_t)at[i * kKvGroup] << (8 * (i % 4));   // (columns are padded to 64)
+                for (int i = 0; i < 8; ++i) b[i] = at[i * kKvGroup];
+                w[0] = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
+                w[1] = b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24;
             }
-        }
-        T v[8];
+            float f[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = from_f32<T>((float)(int8_t)(w[i / 4] >> (8 * (i % 4))) * scale);
-        T* const out = static_cast<T*>(s.out) + t * s.token_stride + head * s.head_stride + d;
-        if (d + 8 <= p.dim && s.wide) {
-            constexpr int PER = 16 / sizeof(T);
-            typedef T piece __attribute__((ext_vector_type(PER)));
-#pragma unroll
-            for (int i = 0; i < 8 / PER; ++i) {
-                piece q;
-#pragma unroll
-                for (int j = 0; j < PER; ++j) q[j] = v[i * PER + j];
-                reinterpret_cast<piece*>(out)[i] = q;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (d + i < p.dim) out[i] = v[i];
+            for (int c = 0; c < 8; ++c) f[c] = held ? byte_of(w[c / 4], c % 4) : 0.0f;   // (a scale that is no number would not let a code of zero be zero)
+            store_eight<T>(static_cast<T*>(s.out) + (t0 + t) * s.token_stride + head * s.head_stride + d, f, held ? scale : 0.0f, p.dim - d, s.wide);
         }
     }
 }
 
-bool pieces_aligned(const void* x, int64_t token_stride, int64_t head_stride, int type) {
+bool pieces_aligned(const void* x, int64_t token_stride, int64_t head_stride, int dim, int type) {
     const int64_t es = type_size(type);
-    return ((reinterpret_cast<uintptr_t>(x) | (uintptr_t)(token_stride * es) | (uintptr_t)(head_stride * es)) & 15) == 0;
+    return dim % 8 == 0 && ((reinterpret_cast<uintptr_t>(x) | (uintptr_t)(token_stride * es) | (uintptr_t)(head_stride * es)) & 15) == 0;
 }
 
 // what append and read have in common; 0, or an error code
@@ -248,9 +417,9 @@ int fill(CacheParams& p, const char* fn, const abft_kv_cache_t* c, const void* K
     if (n_tokens > 0 && !slots) return set_error(ABFT_EINVAL, "%s: null pointer", fn);
     const uintptr_t es = (uintptr_t)type_size(type);
     if (reinterpret_cast<uintptr_t>(K) % es || reinterpret_cast<uintptr_t>(V) % es) return set_error(ABFT_EINVAL, "%s: K or V is not aligned to its type", fn);
-    if ((n_tokens + kReadTokens - 1) / kReadTokens > 0x7fffffll) return set_error(ABFT_EUNSUPPORTED, "%s: n_tokens=%lld too large for one launch", fn, (long long)n_tokens);
-    p.side[0] = {c->k_codes, c->k_scale, K, const_cast<void*>(K), kt, kh, pieces_aligned(K, kt, kh, type)};
-    p.side[1] = {c->v_codes, c->v_scale, V, const_cast<void*>(V), vt, vh, pieces_aligned(V, vt, vh, type)};
+    if (n_tokens > 0xffffffll) return set_error(ABFT_EUNSUPPORTED, "%s: n_tokens=%lld too large for one launch", fn, (long long)n_tokens);
+    p.side[0] = {c->k_codes, c->k_scale, K, const_cast<void*>(K), kt, kh, pieces_aligned(K, kt, kh, c->head_dim, type)};
+    p.side[1] = {c->v_codes, c->v_scale, V, const_cast<void*>(V), vt, vh, pieces_aligned(V, vt, vh, c->head_dim, type)};
     p.slots = slots;
     p.n_tokens = n_tokens;
     p.limit = (int64_t)c->n_blocks * c->block_tokens;
@@ -258,8 +427,16 @@ int fill(CacheParams& p, const char* fn, const abft_kv_cache_t* c, const void* K
     p.dim = c->head_dim;
     p.cols = kv_columns(c->head_dim);
     p.block = c->block_tokens;
+    p.shift = p.block == 16 ? 4 : p.block == 32 ? 5 : p.block == 64 ? 6 : 7;
     p.window = 1;
     return ABFT_OK;
+}
+
+template <typename T>
+void launch_append(const CacheParams& p, hipStream_t s) {
+    const dim3 grid((unsigned)((p.n_tokens + p.window - 1) / p.window), (unsigned)((p.heads + kAppendHeads - 1) / kAppendHeads)), threads(kAppendWaves * 64);
+    if (p.side[0].wide && p.side[1].wide) kv_append_kernel<T, true><<<grid, threads, 0, s>>>(p);
+    else kv_append_kernel<T, false><<<grid, threads, 0, s>>>(p);
 }
 
 }  // namespace
@@ -280,13 +457,14 @@ int abft_kv_append(const abft_kv_cache_t* cache, const void* K, int64_t k_token_
     if (rc != ABFT_OK) return rc;
     if (n_tokens == 0) return ABFT_OK;
     if (!K || !V) return abft::set_error(ABFT_EINVAL, "%s: null pointer", fn);
-    // single tokens get a workgroup each; of many, most lie inside runs, and a workgroup looks at some
-    p.window = n_tokens * p.heads <= 1024 ? 1 : abft::kMaxWindow;
-    const dim3 grid((unsigned)((n_tokens + p.window - 1) / p.window), (unsigned)p.heads, 2);
+    // A workgroup looks for runs among so many tokens: few, so that single tokens do not wait for each other, while that makes up to 2048
+    // workgroups; of more tokens most lie inside runs, and the workgroups that find none would hold up the others.
+    const int64_t all = n_tokens * ((p.heads + abft::kAppendHeads - 1) / abft::kAppendHeads);
+    while (p.window < abft::kMaxWindow && all > 2048ll * p.window) p.window *= 2;
     hipStream_t s = (hipStream_t)stream;
-    if (type == ABFT_TYPE_F32) abft::kv_append_kernel<float><<<grid, dim3(abft::kNT), 0, s>>>(p);
-    else if (type == ABFT_TYPE_F16) abft::kv_append_kernel<abft::f16><<<grid, dim3(abft::kNT), 0, s>>>(p);
-    else abft::kv_append_kernel<abft::bf16><<<grid, dim3(abft::kNT), 0, s>>>(p);
+    if (type == ABFT_TYPE_F32) abft::launch_append<float>(p, s);
+    else if (type == ABFT_TYPE_F16) abft::launch_append<abft::f16>(p, s);
+    else abft::launch_append<abft::bf16>(p, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return abft::set_error(ABFT_EHIP, "%s: %s", fn, hipGetErrorString(e));
     return ABFT_OK;
@@ -299,7 +477,11 @@ int abft_kv_read(const abft_kv_cache_t* cache, const int64_t* slots, int64_t n_t
     const int rc = abft::fill(p, fn, cache, K, k_token_stride, k_head_stride, V, v_token_stride, v_head_stride, type, slots, n_tokens);
     if (rc != ABFT_OK) return rc;
     if (n_tokens == 0 || (!K && !V)) return ABFT_OK;
-    const dim3 grid((unsigned)((n_tokens + abft::kReadTokens - 1) / abft::kReadTokens), (unsigned)p.heads, K && V ? 2 : 1);
+    // all heads of its tokens are a workgroup's where there are enough of them
+    const int64_t windows = (n_tokens + abft::kReadTokens - 1) / abft::kReadTokens;
+    p.window = p.heads;
+    while (p.window > 1 && windows * ((p.heads + p.window - 1) / p.window) < 512) p.window = (p.window + 1) / 2;
+    const dim3 grid((unsigned)windows, K && V ? 2 : 1, (unsigned)((p.heads + p.window - 1) / p.window));
     hipStream_t s = (hipStream_t)stream;
     const int side0 = K ? 0 : 1;
     if (type == ABFT_TYPE_F32) abft::kv_read_kernel<float><<<grid, dim3(abft::kNT), 0, s>>>(p, side0);

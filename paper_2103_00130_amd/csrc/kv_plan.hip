@@ -28,33 +28,49 @@ struct PlanParams {
     int32_t* req_flags;
     int32_t* taken;
     int64_t ldt, n_slots;
-    int n_req, block, width, n_free;
+    uint64_t inverse;   // floor((2^64 - 1) / block) + 1
+    int n_req, block, shift, width, n_free;   // shift: log2 of the block, or -1
 };
 
-// sum over the threads before this one; *total: over all.  s: one word per wavefront
+// x / block for any 32-bit x: a shift, or the upper half of a product with the block's inverse, whose error of less than 2^-32 of a
+// quotient cannot carry it to the next whole number (the general 64-bit division is a hundred instructions).
+__device__ inline uint32_t blocks_below(const PlanParams& p, uint32_t x) { return p.shift >= 0 ? x >> p.shift : (uint32_t)__umul64hi(p.inverse, x); }
+__device__ inline int64_t blocks_for(const PlanParams& p, int64_t tokens) { return tokens > 0 ? (int64_t)blocks_below(p, (uint32_t)(tokens - 1)) + 1 : 0; }
+
+// Sums that stop at 2^31 - 1, which no count that matters reaches: so they fit 32 bits, and are in any order what they are in one.
+__device__ inline uint32_t add31(uint32_t a, uint32_t b) { return min(a + b, 0x7fffffffu); }
+// over the lanes up to and with this one: within rows of 16 lanes, then from row to row
+__device__ inline uint32_t wave_scan(uint32_t x) {
+    x = add31(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));
+    x = add31(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+    x = add31(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+    x = add31(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+    x = add31(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));
+    return add31(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));
+}
+// Two sums over the threads before this one, and over all.  s: two words per wavefront
+struct Two {
+    uint32_t rows, need;
+};
 template <int NT>
-__device__ inline int64_t block_scan(int64_t v, int64_t* s, int64_t* total) {
+__device__ inline Two block_scan(Two v, Two* s, Two* total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t x = v;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    if (lane == 63) s[wave] = x;
+    const Two upto = {wave_scan(v.rows), wave_scan(v.need)};
+    if (lane == 63) s[wave] = upto;
     __syncthreads();
-    int64_t before = 0, all = 0;
+    Two before = {0, 0}, all = {0, 0};
 #pragma unroll
     for (int w = 0; w < NT / 64; ++w) {
-        if (w < wave) before += s[w];
-        all += s[w];
+        const Two x = s[w];
+        if (w < wave) before = {add31(before.rows, x.rows), add31(before.need, x.need)};
+        all = {add31(all.rows, x.rows), add31(all.need, x.need)};
     }
     __syncthreads();
     *total = all;
-    return before + x - v;
+    // (what the lanes before this one have, not a difference: a sum that stopped has lost it)
+    const uint32_t r = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane - 1), (int)upto.rows), n = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane - 1), (int)upto.need);
+    return {add31(before.rows, lane ? r : 0), add31(before.need, lane ? n : 0)};
 }
-
-__device__ inline uint32_t clamp31(int64_t v) { return v > 0x7fffffffll ? 0x7fffffffu : (uint32_t)v; }
 
 // the first request whose sum, without its mark, is larger than v; n if none is
 __device__ inline int first_above(const uint32_t* sums, int n, uint32_t v) {
@@ -67,55 +83,69 @@ __device__ inline int first_above(const uint32_t* sums, int n, uint32_t v) {
     return lo;
 }
 
-template <int NT>
+// NT threads, each of which takes up to PER neighbouring requests.
+template <int NT, int PER>
 __global__ __launch_bounds__(NT) void kv_plan_kernel(const PlanParams p) {
+    constexpr bool kKeepCtx = PER <= 4;          // (for more requests there is no room in LDS)
     extern __shared__ uint32_t s_dyn[];
     uint32_t* const s_rows = s_dyn;              // rows up to and with a request, marked if it is refused
     uint32_t* const s_upto = s_dyn + p.n_req;    // blocks needed up to and with it
-    __shared__ int64_t s_wave[NT / 64];
+    int32_t* const s_ctx = reinterpret_cast<int32_t*>(s_dyn + 2 * p.n_req);
+    __shared__ Two s_wave[NT / 64];
     __shared__ int s_taken;
     const int tid = threadIdx.x;
     if (tid == 0) s_taken = 0;
 
-    // each thread takes neighbouring requests
-    const int per = (p.n_req + NT - 1) / NT, r0 = min(tid * per, p.n_req), r1 = min(r0 + per, p.n_req);
-    int64_t rows = 0, all_rows, all_need;
-    for (int r = r0; r < r1; ++r) rows += max(p.fresh[r], 0);
-    const int64_t rows_before = block_scan<NT>(rows, s_wave, &all_rows);
-    int64_t need = 0;
-    rows = rows_before;
-    for (int r = r0; r < r1; ++r) {
-        const int64_t ctx = max(p.ctx[r], 0), fresh = max(p.fresh[r], 0);
-        rows += fresh;
-        const int64_t have = (ctx + p.block - 1) / p.block, want = (ctx + fresh + p.block - 1) / p.block;
-        if (want <= p.width && rows <= p.n_slots) need += want - have;
+    const int per = (p.n_req + NT - 1) / NT, r0 = min(tid * per, p.n_req), count = min(per, p.n_req - r0);
+    int32_t ctx_in[PER], fresh_in[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int r = min(r0 + i, p.n_req - 1);
+        ctx_in[i] = i < count ? p.ctx[r] : 0;
+        fresh_in[i] = i < count ? p.fresh[r] : 0;
     }
-    const int64_t need_before = block_scan<NT>(need, s_wave, &all_need);
-    rows = rows_before;
-    need = need_before;
+    // blocks a request holds and wants, unless its row of the table is too short
+    auto held = [&](int i) __attribute__((always_inline)) { return blocks_for(p, max(ctx_in[i], 0)); };
+    auto wanted = [&](int i) __attribute__((always_inline)) { return blocks_for(p, (int64_t)max(ctx_in[i], 0) + max(fresh_in[i], 0)); };
+    auto sums = [&](uint32_t rows_before, bool limited) __attribute__((always_inline)) {
+        Two t = {0, 0};
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            t.rows = add31(t.rows, (uint32_t)max(fresh_in[i], 0));
+            const int64_t want = wanted(i);
+            if (want <= p.width && !(limited && add31(rows_before, t.rows) > p.n_slots)) t.need = add31(t.need, (uint32_t)(want - held(i)));
+        }
+        return t;
+    };
+    Two all, before = block_scan<NT>(sums(0, false), s_wave, &all);
+    if (all.rows > p.n_slots) before.need = block_scan<NT>(sums(before.rows, true), s_wave, &all).need;   // some have no rows, and so need no blocks
+    uint32_t rows = before.rows, need = before.need;
     int most = 0;
     // the requests whose outputs this workgroup writes
     const int wr = (p.n_req + gridDim.x - 1) / gridDim.x, w0 = min((int)blockIdx.x * wr, p.n_req), w1 = min(w0 + wr, p.n_req);
-    for (int r = r0; r < r1; ++r) {
-        const int32_t ctx_in = p.ctx[r], fresh_in = p.fresh[r];
-        const int64_t ctx = max(ctx_in, 0), fresh = max(fresh_in, 0);
-        rows += fresh;
-        const int64_t have = (ctx + p.block - 1) / p.block, want = (ctx + fresh + p.block - 1) / p.block;
-        int why = 0;
-        if (want > p.width) why |= ABFT_KV_TABLE_FULL;
-        if (rows > p.n_slots) why |= ABFT_KV_NO_ROW;
-        const int64_t n = why == 0 ? want - have : 0;
-        need += n;
-        if (n > 0) {
-            if (need > p.n_free) why |= ABFT_KV_NO_BLOCK;
-            else most = max(most, (int)need);
-        }
-        s_rows[r] = clamp31(rows) | (why ? kRefused : 0u);
-        s_upto[r] = clamp31(need);
-        if (r >= w0 && r < w1) {
-            p.req_flags[r] = why | (ctx_in < 0 || fresh_in < 0 ? ABFT_KV_BAD_LENGTH : 0);
-            p.seq_len[r] = (int32_t)(why ? ctx : ctx + fresh);
-            p.cu_new[r + 1] = (int32_t)min(rows, p.n_slots);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (i < count) {
+            const int r = r0 + i;
+            const int64_t ctx = max(ctx_in[i], 0), fresh = max(fresh_in[i], 0), have = held(i), want = wanted(i);
+            rows = add31(rows, (uint32_t)fresh);
+            int why = 0;
+            if (want > p.width) why |= ABFT_KV_TABLE_FULL;
+            if (rows > p.n_slots) why |= ABFT_KV_NO_ROW;
+            const int64_t n = why == 0 ? want - have : 0;
+            need = add31(need, (uint32_t)n);
+            if (n > 0) {
+                if (need > (uint32_t)p.n_free) why |= ABFT_KV_NO_BLOCK;
+                else most = max(most, (int)need);
+            }
+            s_rows[r] = rows | (why ? kRefused : 0u);
+            s_upto[r] = need;
+            if (kKeepCtx) s_ctx[r] = (int32_t)ctx;
+            if (r >= w0 && r < w1) {
+                p.req_flags[r] = why | (ctx_in[i] < 0 || fresh_in[i] < 0 ? ABFT_KV_BAD_LENGTH : 0);
+                p.seq_len[r] = (int32_t)(why ? ctx : ctx + fresh);
+                p.cu_new[r + 1] = (int32_t)min((int64_t)rows, p.n_slots);
+            }
         }
     }
     if (most > 0) atomicMax(&s_taken, most);
@@ -124,23 +154,24 @@ __global__ __launch_bounds__(NT) void kv_plan_kernel(const PlanParams p) {
         p.cu_new[0] = 0;
         *p.taken = s_taken;
     }
+    auto ctx_of = [&](int r) __attribute__((always_inline)) { return (int64_t)(kKeepCtx ? s_ctx[r] : max(p.ctx[r], 0)); };
 
     // new blocks: the u-th free one belongs to the first request that needs more than u up to itself
     const int stride = (int)gridDim.x * NT, first = (int)blockIdx.x * NT + tid;
     for (int64_t u = first; u < s_taken; u += stride) {
         const int r = first_above(s_upto, p.n_req, (uint32_t)u);
-        const int64_t have = ((int64_t)max(p.ctx[r], 0) + p.block - 1) / p.block;
+        const int64_t have = blocks_for(p, ctx_of(r));
         p.table[(int64_t)r * p.ldt + have + (u - (r > 0 ? s_upto[r - 1] : 0u))] = p.free_blocks[u];
     }
     for (int64_t t = first; t < p.n_slots; t += stride) {
         const int r = first_above(s_rows, p.n_req, (uint32_t)t);
         int64_t slot = -1;
         if (r < p.n_req && !(s_rows[r] & kRefused)) {
-            const int64_t ctx = max(p.ctx[r], 0), have = (ctx + p.block - 1) / p.block;
-            const int64_t pos = ctx + (t - (r > 0 ? s_rows[r - 1] & ~kRefused : 0u)), at = pos / p.block;
+            const int64_t ctx = ctx_of(r), have = blocks_for(p, ctx);
+            const int64_t pos = ctx + (t - (r > 0 ? s_rows[r - 1] & ~kRefused : 0u)), at = blocks_below(p, (uint32_t)pos);
             const int64_t before = r > 0 ? s_upto[r - 1] : 0u;
             const int32_t b = at < have ? p.table[(int64_t)r * p.ldt + at] : p.free_blocks[before + at - have];
-            slot = (int64_t)b * p.block + pos % p.block;
+            slot = (int64_t)b * p.block + (pos - at * p.block);
         }
         p.slots[t] = slot;
     }
@@ -161,17 +192,22 @@ extern "C" int abft_kv_plan(const int32_t* ctx_len, const int32_t* new_len, int 
     if (ldt < width) return abft::set_error(ABFT_EINVAL, "%s: ldt=%lld smaller than width=%d", fn, (long long)ldt, width);
     if (n_req > abft::kMaxRequests) return abft::set_error(ABFT_EUNSUPPORTED, "%s: n_req=%d (at most %d)", fn, n_req, abft::kMaxRequests);
     if (n_slots >= 0x7fffffffll) return abft::set_error(ABFT_EUNSUPPORTED, "%s: n_slots=%lld too large", fn, (long long)n_slots);
-    abft::PlanParams p{ctx_len, new_len, free_blocks, table, seq_len, cu_new, slots, req_flags, taken, ldt, n_slots, n_req, block_tokens, width, n_free};
-    const size_t lds = (size_t)n_req * 8;
+    abft::PlanParams p{ctx_len, new_len, free_blocks, table, seq_len, cu_new, slots, req_flags, taken, ldt, n_slots, ~0ull / (uint64_t)block_tokens + 1, n_req, block_tokens, -1, width, n_free};
+    for (int k = 0; k < 31; ++k)
+        if (block_tokens == 1 << k) p.shift = k;
     const int nt = n_req <= 256 ? 256 : 1024;
     const int64_t groups = (n_slots + nt - 1) / nt;
-    const unsigned grid = (unsigned)(groups < 1 ? 1 : groups > 256 ? 256 : groups);
-    if (nt == 256) abft::kv_plan_kernel<256><<<dim3(grid), dim3(256), lds, (hipStream_t)stream>>>(p);
-    else {
+    const dim3 grid((unsigned)(groups < 1 ? 1 : groups > 256 ? 256 : groups));
+    hipStream_t s = (hipStream_t)stream;
+    if (n_req <= 256) {
+        abft::kv_plan_kernel<256, 1><<<grid, dim3(256), (size_t)n_req * 12, s>>>(p);
+    } else if (n_req <= 4096) {
+        abft::kv_plan_kernel<1024, 4><<<grid, dim3(1024), (size_t)n_req * 12, s>>>(p);
+    } else {
         static std::atomic<uint64_t> done{0};
-        const hipError_t e = abft::allow_dynamic_lds(reinterpret_cast<const void*>(abft::kv_plan_kernel<1024>), abft::kMaxRequests * 8, done);
+        const hipError_t e = abft::allow_dynamic_lds(reinterpret_cast<const void*>(abft::kv_plan_kernel<1024, 16>), abft::kMaxRequests * 8, done);
         if (e != hipSuccess) return abft::set_error(ABFT_EHIP, "%s: %s", fn, hipGetErrorString(e));
-        abft::kv_plan_kernel<1024><<<dim3(grid), dim3(1024), lds, (hipStream_t)stream>>>(p);
+        abft::kv_plan_kernel<1024, 16><<<grid, dim3(1024), (size_t)n_req * 8, s>>>(p);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return abft::set_error(ABFT_EHIP, "%s: %s", fn, hipGetErrorString(e));
