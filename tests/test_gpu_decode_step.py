@@ -1,0 +1,229 @@
+"""The operators of a decoding step together, as `decode_step` runs them, against the definitions in 64 bits; and the cases of the cache that
+need many tokens or a large cache."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode_oracle as o
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2103_00130_amd import binding
+    assert torch.cuda.is_available()
+    return binding
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).to("cuda")
+    return t if dtype is None else t.to(dtype)
+
+
+def f64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def within(got, want, tol, what):
+    off = np.abs(got - want) > tol
+    assert not (off | ~np.isfinite(got)).any(), f"{what}: {off.sum()} of {got.size} beyond the bound"
+
+
+# ---------------------------------------------------------------------------------------------------------------- together
+HIDDEN, Q_HEADS, HEADS, DIM, BLOCK = 96, 6, 2, 40, 16
+
+
+def weights(b, rng):
+    """(handles, (codes, scale, bias) of each in numpy)"""
+    out = []
+    for n, k in (((Q_HEADS + 2 * HEADS) * DIM, HIDDEN), (HIDDEN, Q_HEADS * DIM)):
+        W = rng.integers(0, 256, (n, k // 2), dtype=np.uint8)
+        scale = torch.full((n, -(-k // 32)), (21.25 * k) ** -0.5)
+        bias = scale * -7.5
+        out.append((b.abft_w4_pack(dev(W), scale.cuda(), bias.cuda(), K=k, group=32), (W, f64(scale), f64(bias))))
+    return [x[0] for x in out], [x[1] for x in out]
+
+
+def make_layer(handles, requests, longest, most_rows):
+    from paper_2103_00130_amd import decode_step
+    return decode_step.DecodeLayer(*handles, Q_HEADS, HEADS, DIM, requests, longest, most_rows, BLOCK, torch.float32)
+
+
+def test_prompts_then_single_tokens(b):
+    """Every stage of every step against its definition applied to what the stage before it gave."""
+    rng = np.random.default_rng(11)
+    handles, plain = weights(b, rng)
+    steps = [[5, 0, 33, 16], [1, 1, 1, 1], [1, 1, 1, 1], [0, 40, 1, 0], [1, 1, 1, 1], [11, 1, 0, 1]]
+    total = np.sum(steps, axis=0)
+    layer = make_layer(handles, 4, int(total.max()), 64)
+    parts = [np.zeros((layer.cache.n_blocks, HEADS, BLOCK, DIM), np.int8) for _ in range(2)]
+    scales = [np.zeros((layer.cache.n_blocks, HEADS), np.float32) for _ in range(2)]
+    held, split = np.zeros(4, np.int64), Q_HEADS * DIM
+    for new in steps:
+        n = sum(new)
+        x = torch.from_numpy(rng.standard_normal((n, HIDDEN)).astype(np.float32)).cuda()
+        y = layer.step(x, new)
+        held += new
+        assert list(held) == layer.lengths
+        qkv = f64(layer.qkv[:n])
+        within(qkv, *o.w4_product(f64(x), *plain[0], 32, "f32"), "first projection")
+        slots, table = layer.slots[:n].cpu().numpy(), layer.table.cpu().numpy()
+        # the host's count of blocks is the plan's, and no two requests share one
+        assert not layer.flags.any() and np.array_equal(layer.seq.cpu().numpy(), held)
+        taken = np.concatenate([row[:-(-int(m) // BLOCK)] for row, m in zip(table, held)])
+        assert len(taken) == len(set(taken)) == layer.used
+        where = np.concatenate([np.arange(m - c, m) for m, c in zip(held, new)])
+        who = np.repeat(np.arange(4), new)
+        assert np.array_equal(slots, table[who, where // BLOCK] * BLOCK + where % BLOCK)
+        for i in range(2):
+            o.append(parts[i], scales[i], qkv[:, split + i * HEADS * DIM:split + (i + 1) * HEADS * DIM].reshape(n, HEADS, DIM).astype(np.float32), slots)
+        for got, want, gs, ws in zip(layer.cache.codes(), parts, (layer.cache.k_scale, layer.cache.v_scale), scales):
+            got, gs = got.cpu().numpy(), gs.cpu().numpy()
+            for r in range(4):
+                for j in range(int(held[r])):
+                    assert np.array_equal(got[table[r, j // BLOCK], :, j % BLOCK], want[table[r, j // BLOCK], :, j % BLOCK])
+            assert np.array_equal(gs[taken], ws[taken])
+        cu = np.concatenate([[0], np.cumsum(new)])
+        mid = f64(layer.mid[:n])
+        want, tol, _, _ = o.attention(qkv[:, :split].reshape(n, Q_HEADS, DIM), *parts, *scales, table, held, cu, DIM ** -0.5, "f32")
+        within(mid, want, tol, "attention")
+        within(f64(y), *o.w4_product(mid.reshape(n, -1), *plain[1], 32, "f32"), "second projection")
+
+
+def test_steps_replayed_from_a_graph_are_the_steps_run(b):
+    """Replays, with work and synchronization of the program's own between them, against the same steps run: the same bits."""
+    rng = np.random.default_rng(12)
+    handles, _ = weights(b, rng)
+    longest = 60
+    ran, replayed = (make_layer(handles, 3, longest, 64) for _ in range(2))
+    prompt = [14, 31, 1]
+    x = torch.from_numpy(rng.standard_normal((sum(prompt), HIDDEN)).astype(np.float32)).cuda()
+    assert torch.equal(ran.step(x, prompt), replayed.step(x, prompt))
+    replayed.record()
+    for i in range(20):
+        x = torch.from_numpy(rng.standard_normal((3, HIDDEN)).astype(np.float32)).cuda()
+        # (both with the same estimate of the longest request, so that they are cut alike)
+        y = torch.empty((3, HIDDEN), device="cuda")
+        first = ran._take([1, 1, 1])
+        ran._launch(x, torch.ones(3, dtype=torch.int32, device="cuda"), ran.pool[first:ran.used], y, 1, longest)
+        assert torch.equal(replayed.replay(x), y), f"replay {i}"
+        assert torch.equal(replayed.table, ran.table) and replayed.used == ran.used
+        torch.ones(1000, device="cuda").sum().item()
+        torch.cuda.synchronize()
+
+
+def test_step_refuses_what_does_not_fit(b):
+    handles, _ = weights(b, np.random.default_rng(13))
+    layer = make_layer(handles, 2, 20, 30)
+    x = torch.zeros((32, HIDDEN), device="cuda")
+    for rows, new in ((3, [3]), (3, [1, 1]), (3, [4, -1]), (21, [21, 0]), (32, [16, 16])):
+        with pytest.raises(ValueError):
+            layer.step(x[:rows], new)
+    assert layer.lengths == [0, 0] and layer.used == 0
+    assert layer.step(x[:0], [0, 0]).shape == (0, HIDDEN)
+
+
+# ---------------------------------------------------------------------------------------------- many tokens, large caches
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,dim,block,tokens", [(2, 64, 16, 2500), (5, 24, 64, 3000), (8, 128, 32, 2100)])
+def test_append_of_many_tokens(b, dtype, heads, dim, block, tokens):
+    """Runs of every length and singles in one long call, blocks in no order; then read back in groups of any alignment."""
+    rng = np.random.default_rng(tokens + heads)
+    types = {"f32": torch.float32, "bf16": torch.bfloat16}
+    slots, blk = [], 0
+    n_blocks = tokens
+    order = rng.permutation(n_blocks)
+    while len(slots) < tokens:
+        kind = rng.integers(0, 5)
+        first = 0 if kind < 2 else int(rng.integers(0, block))
+        n = block if kind == 0 else 1 if kind == 4 else int(rng.integers(1, block - first + 1))
+        slots += [int(order[blk]) * block + first + i for i in range(n)]
+        if rng.integers(0, 6) == 0:
+            slots += [-1] * int(rng.integers(1, 4))
+        blk += 1
+    slots = np.array(slots[:tokens], np.int64)
+    c = b.KvCache(n_blocks, heads, dim, block)
+    k, v = (rng.integers(-127, 128, (n_blocks, heads, block, dim)).astype(np.int8) for _ in range(2))
+    ks, vs = ((rng.random((n_blocks, heads)) * 0.05).astype(np.float32) for _ in range(2))
+    c.load_codes(dev(k), dev(v), dev(ks), dev(vs))
+    kx, vx = (torch.from_numpy(rng.standard_normal((tokens, heads, dim)).astype(np.float32)).to(types[dtype]).cuda() for _ in range(2))
+    for codes, scale, x in ((k, ks, kx), (v, vs, vx)):
+        o.append(codes, scale, x.float().cpu().numpy(), slots)
+    b.abft_kv_append(c, kx, vx, dev(slots))
+    assert np.array_equal(c.k_scale.cpu().numpy(), ks) and np.array_equal(c.v_scale.cpu().numpy(), vs)
+    known = np.ones((n_blocks, block), bool)      # what lies behind a run is nobody's
+    last = {}
+    for s in slots[slots >= 0]:
+        last[int(s) // block] = int(s) % block + 1
+    for i, end in last.items():
+        known[i, end:] = False
+    for got, want in zip(c.codes(), (k, v)):
+        got = got.cpu().numpy()
+        assert np.array_equal(got.transpose(0, 2, 1, 3)[known], want.transpose(0, 2, 1, 3)[known])
+    # whole blocks in order, the same shifted by a token, and single tokens
+    gk, gv = (x.cpu().numpy() for x in c.codes())
+    n = min(n_blocks * block, 4096)
+    for back in (np.arange(n), np.arange(n - 1) + 1, rng.integers(-1, n_blocks * block + 1, 3000)):
+        back = back.astype(np.int64)
+        kb, vb = (torch.full((len(back), heads, dim), 5.0, dtype=types[dtype], device="cuda") for _ in range(2))
+        b.abft_kv_read(c, dev(back), kb, vb)
+        for got, codes, scale in ((kb, gk, ks), (vb, gv, vs)):
+            assert torch.equal(got.cpu(), torch.from_numpy(o.read(codes, scale, back).astype(np.float32)).to(types[dtype]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_cache_of_more_than_4_gib(b, dtype):
+    """The blocks at the end of a cache whose offsets pass 32 bits: append, read and attention there, and nothing written elsewhere."""
+    rng = np.random.default_rng(3)
+    heads, dim, block = 8, 256, 128
+    n_blocks = 2 ** 32 // (heads * dim * block) + 40
+    types = {"f32": torch.float32, "bf16": torch.bfloat16}
+    c = b.KvCache(n_blocks, heads, dim, block)
+    assert c.k_codes.numel() > 2 ** 32
+    small = 6
+    base = n_blocks - small
+    T = 300     # two blocks and a part of one, from the last block down
+    ids = np.array([n_blocks - 1, n_blocks - 4, n_blocks - 2])
+    pos = np.arange(T)
+    slots = ids[pos // block].astype(np.int64) * block + pos % block
+    kx, vx, q = (torch.from_numpy(rng.standard_normal((T, heads, dim)).astype(np.float32)).to(types[dtype]).cuda() for _ in range(3))
+    k, v = (np.zeros((small, heads, block, dim), np.int8) for _ in range(2))
+    ks, vs = (np.zeros((small, heads), np.float32) for _ in range(2))
+    for codes, scale, x in ((k, ks, kx), (v, vs, vx)):
+        o.append(codes, scale, x.float().cpu().numpy(), slots - base * block)
+    b.abft_kv_append(c, kx, vx, dev(slots))
+    assert not c.k_codes[:base].any() and not c.v_codes[:base].any() and not c.k_scale[:base].any() and not c.v_scale[:base].any()
+    end = c.k_codes[base:, ..., :dim].cpu().numpy(), c.v_codes[base:, ..., :dim, :].transpose(3, 4).flatten(2, 3).cpu().numpy()
+    for i, blk in enumerate(ids - base):
+        m = min(block, T - i * block)
+        assert np.array_equal(end[0][blk, :, :m], k[blk, :, :m]) and np.array_equal(end[1][blk, :, :m], v[blk, :, :m])
+    assert np.array_equal(c.k_scale[base:].cpu().numpy(), ks) and np.array_equal(c.v_scale[base:].cpu().numpy(), vs)
+    kb, vb = (torch.empty_like(kx) for _ in range(2))
+    b.abft_kv_read(c, dev(slots), kb, vb)
+    for got, codes, scale in ((kb, k, ks), (vb, v, vs)):
+        assert torch.equal(got.cpu(), torch.from_numpy(o.read(codes, scale, slots - base * block).astype(np.float32)).to(types[dtype]))
+    table = ids[None, :].astype(np.int32)
+    for rows in (1, T):
+        cu = np.array([0, rows], np.int32)
+        out = torch.empty((rows, heads, dim), dtype=types[dtype], device="cuda")
+        b.abft_kv_attention(c, q[:rows], dev(table), dev(np.array([T], np.int32)), dev(cu), out, rows, T, workspace=b.KvWorkspace(c, 1, heads, rows, T).tensor)
+        want, tol, _, _ = o.attention(f64(q[:rows]), k, v, ks, vs, table - base, [T], cu, dim ** -0.5, dtype)
+        within(f64(out), want, tol, f"attention of {rows} rows")
+
+
+def test_calls_agree_with_and_without_their_native_marshalling(b, monkeypatch):
+    """The binding's own marshalling, which takes what the native one declines, makes the same calls."""
+    rng = np.random.default_rng(14)
+    handles, _ = weights(b, rng)
+    x = torch.from_numpy(rng.standard_normal((20, HIDDEN)).astype(np.float32)).cuda()
+    native = make_layer(handles, 2, 40, 20)
+    first = native.step(x, [3, 17])
+    read = [torch.zeros((20, HEADS, DIM), device="cuda") for _ in range(4)]
+    b.abft_kv_read(native.cache, native.slots[:20], *read[:2])
+    for name in ("w4", "plan", "append", "read", "attention"):
+        monkeypatch.setattr(b._fastcall, name, lambda *a: None)
+    plain = make_layer(handles, 2, 40, 20)
+    assert torch.equal(plain.step(x, [3, 17]), first)
+    b.abft_kv_read(plain.cache, plain.slots[:20], *read[2:])
+    assert torch.equal(read[0], read[2]) and torch.equal(read[1], read[3])
