@@ -16,6 +16,7 @@
 //    has to bring to the product with V, whose codes stand 16 tokens of a column side by side: no lane passes a score to another.
 //  * Codes go from global memory straight to registers: no other wavefront needs them (tokens are split among the wavefronts), or
 //    all read the same ones at about the same time and find them in the caches (rows are split).
+//    A workgroup's rows are made digits once and kept in LDS.
 //  * A request longer than a part (params.chunk) is cut into parts, each a workgroup; a second kernel joins them.
 //
 // Scales of a block: that of the keys multiplies the scores.  That of the values multiplies what a tile adds to the sums; where a
@@ -26,6 +27,10 @@
 // one for the sum, 2.75 to make it digits; for each sum of values two to make it a float and one multiply-add.  The sums are
 // relative to a maximum that is only moved when a row's largest score has grown by more than 2^kSlack, which spares their
 // multiplication for nearly every tile.
+//
+// Measured, bf16, 32 query heads over 8 cached ones of 128, blocks of 64: a token each for 64 requests of 4000 96 us (5.5 TB/s), of uneven
+// lengths up to 8000 98 us (4.4 TB/s: what is left of the last long ones); for one of 100 6.4 us, of 8000 12.4.  512 new tokens each for two of up to 4096 115
+// us, 330e12 operations of the definition a second (the matrix cores do twice as many: two digits).
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -54,16 +59,16 @@ struct AttnParams {
     int n_blocks, heads, q_heads, group, dim, block_shift, width, n_req;
     int groups;         // workgroups for the rows of a head and request
     int parts, chunk;   // a part is `chunk` tokens, a multiple of 256; the last takes what is left
-    int stride;
+    int stride;         // see the kernel
     float scale2;       // the scale of the scores, times log2(e)
-    bool q_wide;        // rows of Q are whole aligned pieces of 16 bytes
+    bool q_wide;        // rows of Q are whole aligned pieces of four columns
 };
 
 // which kernel (one for each of them and each type, number of columns and kind of block)
 enum AttnShape {
-    kAttnTokens1,   // 16 rows, tokens split among the wavefronts
-    kAttnTokens2,   // 32, where a wavefront holds that many
-    kAttnRows       // rows split among the wavefronts
+    kAttnTokens,    // 16 rows, tokens split among four wavefronts
+    kAttnTokens8,   // among eight (up to 128 columns)
+    kAttnRows       // rows split among four wavefronts
 };
 // Most rows of a wavefront, in sixteens.  More do not fit its registers, and a kernel that spills is not to be had: the compiler has put
 // the copy of a spilled register before the end of a divergent branch, where not every lane made it.
@@ -149,29 +154,33 @@ __device__ inline float meet(const v4i (&acc)[ND], int i) {
     else return __builtin_fmaf((float)acc[2][i], 65536.0f, low);
 }
 
-template <typename T, int COLS, int RT, bool SMALL, bool BY_ROWS>
-__global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), COLS, RT)) void kv_attention_kernel(const AttnParams p) {
+// NW wavefronts
+template <typename T, int COLS, int RT, bool SMALL, bool BY_ROWS, int NW>
+__global__ __launch_bounds__(64 * NW, NW > 4 ? NW / 4 : attn_waves(attn_digits(sizeof(T)), COLS, RT)) void kv_attention_kernel(const AttnParams p) {
     constexpr int ND = attn_digits(sizeof(T));
     constexpr int KC = COLS / 64, VT = COLS / 16;
-    constexpr int kRows = RT * 16 * (BY_ROWS ? 4 : 1);         // rows of a workgroup
-    constexpr int kStep = kAttnTile * (BY_ROWS ? 1 : 4);       // tokens that it takes at a time
+    constexpr int kRows = RT * 16 * (BY_ROWS ? NW : 1);         // rows of a workgroup
+    constexpr int kStep = kAttnTile * (BY_ROWS ? 1 : NW);       // tokens that it takes at a time
     constexpr int kPitch = COLS + 4;
+    // positions of scores worked out only for tiles that are masked (not where the order that this gives the rest would spill registers)
+    constexpr bool kMasksApart = BY_ROWS || COLS != 128 || ND == 3 || NW > 4;
     __shared__ v4i s_q[kRows / 16][KC][ND][64];                // digits of the rows, as the lanes of a product take them
     __shared__ float s_q_scale[kRows];
     __shared__ int s_token[kRows], s_head[kRows], s_limit[kRows];   // of a row: new token (-1: no such row), query head, last position it sees
-    __shared__ float s_o[BY_ROWS ? 1 : 4 * 16 * kPitch];
-    __shared__ float s_m[4][16], s_l[4][16];
+    __shared__ float s_o[BY_ROWS ? 1 : NW * 16 * kPitch];
+    __shared__ float s_m[NW][16], s_l[NW][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15, lq = lane >> 4;
-    // Which part and group of rows (`late`: the last ones, of which only long requests have any and which see most, come first) of which
-    // head of which request.  Neighbouring workgroups run in different eighths of the chip, and those 256 apart on one compute unit.
-    // Rows split: what a head and request has stands together, since it reads the same codes.  Tokens split: every head and request of one
-    // part ahead of the next part's, and from part to part they move on by p.stride, so that neither an eighth nor a compute unit has
-    // much of one long request (64 requests of uneven lengths up to 8000 in four parts: 97 us, 127 with the parts of a request next
-    // to each other, where an eighth had the first parts of all).
+    // Which part and group of rows of which head of which request.  Neighbouring workgroups run in different eighths of the chip, and those 256
+    // apart on one compute unit.  Every head and request has its last part and rows, of which only long requests have any and which
+    // see most, ahead of any one's next; from turn to turn they move on by p.stride, and from 256 workgroups to the next by half of
+    // all, so that neither an eighth nor a compute unit has much of one long request (64 requests of uneven lengths up to 8000 in four
+    // parts: 97 us, 127 with the parts of a request next to each other, where an eighth had the first parts of all; prompts of 2000,
+    // 32 heads of 128: 110, 172 with the rows of a head together; 512 new of up to 4096 for two requests: 115, 154 without the half).
     const uint32_t many = (uint32_t)(p.groups * p.parts), pairs = (uint32_t)(p.heads * p.n_req);
-    const uint32_t turn = BY_ROWS ? blockIdx.x % many : blockIdx.x / pairs, late = many - 1 - turn;
+    const uint32_t turn = blockIdx.x / pairs, late = many - 1 - turn;
+    const uint64_t moved = turn * (uint64_t)p.stride + turn * (uint64_t)pairs / 256 * (pairs / 2);
     const int part = (int)(late / (uint32_t)p.groups), first_group = (int)(late % (uint32_t)p.groups), groups = p.groups;
-    const int pair = (int)(BY_ROWS ? blockIdx.x / many : (blockIdx.x % pairs + turn * (uint64_t)p.stride) % pairs), req = pair / p.heads, head = pair - req * p.heads;
+    const int pair = (int)((blockIdx.x % pairs + moved) % pairs), req = pair / p.heads, head = pair - req * p.heads;
     const int block_tokens = 1 << p.block_shift;
 
     const int64_t room = (int64_t)p.width << p.block_shift;
@@ -210,14 +219,14 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), COLS, RT)) 
             return x;
         };
         auto exists = [&](int id) __attribute__((always_inline)) { return (uint32_t)id < (uint32_t)p.n_blocks; };
-        const int64_t block_bytes = (int64_t)COLS << p.block_shift;   // of one head
+        const uint32_t block_bytes = (uint32_t)COLS << p.block_shift;   // of one head (there are fewer than 2^31 heads of blocks)
         const int k_lane = (SMALL ? (lr & 3) : 16 * (lr >> 2) + (lr & 3)) * COLS + 16 * lq;
         const int v_lane = (SMALL ? 0 : lq * COLS * kKvGroup) + lr * 16;
         v4i kf[4][KC];
         auto load_k = [&](int id, int t) __attribute__((always_inline)) {
-            const int64_t b = exists(id) ? id : 0;
+            const uint32_t block_head = (uint32_t)(exists(id) ? id : 0) * (uint32_t)p.heads + (uint32_t)head;
             const int off = (SMALL ? t + 16 * (lr >> 2) : t) & (block_tokens - 1);
-            const int8_t* const at = p.k_codes + (b * p.heads + head) * block_bytes + off * COLS;
+            const int8_t* const at = p.k_codes + (uint64_t)block_head * block_bytes + (uint32_t)(off * COLS);
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -226,9 +235,9 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), COLS, RT)) 
         v4i vf[VT];
         float ks = 0.0f, vs = 0.0f;   // (of block 0 where there is none: nothing is seen of it)
         auto load_v = [&](int id, int t) __attribute__((always_inline)) {
-            const int64_t block_head = (int64_t)(exists(id) ? id : 0) * p.heads + head;
+            const uint32_t block_head = (uint32_t)(exists(id) ? id : 0) * (uint32_t)p.heads + (uint32_t)head;
             const int off = (SMALL ? t + 16 * lq : t) & (block_tokens - 1);
-            const int8_t* const at = p.v_codes + block_head * block_bytes + off * COLS;
+            const int8_t* const at = p.v_codes + (uint64_t)block_head * block_bytes + (uint32_t)(off * COLS);
 #pragma unroll
             for (int v = 0; v < VT; ++v) vf[v] = *reinterpret_cast<const v4i*>(at + v_lane + v * 256);
             ks = p.k_scale[block_head];
@@ -240,36 +249,37 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), COLS, RT)) 
             now = blocks_of(t0);
             load_k(now.k, t0);
         }
-        // ---- the rows, once for the workgroup: sixteen threads a row, sixteen columns a thread
+        // ---- the rows, once for the workgroup: sixteen threads a row
+        constexpr int kOwn = COLS / 16;   // columns of a thread
         __syncthreads();
 #pragma unroll 1
         for (int tile = 0; tile < kRows / 16; ++tile) {
-            const int tid = here_only(threadIdx.x), row16 = tid >> 4, at = tile * 16 + row16, pc = tid & 15, d = 16 * pc;
+            if (NW > 4 && threadIdx.x >= 256) break;
+            const int tid = here_only(threadIdx.x), row16 = tid >> 4, at = tile * 16 + row16, pc = tid & 15, d = kOwn * pc;
             const int64_t row = row0 + at;
             const bool real = row < rows;
             const int i = real ? (int)((uint32_t)row / (uint32_t)p.group) : 0, qh = head * p.group + (real ? (int)row - i * p.group : 0);
             const T* const q = static_cast<const T*>(p.Q) + (c0 + i) * p.q_token + qh * p.q_head;
             // (every thread loads, from columns that exist, whatever its own are)
-            float x[16];
+            float x[kOwn];
             if (p.q_wide) {
-                constexpr int PER = 16 / sizeof(T);
-                typedef T piece __attribute__((ext_vector_type(PER)));
+                typedef T piece __attribute__((ext_vector_type(4)));
 #pragma unroll
-                for (int k = 0; k < 16 / PER; ++k) {
-                    const piece v = *reinterpret_cast<const piece*>(q + min(d + PER * k, p.dim - PER));
+                for (int k = 0; k < kOwn; k += 4) {
+                    const piece v = *reinterpret_cast<const piece*>(q + min(d + k, p.dim - 4));
 #pragma unroll
-                    for (int j = 0; j < PER; ++j) x[PER * k + j] = d + PER * k < p.dim ? to_f32((T)v[j]) : 0.0f;
+                    for (int j = 0; j < 4; ++j) x[k + j] = d + k < p.dim ? to_f32((T)v[j]) : 0.0f;
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
+                for (int j = 0; j < kOwn; ++j) {
                     const float v = to_f32(q[min(d + j, p.dim - 1)]);
                     x[j] = d + j < p.dim ? v : 0.0f;
                 }
             }
             float most = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
+            for (int j = 0; j < kOwn; ++j) {
                 const float a = fabsf(x[j]);
                 most = a < INFINITY ? fmaxf(most, a) : INFINITY;   // (an infinity or a NaN makes the row's scores NaN)
                 x[j] = a < INFINITY ? x[j] : 0.0f;
@@ -278,17 +288,14 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), COLS, RT)) 
             for (int m = 1; m < 16; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
             constexpr float one = Fixed<ND, true>::kOne;
             const float inv = most >= 0x1p-100f && most < INFINITY ? __builtin_copysignf(one / most, p.scale2) : 0.0f;   // (a score's factor is not negative)
-            v4i digits[ND];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
+            for (int k = 0; k < kOwn; k += 4) {
                 uint32_t digit[ND];
-                four_digits<ND, true>(x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3], inv, digit);
+                four_digits<ND, true>(x[k], x[k + 1], x[k + 2], x[k + 3], inv, digit);
+                const int at_d = d + k;
 #pragma unroll
-                for (int t = 0; t < ND; ++t) digits[t][w] = (int)digit[t];
+                for (int t = 0; t < ND; ++t) reinterpret_cast<uint32_t*>(&s_q[tile][at_d / 64][t][at_d % 64 / 16 * 16 + row16])[at_d % 16 / 4] = digit[t];
             }
-            if (d < COLS)
-#pragma unroll
-                for (int t = 0; t < ND; ++t) s_q[tile][pc / 4][t][pc % 4 * 16 + row16] = digits[t];
             if (pc == 0) {
                 s_q_scale[at] = most < INFINITY ? most / one * fabsf(p.scale2) : NAN;
                 s_token[at] = real ? (int)(c0 + i) : -1;
@@ -350,8 +357,14 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), COLS, RT)) 
                 }
                 float f = q_scale[rt] * ks;   // makes a score of a sum, base 2
                 if (!__all(here && t0 + kAttnTile - 1 <= limit[rt])) {
+                    if constexpr (kMasksApart) {
+                        const int first = here_only(t0 + 16 * lq);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) z[j] = here && t0 + 16 * lq + j <= limit[rt] ? z[j] * f : -INFINITY;
+                        for (int j = 0; j < 16; ++j) z[j] = here && first + j <= limit[rt] ? z[j] * f : -INFINITY;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) z[j] = here && t0 + 16 * lq + j <= limit[rt] ? z[j] * f : -INFINITY;
+                    }
                     f = 1.0f;
                 }
                 float mine_most = z[0];
@@ -429,7 +442,7 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), COLS, RT)) 
                 const int token = s_token[wave_rows + rt * 16 + lr], qh = s_head[wave_rows + rt * 16 + lr];
                 const int64_t at = (int64_t)token * p.q_heads + qh;
                 if (token < 0) continue;
-                if (p.parts > 1) {
+                if (mine > 1) {
                     float* const po = p.part_o + ((int64_t)part * all_rows + at) * COLS;
 #pragma unroll
                     for (int v = 0; v < VT; ++v) *reinterpret_cast<attn_v4f*>(po + 16 * v + 4 * lq) = o[rt][v];
@@ -459,22 +472,22 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), COLS, RT)) 
                 for (int v = 0; v < VT; ++v) *reinterpret_cast<attn_v4f*>(&s_o[(wave * 16 + lr) * kPitch + 16 * v + 4 * lq]) = o[rt][v];
                 __syncthreads();
 #pragma unroll 1
-                for (int e = here_only(threadIdx.x); e < 16 * COLS; e += 256) {
+                for (int e = here_only(threadIdx.x); e < 16 * COLS; e += 64 * NW) {
                     const int r = e / COLS, d = e % COLS, token = s_token[rt * 16 + r], qh = s_head[rt * 16 + r];
                     if (token < 0) break;   // (rows that exist come first)
                     float m = s_m[0][r];
 #pragma unroll
-                    for (int w = 1; w < 4; ++w) m = fmaxf(m, s_m[w][r]);
+                    for (int w = 1; w < NW; ++w) m = fmaxf(m, s_m[w][r]);
                     const float ref = m == -INFINITY ? 0.0f : m;
                     float l = 0.0f, x = 0.0f;
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
+                    for (int w = 0; w < NW; ++w) {
                         const float f = __builtin_amdgcn_exp2f(s_m[w][r] - ref);
                         l = __builtin_fmaf(s_l[w][r], f, l);
                         x = __builtin_fmaf(s_o[(w * 16 + r) * kPitch + d], f, x);
                     }
                     const int64_t at = (int64_t)token * p.q_heads + qh;
-                    if (p.parts > 1) {
+                    if (mine > 1) {
                         p.part_o[((int64_t)part * all_rows + at) * COLS + d] = x;
                         if (d == 0) {
                             float* const ml = p.part_ml + ((int64_t)part * all_rows + at) * 2;
@@ -492,76 +505,85 @@ __global__ __launch_bounds__(256, attn_waves(attn_digits(sizeof(T)), COLS, RT)) 
     if (p.req_flags && __any(bad_block) && lane == 0) atomicOr(p.req_flags + req, ABFT_KV_BAD_BLOCK);
 }
 
-// Joins the parts of a request's rows: NW wavefronts a row, which take parts in turn, lanes own columns.
-template <typename T, int COLS, int NW>
+// Joins the parts of the rows of requests that have several.  Lanes own four columns, and as many of them as a row needs make a team;
+// SHARE: the four wavefronts of a workgroup share a row's parts.
+template <typename T, int COLS, bool SHARE>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(const AttnParams p) {
-    constexpr int PER = COLS / 64, kRows = 4 / NW;
-    __shared__ float s_x[NW > 1 ? NW : 1][NW > 1 ? COLS : 1], s_l[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine_first = wave % NW, req = blockIdx.y;
+    constexpr int kTeam = SHARE || COLS > 128 ? 64 : COLS / 4;         // lanes of a team
+    constexpr int kRows = SHARE ? 1 : 256 / kTeam;                     // rows that a workgroup takes at a time
+    constexpr int kSplit = SHARE ? 4 * (COLS > 128 ? 1 : 64 / (COLS / 4)) : 1;   // teams that share a row's parts
+    constexpr int kLanes = SHARE ? 256 / kSplit : kTeam;               // lanes that hold a row's columns
+    __shared__ attn_v4f s_x[SHARE ? kSplit : 1][SHARE ? COLS / 4 : 1];
+    __shared__ float s_l[kSplit];
+    const int t = threadIdx.x % kLanes, turn = SHARE ? threadIdx.x / kLanes : 0, req = blockIdx.y;
     const int64_t room = (int64_t)p.width << p.block_shift;
     const int len = (int)min((int64_t)max(p.seq_len[req], 0), room);
     const int64_t c0 = min((int64_t)max(p.cu_new[req], 0), p.n_rows), c1 = min(max((int64_t)p.cu_new[req + 1], c0), p.n_rows);
     const int parts = len <= 0 ? 1 : min(p.parts, (len + p.chunk - 1) / p.chunk);
+    if (parts <= 1) return;
     const int64_t all_rows = p.n_rows * p.q_heads;
-    // (with several wavefronts a row, all of a workgroup are at the same row)
-    for (int64_t r = c0 * p.q_heads + (int64_t)blockIdx.x * kRows + wave / NW; r < c1 * p.q_heads; r += (int64_t)gridDim.x * kRows) {
+    // (with a row shared, all of a workgroup are at the same one)
+    for (int64_t r = c0 * p.q_heads + (int64_t)blockIdx.x * kRows + (SHARE ? 0 : threadIdx.x / kTeam); r < c1 * p.q_heads; r += (int64_t)gridDim.x * kRows) {
         float m = -INFINITY;
-        for (int s = lane; s < parts; s += 64) m = fmaxf(m, p.part_ml[(s * all_rows + r) * 2]);
+        for (int s = threadIdx.x % kTeam; s < parts; s += kTeam) m = fmaxf(m, p.part_ml[(s * all_rows + r) * 2]);
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+        for (int d = 1; d < kTeam; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
         const float ref = m == -INFINITY ? 0.0f : m;
-        float l = 0.0f, x[PER];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) x[i] = 0.0f;
+        float l = 0.0f;
+        attn_v4f x = {0, 0, 0, 0};
 #pragma unroll 4
-        for (int s = mine_first; s < parts; s += NW) {
+        for (int s = turn; s < parts; s += kSplit) {
             const float* const ml = p.part_ml + (s * all_rows + r) * 2;
-            const float* const po = p.part_o + (s * all_rows + r) * COLS + lane * PER;
+            const attn_v4f v = *reinterpret_cast<const attn_v4f*>(p.part_o + (s * all_rows + r) * COLS + 4 * min(t, COLS / 4 - 1));
             const float f = __builtin_amdgcn_exp2f(ml[0] - ref);
             l = __builtin_fmaf(ml[1], f, l);
 #pragma unroll
-            for (int i = 0; i < PER; ++i) x[i] = __builtin_fmaf(po[i], f, x[i]);
+            for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(v[i], f, x[i]);
         }
-        if constexpr (NW > 1) {
+        if constexpr (SHARE) {
             __syncthreads();
-#pragma unroll
-            for (int i = 0; i < PER; ++i) s_x[wave][lane * PER + i] = x[i];
-            if (lane == 0) s_l[wave] = l;
+            if (4 * t < COLS) s_x[turn][t] = x;
+            if (t == 0) s_l[turn] = l;
             __syncthreads();
-            if (wave > 0) continue;
+            if (turn > 0 || 4 * t >= COLS) continue;
 #pragma unroll
-            for (int w = 1; w < NW; ++w) {
+            for (int w = 1; w < kSplit; ++w) {
                 l += s_l[w];
+                const attn_v4f y = s_x[w][t];
 #pragma unroll
-                for (int i = 0; i < PER; ++i) x[i] += s_x[w][lane * PER + i];
+                for (int i = 0; i < 4; ++i) x[i] += y[i];
             }
         }
         const int64_t token = r / p.q_heads;
         const int qh = (int)(r - token * p.q_heads);
         T* const out = static_cast<T*>(p.O) + token * p.o_token + qh * p.o_head;
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (lane * PER + i < p.dim) out[lane * PER + i] = from_f32<T>(l == 0.0f ? 0.0f : x[i] / l);
-        if (p.lse && lane == 0) p.lse[r] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718f;
+        for (int i = 0; i < 4; ++i)
+            if (4 * t + i < p.dim) out[4 * t + i] = from_f32<T>(l == 0.0f ? 0.0f : x[i] / l);
+        if (p.lse && t == 0) p.lse[r] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718f;
     }
 }
 
 template <typename T, int COLS, bool SMALL>
 hipError_t launch_attention_block(AttnShape shape, const AttnParams& p, unsigned grid, hipStream_t s) {
     constexpr int kMost = attn_rows_tiles(COLS);
-    if (shape == kAttnRows) kv_attention_kernel<T, COLS, kMost, SMALL, true><<<dim3(grid), dim3(256), 0, s>>>(p);
-    else if (shape == kAttnTokens2) kv_attention_kernel<T, COLS, kMost, SMALL, false><<<dim3(grid), dim3(256), 0, s>>>(p);
-    else kv_attention_kernel<T, COLS, 1, SMALL, false><<<dim3(grid), dim3(256), 0, s>>>(p);
+    if (shape == kAttnRows) kv_attention_kernel<T, COLS, kMost, SMALL, true, 4><<<dim3(grid), dim3(256), 0, s>>>(p);
+    else if (shape == kAttnTokens8) kv_attention_kernel<T, COLS, 1, SMALL, false, COLS <= 128 ? 8 : 4><<<dim3(grid), dim3(COLS <= 128 ? 512 : 256), 0, s>>>(p);
+    else kv_attention_kernel<T, COLS, 1, SMALL, false, 4><<<dim3(grid), dim3(256), 0, s>>>(p);
     return hipGetLastError();
 }
 template <typename T, int COLS>
 hipError_t launch_attention_cols(AttnShape shape, bool small_blocks, const AttnParams& p, unsigned grid, hipStream_t s) {
     const hipError_t e = small_blocks ? launch_attention_block<T, COLS, true>(shape, p, grid, s) : launch_attention_block<T, COLS, false>(shape, p, grid, s);
     if (e != hipSuccess || p.parts <= 1) return e;
-    // many parts, few rows: the wavefronts of a workgroup share a row's
     const int64_t rows = (p.n_rows + p.n_req - 1) / p.n_req * p.q_heads;
-    if (p.parts > 8) kv_attention_join_kernel<T, COLS, 4><<<dim3((unsigned)(rows < 4096 ? rows : 4096), (unsigned)p.n_req), dim3(256), 0, s>>>(p);
-    else kv_attention_join_kernel<T, COLS, 1><<<dim3((unsigned)((rows + 3) / 4 < 1024 ? (rows + 3) / 4 : 1024), (unsigned)p.n_req), dim3(256), 0, s>>>(p);
+    if (p.parts > 8 || (p.parts > 2 && rows * p.n_req <= 2048)) {   // many parts, few rows: the wavefronts of a workgroup share a row's
+        kv_attention_join_kernel<T, COLS, true><<<dim3((unsigned)(rows < 4096 ? rows : 4096), (unsigned)p.n_req), dim3(256), 0, s>>>(p);
+    } else {
+        constexpr int kTake = COLS <= 64 ? 16 : COLS <= 128 ? 8 : 4;
+        const int64_t need = (rows + kTake - 1) / kTake;
+        kv_attention_join_kernel<T, COLS, false><<<dim3((unsigned)(need < 4096 ? need : 4096), (unsigned)p.n_req), dim3(256), 0, s>>>(p);
+    }
     return hipGetLastError();
 }
 template <typename T>

@@ -6,7 +6,24 @@
 namespace abft {
 namespace {
 
-// How a call is cut, by what the host knows of it.
+// How a call is cut, by what the host knows of it.  Rows of a request and cached head: new tokens times the query heads that share the
+// head.  All figures in us; heads "32 / 8" are 32 query heads over 8 cached ones, lengths ragged unless said otherwise.
+//
+// Which kernel.  Tokens split among the wavefronts, 16 rows to a workgroup: work of many small pieces, evenly dealt.  Rows split,
+// 64 (or 128) to a workgroup: less joining, fewer rows worked out twice; that wins where there are so many workgroups that pieces need not
+// be small, and loses where there are not (tokens / rows split; workgroups of the latter: 32 + 32 heads of 128, prompts of 2000,
+// 2048: 146 / 110; 16 + 16 of 64, 8 of 1024, 1024: 94 / 67; 32 / 8 of 128, 512 new of 4096, 512: 124 / 115; 40 / 8, 300 new of 6000,
+// 576: 176 / 326; 32 / 8, 150 new of 600, 480: 34 / 42; 12 + 12 of 64, 512 new of 4500, 192: 58 / 130, in 5 parts 66; 16 / 4, 64 new of
+// 2000, 128: 25 / 58, in 4 parts 37).
+// Eight wavefronts for a workgroup instead of four where that spares the cut and the join: a tile for each, or as many workgroups as fit at once
+// (eight / four, 32 / 8 of 128, single tokens: 1 request of 500 8.5 / 10.6, of 1000 11.1 / 10.7, of 200 7.2 / 7.1; 8 up to 1500
+// 14.5 / 12.7; 32 up to 1000 12.7 / 15.9, up to 2000 19.4 / 22.5, up to 3000 25.5 / 27.1).
+//
+// Parts, where tokens are split: enough for 512 workgroups, of no fewer tokens than a pass of the four wavefronts, or two if it is long (parts:
+// 1 / 4 / 16 / 64; 32 / 8 of 128, one of 8000 55.6 / 22.2 / 13.3 / 12.3; 8 up to 2000 18.9 / 13.7 / 13.3 / 13.4; 16 up to 30000,
+// 64 workgroups 237 / 77 / 63 / 61; 4 up to 200000, 32 workgroups 1465 / 411 / 196 / 187; 32 of up to 2000 19.4 / 28.5 / 37 / 37).
+// And of no more than 2048 tokens while that makes no more than 2048 workgroups, so that a long request does not run on alone (64 up
+// to 8000: 108 / 96 / 100 / 113; all of 4000: 96 / 106 / 121 / 121).
 struct AttnCut {
     AttnShape shape;
     int groups;   // workgroups for the rows of a request and head
@@ -14,27 +31,25 @@ struct AttnCut {
 };
 AttnCut cut(int cols, int n_req, int heads, int group, int max_new, int max_len) {
     AttnCut c;
-    const int64_t rows = (int64_t)max_new * group;
-    const int most = attn_rows_tiles(cols);
-    c.shape = rows <= 16 ? kAttnTokens1 : rows <= 32 ? (most > 1 ? kAttnTokens2 : kAttnTokens1) : kAttnRows;
-    const int64_t per = c.shape == kAttnTokens1 ? 16 : c.shape == kAttnTokens2 ? 32 : 64 * most;
-    const int64_t groups = (rows + per - 1) / per;
-    c.groups = (int)(groups < 1 ? 1 : groups > 4096 ? 4096 : groups);   // (they take rows in turn)
-    const int64_t whole = (int64_t)n_req * heads * c.groups;
+    const int64_t rows = (int64_t)max_new * group, pairs = (int64_t)n_req * heads, by_rows = 64 * attn_rows_tiles(cols);
+    c.shape = pairs * ((rows + by_rows - 1) / by_rows) >= 1000 && rows > 16 ? kAttnRows : kAttnTokens;
+    const int64_t per = c.shape == kAttnRows ? by_rows : 16, groups = (rows + per - 1) / per;
+    c.groups = (int)(groups > 4096 ? 4096 : groups);   // (they take rows in turn)
+    const int64_t whole = pairs * c.groups;
     int64_t parts = 1;
-    auto limited = [](int64_t x, int64_t most) { return x < most ? x : most; };
-    if (c.shape == kAttnRows) {
-        if (whole < 400) parts = limited(1024 / whole, (max_len + 511) / 512);
-    } else {
-        const int64_t least = max_len > 16384 ? 512 : 256;
-        const int64_t fill = limited((512 + whole / 2) / whole, (max_len + least - 1) / least), even = limited(2048 / whole, max_len / 2048);
-        parts = fill > even ? fill : even;
+    if (c.shape == kAttnTokens) {
+        auto limited = [](int64_t x, int64_t most) { return x < most ? x : most; };
+        if (cols <= 128 && max_len > 256 && (max_len <= 512 || (whole > 128 && whole <= 256 && max_len <= 4096))) {
+            c.shape = kAttnTokens8;
+        } else {
+            const int64_t least = max_len > 16384 ? 512 : 256;
+            const int64_t fill = limited((512 + whole / 2) / whole, (max_len + least - 1) / least), even = limited(2048 / whole, max_len / 2048);
+            parts = fill > even ? fill : even;
+            if (parts < 1) parts = 1;
+        }
     }
-    if (parts < 1) parts = 1;
     c.chunk = (int)((((int64_t)max_len + parts - 1) / parts + 255) / 256 * 256);
-    if (c.chunk < 256) c.chunk = 256;
     c.parts = (int)(((int64_t)max_len + c.chunk - 1) / c.chunk);
-    if (c.parts < 1) c.parts = 1;
     return c;
 }
 size_t part_bytes(int64_t rows, int cols) { return (size_t)rows * ((size_t)cols + 2) * sizeof(float); }
@@ -119,10 +134,10 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
     p.n_req = n_req;
     p.groups = c.groups;
     p.parts = c.parts;
-    p.stride = (int)(pairs * 382 / 1000 / 8 * 8 + 1);   // (far, by no simple fraction, and on to the next eighth)
+    p.stride = (int)(pairs * 382 / 1000 / 8 * 8 + 1);   // (far, by no simple fraction, and on to the next eighth of the chip)
     p.chunk = c.chunk;
     p.scale2 = scale * 1.44269504f;
-    p.q_wide = ((reinterpret_cast<uintptr_t>(Q) | (uintptr_t)(q_token_stride * (int64_t)es) | (uintptr_t)(q_head_stride * (int64_t)es) | (uintptr_t)(cache->head_dim * (int64_t)es)) & 15) == 0;
+    p.q_wide = ((reinterpret_cast<uintptr_t>(Q) | (uintptr_t)(q_token_stride * (int64_t)es) | (uintptr_t)(q_head_stride * (int64_t)es) | (uintptr_t)(cache->head_dim * (int64_t)es)) & (4 * es - 1)) == 0;
     hipStream_t s = (hipStream_t)stream;
     hipError_t e = hipSuccess;
     if (req_flags) {
