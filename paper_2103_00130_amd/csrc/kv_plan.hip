@@ -5,7 +5,7 @@
 // lengths itself (8 bytes a request, which the caches hold), so each workgroup makes both sums of all requests in LDS and writes its
 // share of the outputs.  Nothing is read that another workgroup writes: entries of the table are read below a request's blocks and
 // written from there on, and rows in new blocks are numbered from free_blocks.  Bound by latency: two dependent loads, two scans,
-// the bisections.
+// the bisections (64 requests of a token each 4.2 us, 3.4 for one request; 2000 of up to 1000 tokens 9.5).
 #include <hip/hip_runtime.h>
 
 #include "../../include/abft_eb.h"
@@ -195,12 +195,18 @@ extern "C" int abft_kv_plan(const int32_t* ctx_len, const int32_t* new_len, int 
     abft::PlanParams p{ctx_len, new_len, free_blocks, table, seq_len, cu_new, slots, req_flags, taken, ldt, n_slots, ~0ull / (uint64_t)block_tokens + 1, n_req, block_tokens, -1, width, n_free};
     for (int k = 0; k < 31; ++k)
         if (block_tokens == 1 << k) p.shift = k;
-    const int nt = n_req <= 256 ? 256 : 1024;
+    // As few threads to a workgroup as have the requests in four steps, or in one, while a thread has no more than a row then (us, workgroups
+    // of 256 / 512 / 1024: 64 requests of a token 4.2 / 4.5 / 5.3, 250 of them 4.5 / 4.8 / 5.5, 300 5.4 / 5.0 / 5.6, 1000 6.5 / 5.6 /
+    // 6.2, 2000 8.8 / 6.9 / 7.1; 2000 of up to 1000 tokens in blocks of 16 512 10.2, 1024 9.5).
+    const bool middle = n_req > 256 && n_req <= 2048 && n_slots <= 256 * 512;
+    const int nt = n_req <= 256 ? 256 : middle ? 512 : 1024;
     const int64_t groups = (n_slots + nt - 1) / nt;
     const dim3 grid((unsigned)(groups < 1 ? 1 : groups > 256 ? 256 : groups));
     hipStream_t s = (hipStream_t)stream;
     if (n_req <= 256) {
         abft::kv_plan_kernel<256, 1><<<grid, dim3(256), (size_t)n_req * 12, s>>>(p);
+    } else if (middle) {
+        abft::kv_plan_kernel<512, 4><<<grid, dim3(512), (size_t)n_req * 12, s>>>(p);
     } else if (n_req <= 4096) {
         abft::kv_plan_kernel<1024, 4><<<grid, dim3(1024), (size_t)n_req * 12, s>>>(p);
     } else {

@@ -20,25 +20,6 @@ __device__ inline float to_f32(bf16 x) { return (float)x; }
 // rounded to nearest even
 template <typename T>
 __device__ inline T from_f32(float x) { return (T)x; }
-
-// N values from an address of any alignment that the type allows; `wide`: 16-byte aligned
-template <typename T, int N>
-__device__ inline void load_values(float (&out)[N], const T* p, bool wide) {
-    constexpr int PER = 16 / sizeof(T);
-    static_assert(N % PER == 0, "whole pieces of 16 bytes");
-    if (wide) {
-#pragma unroll
-        for (int i = 0; i < N / PER; ++i) {
-            typedef T piece __attribute__((ext_vector_type(PER)));
-            const piece v = reinterpret_cast<const piece*>(p)[i];
-#pragma unroll
-            for (int j = 0; j < PER; ++j) out[PER * i + j] = to_f32((T)v[j]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) out[i] = to_f32(p[i]);
-    }
-}
 #endif
 
 }  // namespace abft

@@ -159,6 +159,13 @@ def test_plan(b, R, longest, new, block, width, short, slots_short):
     assert got[5] == taken
 
 
+@pytest.mark.parametrize("R", [2047, 2048, 2049, 4096, 4097])
+def test_plan_where_the_workgroups_change(b, R):
+    test_plan(b, R, 70, 20, 16, 6, 50, 30)
+    if R <= 2048:
+        test_plan(b, R, 70, 150, 16, 14, 50, 0)    # (more rows than a workgroup of 512 on every compute unit has threads)
+
+
 def test_plan_of_nothing_and_of_lengths_past_32_bits(b):
     empty = torch.empty(0, dtype=torch.int32, device="cuda")
     cu, taken = torch.full((1,), 5, dtype=torch.int32, device="cuda"), torch.full((1,), 5, dtype=torch.int32, device="cuda")
