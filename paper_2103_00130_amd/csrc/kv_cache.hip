@@ -3,9 +3,9 @@
 //
 // A block and head has one scale, so a run of tokens of one block is one wavefront's for each head, and for keys and values: it takes the
 // largest value of the run, settles the scale, brings the codes that the block held before to it if it grew, and writes the
-// run's.  A workgroup looks for runs among some tokens and deals two heads of each to its four wavefronts.  Long runs: a lane has 16
-// tokens of 8 columns, 16 loads of 16 bytes under way at once, kept in registers from their one read to their codes; what it writes
-// are 8 bytes of 16 rows of keys, or 128 bytes of values as they stand.  Few tokens: a lane has 8 columns of one.  Bound by
+// run's.  A workgroup looks for runs among some tokens and deals two heads of each to its four wavefronts.  Long runs: a lane has 16, 8 or
+// 4 tokens of 8 columns, as many loads under way at once, kept in registers from their one read to their codes; what it writes
+// are 8 bytes of a row of keys each, or 16, 8 or 4 bytes of values as they stand.  Few tokens: a lane has 8 columns of one.  Bound by
 // memory for prompts (6000 tokens, 8 heads of 128, bf16, rows of a fused projection: 11.3 us, 3.3 TB/s; workgroups of two wavefronts for
 // each run and head, whose threads had no more than a token's columns, 38), by two dependent trips to it (slots, then values and scale) for single tokens
 // (64 of them: 4.3 us).
@@ -143,13 +143,12 @@ __device__ inline Settled settle(float peak, float old, int first) {
     return r;
 }
 
-// Codes of a run's 16 tokens of 8 columns (those of the group that are the run's), to where they stand.
-template <typename T, bool VALUES, bool FINITE>
-__device__ inline void store_unit(const CacheParams& p, const Eight<T> (&v)[kKvGroup], int8_t* codes, int o, int d, int first, int n, const Settled& r) {
-    const bool whole = o >= first && o + kKvGroup <= first + n;
+// Codes of U tokens of 8 columns (those that are the run's), to where they stand.
+template <typename T, bool VALUES, bool FINITE, int U>
+__device__ inline void store_unit(const CacheParams& p, const Eight<T> (&v)[U], int8_t* codes, int o, int d, int first, int n, const Settled& r) {
     if constexpr (!VALUES) {
 #pragma unroll
-        for (int j = 0; j < kKvGroup; ++j) {
+        for (int j = 0; j < U; ++j) {
             uint32_t c[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) c[k] = code_of<FINITE>(value_of(v[j], k), r.inv);
@@ -157,40 +156,48 @@ __device__ inline void store_unit(const CacheParams& p, const Eight<T> (&v)[kKvG
                 *reinterpret_cast<v2u*>(codes + (o + j) * p.cols + d) = v2u{low_bytes(c[0], c[1], c[2], c[3]), low_bytes(c[4], c[5], c[6], c[7])};
         }
     } else {
-        v4u* const group = reinterpret_cast<v4u*>(codes + ((int64_t)o / kKvGroup * p.cols + d) * kKvGroup);
-        v4u mask = {0, 0, 0, 0};
+        typedef uint32_t words __attribute__((ext_vector_type(U / 4)));
+        const bool whole = o >= first && o + U <= first + n;
+        int8_t* const at = codes + ((int64_t)o / kKvGroup * p.cols + d) * kKvGroup + o % kKvGroup;
+        words mask;
 #pragma unroll
-        for (int j = 0; j < kKvGroup; ++j) mask[j / 4] |= o + j >= first && o + j < first + n ? 255u << (8 * (j % 4)) : 0u;
+        for (int q = 0; q < U / 4; ++q) {
+            mask[q] = 0;
+#pragma unroll
+            for (int j = 4 * q; j < 4 * q + 4; ++j) mask[q] |= o + j >= first && o + j < first + n ? 255u << (8 * (j % 4)) : 0u;
+        }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            v4u w;
+            words* const to = reinterpret_cast<words*>(at + k * kKvGroup);
+            words w;
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < U / 4; ++q)
                 w[q] = low_bytes(code_of<FINITE>(value_of(v[4 * q], k), r.inv), code_of<FINITE>(value_of(v[4 * q + 1], k), r.inv),
                                  code_of<FINITE>(value_of(v[4 * q + 2], k), r.inv), code_of<FINITE>(value_of(v[4 * q + 3], k), r.inv));
             if (!whole) {   // (what else stands there: tokens before the run, already at its scale, and what is past it, of no token)
-                const v4u was = group[k];
+                const words was = *to;
                 w = (w & mask) | (was & ~mask);
             }
-            group[k] = w;
+            *to = w;
         }
     }
 }
 
 // A run of n tokens from x on, whose slots begin at token `first` of a block, by one wavefront.  codes: of the block and head.
-template <typename T, bool VALUES, bool WIDE>
+// U: tokens of a lane's units where the run is no short one.
+template <typename T, bool VALUES, bool WIDE, int U>
 __device__ inline void append_run(const CacheParams& p, const T* x, int64_t stride, int8_t* codes, float* scale_at, int first, int n) {
     const int lane = threadIdx.x & 63, pieces = (p.dim + 7) / 8, items = n * pieces;
     const float old = first > 0 ? *scale_at : 0.0f;
     const bool few = !WIDE || items <= 64;
-    // Few tokens (and rows that are read by elements): a lane has 8 columns of a token, as often as it takes.  Else it has units of 16
+    // Few tokens (and rows that are read by elements): a lane has 8 columns of a token, as often as it takes.  Else it has units of U
     // tokens of a group and 8 columns, mostly one.
-    const int units = p.block / kKvGroup * pieces;
-    Eight<T> e, v[WIDE ? kKvGroup : 1];
-    // (every token of a group is loaded, from rows that exist, so that the loads go out together)
+    const int units = p.block / U * pieces;
+    Eight<T> e, v[U];
+    // (every token of a unit is loaded, from rows that exist, so that the loads go out together)
     auto load = [&](int o, int d) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < (WIDE ? kKvGroup : 1); ++j) load_eight<T, WIDE>(v[j], x + (int64_t)min(max(o + j - first, 0), n - 1) * stride, d, p.dim);
+        for (int j = 0; j < U; ++j) load_eight<T, WIDE>(v[j], x + (int64_t)min(max(o + j - first, 0), n - 1) * stride, d, p.dim);
     };
     uint32_t most = 0;
     if (few) {
@@ -202,11 +209,11 @@ __device__ inline void append_run(const CacheParams& p, const T* x, int64_t stri
     } else if constexpr (WIDE) {
 #pragma unroll 1
         for (int u = lane; u < units; u += 64) {
-            const int o = u / pieces * kKvGroup, d = u % pieces * 8;
-            if (o + kKvGroup <= first || o >= first + n) continue;
+            const int o = u / pieces * U, d = u % pieces * 8;
+            if (o + U <= first || o >= first + n) continue;
             load(o, d);
 #pragma unroll
-            for (int j = 0; j < kKvGroup; ++j) most = max_bits(most, v[j]);
+            for (int j = 0; j < U; ++j) most = max_bits(most, v[j]);
         }
     }
     // (as bits: those of an infinity or a NaN are above all others, where a maximum of floats would pass a NaN by)
@@ -260,17 +267,17 @@ __device__ inline void append_run(const CacheParams& p, const T* x, int64_t stri
     } else if constexpr (WIDE) {
 #pragma unroll 1
         for (int u = lane; u < units; u += 64) {
-            const int o = u / pieces * kKvGroup, d = u % pieces * 8;
-            if (o + kKvGroup <= first || o >= first + n) continue;
+            const int o = u / pieces * U, d = u % pieces * 8;
+            if (o + U <= first || o >= first + n) continue;
             if (units > 64) load(o, d);   // (with one unit to a lane it is there)
-            if (finite) store_unit<T, VALUES, true>(p, v, codes, o, d, first, n, r);
-            else store_unit<T, VALUES, false>(p, v, codes, o, d, first, n, r);
+            if (finite) store_unit<T, VALUES, true, U>(p, v, codes, o, d, first, n, r);
+            else store_unit<T, VALUES, false, U>(p, v, codes, o, d, first, n, r);
         }
     }
 }
 
 constexpr int kAppendHeads = 2, kAppendWaves = 2 * kAppendHeads;
-template <typename T, bool WIDE>
+template <typename T, bool WIDE, int U>
 __global__ __launch_bounds__(kAppendWaves * 64) void kv_append_kernel(const CacheParams p) {
     __shared__ int64_t s_slot[kMaxWindow + kMaxBlock + 1];   // of the token before the window, the window, and what a run can reach
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -308,8 +315,8 @@ __global__ __launch_bounds__(kAppendWaves * 64) void kv_append_kernel(const Cach
         const T* const x = static_cast<const T*>(s.x) + (t0 + w) * s.token_stride + head * s.head_stride;
         int8_t* const codes = s.codes + (block * p.heads + head) * p.block * p.cols;
         float* const scale_at = s.scale + block * p.heads + head;
-        if (side == 0) append_run<T, false, WIDE>(p, x, s.token_stride, codes, scale_at, first, n);
-        else append_run<T, true, WIDE>(p, x, s.token_stride, codes, scale_at, first, n);
+        if (side == 0) append_run<T, false, WIDE, U>(p, x, s.token_stride, codes, scale_at, first, n);
+        else append_run<T, true, WIDE, U>(p, x, s.token_stride, codes, scale_at, first, n);
     }
 }
 
@@ -470,8 +477,14 @@ int fill(CacheParams& p, const char* fn, const abft_kv_cache_t* c, const void* K
 template <typename T>
 void launch_append(const CacheParams& p, hipStream_t s) {
     const dim3 grid((unsigned)((p.n_tokens + p.window - 1) / p.window), (unsigned)((p.heads + kAppendHeads - 1) / kAppendHeads)), threads(kAppendWaves * 64);
-    if (p.side[0].wide && p.side[1].wide) kv_append_kernel<T, true><<<grid, threads, 0, s>>>(p);
-    else kv_append_kernel<T, false><<<grid, threads, 0, s>>>(p);
+    // So few tokens to a lane's units that a block has one for every lane, if it can (us with the read behind, 16 tokens / the rule: 6000 tokens of
+    // one request, 8 heads of 128, blocks of 16 24.3 / 20.8, of 32 22.2 / 20.2; 40 requests of up to 300, 5 heads of 80, blocks of 16 15.7 / 12.8;
+    // 30 of up to 200, 8 heads of 64, binary32, blocks of 16 18.1 / 13.0).
+    const int pieces = (p.dim + 7) / 8, unit = p.block / 4 * pieces <= 64 ? 4 : p.block / 8 * pieces <= 64 ? 8 : 16;
+    if (!p.side[0].wide || !p.side[1].wide) kv_append_kernel<T, false, 4><<<grid, threads, 0, s>>>(p);
+    else if (unit == 4) kv_append_kernel<T, true, 4><<<grid, threads, 0, s>>>(p);
+    else if (unit == 8) kv_append_kernel<T, true, 8><<<grid, threads, 0, s>>>(p);
+    else kv_append_kernel<T, true, 16><<<grid, threads, 0, s>>>(p);
 }
 
 }  // namespace
