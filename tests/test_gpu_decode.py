@@ -343,6 +343,36 @@ def test_attention_several_new_tokens(b, dtype, dim, block, group):
         check(b, c, parts, table, lengths, cu, q, dtype, max(fresh), max(lengths))
 
 
+@pytest.mark.parametrize("dtype,dim,block", [("f32", 16, 16), ("bf16", 64, 64), ("f16", 100, 32), ("f32", 128, 128), ("bf16", 192, 16), ("f32", 256, 64)])
+def test_attention_with_rows_split(b, dtype, dim, block):
+    """As many heads and requests as take the kernel whose wavefronts split the rows: 1000 workgroups."""
+    rng = np.random.default_rng(dim)
+    lengths = rng.integers(17, 140, 25)
+    fresh = rng.integers(1, 18, 25)
+    fresh[3], lengths[5], fresh[7] = 0, 0, 17
+    c, parts, table, cu, q = build(b, rng, lengths, fresh, 40, 40, dim, block, dtype)
+    check(b, c, parts, table, lengths, cu, q, dtype, 17, 140)
+
+
+def test_attention_with_rows_split_over_several_workgroups(b):
+    rng = np.random.default_rng(9)
+    lengths, fresh = np.array([150, 131]), np.array([129, 131])
+    c, parts, table, cu, q = build(b, rng, lengths, fresh, 250, 250, 8, 32, "bf16")
+    check(b, c, parts, table, lengths, cu, q, "bf16", 131, 150)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,block", [(64, 16), (128, 64), (100, 32)])
+def test_attention_with_eight_wavefronts(b, dtype, dim, block):
+    rng = np.random.default_rng(dim + block)
+    lengths = rng.integers(1, 1300, 13)
+    lengths[2], lengths[4] = 0, 1300
+    c, parts, table, cu, q = build(b, rng, lengths, np.ones(13, int), 20, 10, dim, block, dtype)
+    check(b, c, parts, table, lengths, cu, q, dtype, 1, 1300)
+    lengths = np.minimum(lengths, 511)
+    check(b, c, parts, table, lengths, cu, q, dtype, 1, 512)
+
+
 @pytest.mark.parametrize("block", [16, 64])
 def test_attention_in_parts_with_any_workspace_and_any_hint(b, block):
     """Long requests are cut; sizes that are only hints, and too small a workspace, change the cut and not the result."""

@@ -126,7 +126,7 @@ def test_step_refuses_what_does_not_fit(b):
 
 # ---------------------------------------------------------------------------------------------- many tokens, large caches
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("heads,dim,block,tokens", [(2, 64, 16, 2500), (5, 24, 64, 3000), (8, 128, 32, 2100)])
+@pytest.mark.parametrize("heads,dim,block,tokens", [(2, 64, 16, 2500), (5, 24, 64, 3000), (8, 128, 32, 2100), (3, 128, 64, 2200), (3, 33, 32, 2200)])
 def test_append_of_many_tokens(b, dtype, heads, dim, block, tokens):
     """Runs of every length and singles in one long call, blocks in no order; then read back in groups of any alignment."""
     rng = np.random.default_rng(tokens + heads)
