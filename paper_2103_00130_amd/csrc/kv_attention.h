@@ -88,6 +88,7 @@ typedef uint32_t attn_v4u __attribute__((ext_vector_type(4)));
 typedef float attn_v4f __attribute__((ext_vector_type(4)));
 
 constexpr int kAttnTile = kKvTile;
+constexpr float kLargeScore = 16384.0f;   // (base 2; half a step of anything smaller is 2^-11, a numerator of 1.0003)
 constexpr float kSlack = 12.0f;   // (a sum of 2^31 numerators of 2^12 is far from binary32's end)
 
 // over the lanes l % 16, + 16, + 32, + 48
@@ -372,6 +373,13 @@ __global__ __launch_bounds__(64 * NW, NW > 4 ? NW / 4 : attn_waves(attn_digits(s
                 for (int j = 1; j < 16; ++j) mine_most = fmaxf(mine_most, z[j]);
                 mine_most *= f;
                 const float most = max_of_four(mine_most), ref = most == -INFINITY ? 0.0f : most;
+                // The largest is a rounded product, a numerator's exponent an unrounded one less that: up to half a step of the largest above
+                // zero, and numerators have room for 1.0039.  Where a step is no longer small, products are rounded first: nothing is above zero then.
+                if (__any(fabsf(most) >= kLargeScore && most != -INFINITY)) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) z[j] *= f;
+                    f = 1.0f;
+                }
                 float part_sum = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {

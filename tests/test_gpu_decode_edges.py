@@ -1,0 +1,81 @@
+"""The decoding-step operators at the ends of what they take: scores, scales, lengths and estimates far from the usual."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode_oracle as o
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2103_00130_amd import binding
+    assert torch.cuda.is_available()
+    return binding
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).to("cuda")
+    return t if dtype is None else t.to(dtype)
+
+
+def f64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def within(got, want, tol, what):
+    off = np.abs(got - want) > tol
+    assert not (off | ~np.isfinite(got)).any(), f"{what}: {off.sum()} of {got.size} beyond the bound, worst {np.max(np.abs(got - want) / np.maximum(tol, 1e-300)):.3g} times"
+
+
+# ---------------------------------------------------------------------------------------------------------- large scores
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("block", [16, 64])
+@pytest.mark.parametrize("requests,heads,group,new", [(6, 2, 4, 1), (3, 2, 3, 20), (25, 40, 1, 17)])
+def test_attention_of_large_scores(b, dtype, block, requests, heads, group, new):
+    """One token's score is far above all others, by so much that the weight of any other is zero: the output is that token's value,
+    whatever the size and sign of the scores.  New tokens see whole tiles and parts of one."""
+    rng = np.random.default_rng(block + requests)
+    dim, length = 64, 192 + new
+    n = -(-length // block)
+    table = rng.permutation(requests * n).reshape(requests, n).astype(np.int32)
+    rows = requests * new
+    cu = np.arange(requests + 1, dtype=np.int32) * new
+    at = rng.integers(0, 192, (requests, heads))              # the token that stands out
+    sign = rng.choice([-1.0, 1.0], (requests, heads, dim))
+    v = rng.integers(-127, 128, (requests * n, heads, block, dim)).astype(np.int8)
+    ks, vs = ((np.exp(rng.standard_normal((requests * n, heads)) * 0.4) * 0.03).astype(np.float32) for _ in range(2))
+    # rows of Q whose elements are all of one size, so that they are whole steps of their row's largest
+    amp = torch.from_numpy(rng.uniform(1, 4, (rows, heads * group, 1)).astype(np.float32)).to(TYPES[dtype]).float()
+    q = (amp * torch.from_numpy(np.repeat(np.repeat(sign, group, 1), new, 0).astype(np.float32))).to(TYPES[dtype]).cuda()
+    who = np.repeat(np.arange(requests), new)
+    for size in (1e5, 1e6, 1e7, 1e12):
+        for least, most in ((20, 127), (20, -127), (-127, -60)):
+            # codes along the row's signs: of others up to `least` (or all `least`), of the one `most`; a negative scale for a negative one
+            near = rng.integers(-20, 21, (requests * n, heads, block, dim)).astype(np.float64)
+            k = near if least == 20 else np.full(near.shape, float(least))
+            scale = size / (127 * dim * 4 * 0.03) * (-1 if most == -127 else 1)
+            for r in range(requests):
+                for h in range(heads):
+                    if least != 20:
+                        for blk in table[r]:
+                            k[blk, h] *= sign[r, h]
+                    k[table[r, at[r, h] // block], h, at[r, h] % block] = most * sign[r, h]
+            ks_now = np.full_like(ks, 0.03) if least != 20 else ks
+            k = k.astype(np.int8)
+            c = b.KvCache(requests * n, heads, dim, block)
+            c.load_codes(dev(k), dev(v), dev(ks_now), dev(vs))
+            out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+            b.abft_kv_attention(c, q, dev(table), dev(np.full(requests, length, np.int32)), dev(cu), out, new, length, scale=scale, lse=lse,
+                                workspace=b.KvWorkspace(c, requests, heads * group, new, length).tensor)
+            of_head = np.arange(heads * group) // group
+            blk = table[who[:, None], at[who][:, of_head] // block]
+            off = at[who][:, of_head] % block
+            want = v[blk, of_head[None], off].astype(np.float64) * vs[blk, of_head[None]].astype(np.float64)[:, :, None]
+            # a dozen roundings of binary32 (its weight is one, a whole number of steps), and the one to the type
+            within(f64(out), want, np.abs(want) * (2.0 ** -19 + o.UNIT[dtype]), f"scores of {size} ({least}, {most})")
+            score = (k[blk, of_head[None], off].astype(np.float64) * f64(q)).sum(2) * ks_now[blk, of_head[None]].astype(np.float64) * scale
+            within(f64(lse), score, np.abs(score) * 2.0 ** -20, f"lse of scores of {size} ({least}, {most})")
