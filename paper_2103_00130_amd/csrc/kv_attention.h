@@ -105,6 +105,10 @@ __device__ inline float sum_of_four(float v) {
     return __builtin_bit_cast(float, (uint32_t)b[0]) + __builtin_bit_cast(float, (uint32_t)b[1]);
 }
 
+// Parts that a request of len tokens has: what lies past the last one's chunk is the last one's too.  (Chunks go up to the longest length
+// that there is: nothing is added to a length.)
+__device__ inline int parts_of(const AttnParams& p, int len) { return len <= 0 ? 1 : min(p.parts, (len - 1) / p.chunk + 1); }
+
 // The same number, of which the compiler knows nothing: what depends on it is computed where it is used, not ahead of a loop in
 // which it would hold registers.
 __device__ inline int here_only(int x) {
@@ -191,8 +195,7 @@ __global__ __launch_bounds__(64 * NW, NW > 4 ? NW / 4 : attn_waves(attn_digits(s
     const int fresh = (int)(c1 - c0);
     const int rows = fresh * p.group;   // (n_rows * q_heads is below 2^31)
     const int32_t* const table = p.table + (int64_t)req * p.ldt;
-    // parts that this request has: what lies past the last one's chunk is the last one's too
-    const int mine = len <= 0 ? 1 : min(p.parts, (len + p.chunk - 1) / p.chunk);
+    const int mine = parts_of(p, len);
     if (part >= mine) return;
     bool bad_block = false;
 
@@ -527,7 +530,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(const AttnParams
     const int64_t room = (int64_t)p.width << p.block_shift;
     const int len = (int)min((int64_t)max(p.seq_len[req], 0), room);
     const int64_t c0 = min((int64_t)max(p.cu_new[req], 0), p.n_rows), c1 = min(max((int64_t)p.cu_new[req + 1], c0), p.n_rows);
-    const int parts = len <= 0 ? 1 : min(p.parts, (len + p.chunk - 1) / p.chunk);
+    const int parts = parts_of(p, len);
     if (parts <= 1) return;
     const int64_t all_rows = p.n_rows * p.q_heads;
     // (with a row shared, all of a workgroup are at the same one)

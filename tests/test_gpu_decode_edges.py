@@ -79,3 +79,28 @@ def test_attention_of_large_scores(b, dtype, block, requests, heads, group, new)
             within(f64(out), want, np.abs(want) * (2.0 ** -19 + o.UNIT[dtype]), f"scores of {size} ({least}, {most})")
             score = (k[blk, of_head[None], off].astype(np.float64) * f64(q)).sum(2) * ks_now[blk, of_head[None]].astype(np.float64) * scale
             within(f64(lse), score, np.abs(score) * 2.0 ** -20, f"lse of scores of {size} ({least}, {most})")
+
+
+# ------------------------------------------------------------------------------------------------------ lengths as estimates
+@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("f32", 20)])
+@pytest.mark.parametrize("workspace", [False, True])
+def test_attention_with_the_longest_estimate(b, dtype, new, workspace):
+    """max_len is an estimate: the largest that is taken gives the results of any other."""
+    rng = np.random.default_rng(new)
+    heads, group, dim, block = 2, 4, 64, 64
+    lengths = np.array([700, 30, 0, 513, 1025])
+    n_blocks = 40
+    k, v = (rng.integers(-127, 128, (n_blocks, heads, block, dim)).astype(np.int8) for _ in range(2))
+    ks, vs = ((rng.random((n_blocks, heads)) * 0.03 + 0.01).astype(np.float32) for _ in range(2))
+    c = b.KvCache(n_blocks, heads, dim, block)
+    c.load_codes(dev(k), dev(v), dev(ks), dev(vs))
+    table = np.concatenate([rng.permutation(n_blocks)[:17] for _ in lengths]).reshape(len(lengths), 17).astype(np.int32)
+    cu = (np.arange(len(lengths) + 1) * new).astype(np.int32)
+    q = torch.from_numpy(rng.standard_normal((int(cu[-1]), heads * group, dim)).astype(np.float32)).to(TYPES[dtype]).cuda()
+    want, tol, _, _ = o.attention(f64(q), k, v, ks, vs, table, lengths, cu, dim ** -0.5, dtype)
+    longest = 2 ** 31 - 512
+    ws = b.KvWorkspace(c, len(lengths), heads * group, new, longest).tensor if workspace else None
+    for max_len in (longest, longest - 1, 2 ** 31 - 1200, 2 ** 30):
+        out = torch.full_like(q, 9.0)
+        b.abft_kv_attention(c, q, dev(table), dev(lengths.astype(np.int32)), dev(cu), out, new, max_len, workspace=ws)
+        within(f64(out), want, tol, f"max_len {max_len}")
