@@ -147,7 +147,7 @@ size_t abft_kv_code_bytes(const abft_kv_cache_t* cache);
 
 /* bits of the flags that abft_kv_plan and abft_kv_attention write for each request */
 #define ABFT_KV_NO_BLOCK 1     /* plan: the pool ran out of free blocks */
-#define ABFT_KV_TABLE_FULL 2   /* plan: more tokens than a row of the table has blocks for */
+#define ABFT_KV_TABLE_FULL 2   /* plan: more tokens than a row of the table has blocks for, or than 2^31 - 1 */
 #define ABFT_KV_NO_ROW 4       /* plan: its tokens lie past n_slots */
 #define ABFT_KV_BAD_LENGTH 8   /* plan: a negative length, taken as 0 */
 #define ABFT_KV_BAD_BLOCK 16   /* attention: the table names a block that the cache does not have; its tokens were left out */

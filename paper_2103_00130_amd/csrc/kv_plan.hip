@@ -106,14 +106,19 @@ __global__ __launch_bounds__(NT) void kv_plan_kernel(const PlanParams p) {
     }
     // blocks a request holds and wants, unless its row of the table is too short
     auto held = [&](int i) __attribute__((always_inline)) { return blocks_for(p, max(ctx_in[i], 0)); };
-    auto wanted = [&](int i) __attribute__((always_inline)) { return blocks_for(p, (int64_t)max(ctx_in[i], 0) + max(fresh_in[i], 0)); };
+    // (no row of the table has so many blocks as 2^31 tokens or more come to here: blocks can be so large that it has room for them, but
+    // a length has 31 bits)
+    auto wanted = [&](int i) __attribute__((always_inline)) {
+        const uint32_t tokens = (uint32_t)max(ctx_in[i], 0) + (uint32_t)max(fresh_in[i], 0);
+        return (int)tokens < 0 ? 0x80000000u : tokens ? blocks_below(p, tokens - 1) + 1 : 0u;
+    };
     auto sums = [&](uint32_t rows_before, bool limited) __attribute__((always_inline)) {
         Two t = {0, 0};
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             t.rows = add31(t.rows, (uint32_t)max(fresh_in[i], 0));
-            const int64_t want = wanted(i);
-            if (want <= p.width && !(limited && add31(rows_before, t.rows) > p.n_slots)) t.need = add31(t.need, (uint32_t)(want - held(i)));
+            const uint32_t want = wanted(i);
+            if (want <= (uint32_t)p.width && !(limited && add31(rows_before, t.rows) > p.n_slots)) t.need = add31(t.need, want - (uint32_t)held(i));
         }
         return t;
     };

@@ -104,3 +104,21 @@ def test_attention_with_the_longest_estimate(b, dtype, new, workspace):
         out = torch.full_like(q, 9.0)
         b.abft_kv_attention(c, q, dev(table), dev(lengths.astype(np.int32)), dev(cu), out, new, max_len, workspace=ws)
         within(f64(out), want, tol, f"max_len {max_len}")
+
+
+# ------------------------------------------------------------------------------------------------------------------- plans
+def test_plan_refuses_lengths_past_32_bits(b):
+    """A request that would hold 2^31 tokens or more is refused, though its row of the table has blocks for them: a length has 32 bits."""
+    most, block = 2 ** 31 - 1, 2 ** 20
+    ctx, new = [most - 3, most, 7, most - 3, 0], [3, 5, 2, 4, most]
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    table = torch.full((5, 2050), -1, dtype=torch.int32, device="cuda")
+    table[:, :2048] = torch.arange(2048, dtype=torch.int32, device="cuda")
+    free = i32([5000, 5001, 5002])
+    seq, cu, flags, taken = i32([-77] * 5), i32([-77] * 6), i32([-77] * 5), i32([-77])
+    slots = torch.full((16,), -77, dtype=torch.int64, device="cuda")
+    b.abft_kv_plan(i32(ctx), i32(new), block, table, free, seq, cu, slots, flags, taken)
+    assert flags.tolist() == [0, b.ABFT_KV_TABLE_FULL, 0, b.ABFT_KV_TABLE_FULL, b.ABFT_KV_NO_ROW]
+    assert seq.tolist() == [most, most, 9, most - 3, 0] and cu.tolist() == [0, 3, 8, 10, 14, 16] and taken.tolist() == [0]
+    assert slots.tolist() == [most - 3, most - 2, most - 1] + [-1] * 5 + [7, 8] + [-1] * 6
+    assert (table[:, 2048:] == -1).all()
