@@ -378,16 +378,25 @@ __global__ __launch_bounds__(64 * NW, NW > 4 ? NW / 4 : attn_waves(attn_digits(s
                 const float most = max_of_four(mine_most), ref = most == -INFINITY ? 0.0f : most;
                 // The largest is a rounded product, a numerator's exponent an unrounded one less that: up to half a step of the largest above
                 // zero, and numerators have room for 1.0039.  Where a step is no longer small, products are rounded first: nothing is above zero then.
-                if (__any(fabsf(most) >= kLargeScore && most != -INFINITY)) {
+                const float at_most = SMALL ? mine_most : most;   // (what the exponents are relative to, below)
+                if (__any(fabsf(at_most) >= kLargeScore && at_most != -INFINITY)) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) z[j] *= f;
                     f = 1.0f;
                 }
+                // (small blocks: relative to the largest of the lane, so that what makes them digits is bounded whatever the lanes' scales are)
+                const float own_ref = at_most == -INFINITY ? 0.0f : at_most;
                 float part_sum = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    z[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], f, -ref));
+                    z[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], f, -own_ref));
                     part_sum += z[j];
+                }
+                float own = 0.0f;   // the lane's largest numerator, times its block's scale
+                if constexpr (SMALL) {
+                    const float share = mine_most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine_most - ref);
+                    part_sum *= share;
+                    own = mine_most == -INFINITY ? 0.0f : share * vs;   // (a lane that sees nothing has no say, whatever its block's scale is)
                 }
                 if (__any(most > top[rt] + kSlack)) {   // (the first tile's too)
                     const float up = fmaxf(top[rt], most), keep = up == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[rt] - up);
@@ -403,10 +412,8 @@ __global__ __launch_bounds__(64 * NW, NW > 4 ? NW / 4 : attn_waves(attn_digits(s
                 constexpr float one = Fixed<ND, false>::kOne;
                 float to_one = one, worth;   // what makes a numerator a fixed-point number, and what a step of that is worth
                 if constexpr (SMALL) {
-                    // (a lane that sees nothing has no say, whatever its block's scale is)
-                    const float own = mine_most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine_most - ref) * vs;
                     const float big = max_of_four(own);
-                    to_one = big >= 0x1p-100f && mine_most != -INFINITY ? one / big * vs : 0.0f;
+                    to_one = big >= 0x1p-100f ? own / big * one : 0.0f;
                     worth = add * big * (1.0f / one);
                 } else {
                     worth = add > 0.0f ? add * vs * (1.0f / one) : add * 0.0f;

@@ -122,3 +122,31 @@ def test_plan_refuses_lengths_past_32_bits(b):
     assert seq.tolist() == [most, most, 9, most - 3, 0] and cu.tolist() == [0, 3, 8, 10, 14, 16] and taken.tolist() == [0]
     assert slots.tolist() == [most - 3, most - 2, most - 1] + [-1] * 5 + [7, 8] + [-1] * 6
     assert (table[:, 2048:] == -1).all()
+
+
+# ------------------------------------------------------------------------------------------------------ scales of values
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("block", [16, 32, 64])
+@pytest.mark.parametrize("heads,new", [(2, 1), (40, 17)])
+def test_attention_with_scales_of_values_far_apart(b, dtype, block, heads, new):
+    """Blocks whose tokens have no weight hold values that are forty orders of magnitude above those of the blocks that have all of it."""
+    rng = np.random.default_rng(block + heads)
+    dim, length, requests = 64, 128 + new, 25 if heads == 40 else 3
+    n = -(-length // block)
+    table = rng.permutation(requests * n).reshape(requests, n).astype(np.int32)
+    shape = (requests * n, heads)
+    k, v = (rng.integers(1, 128, shape + (block, dim)).astype(np.int8) for _ in range(2))
+    ks, vs = np.zeros(shape, np.float32), np.full(shape, 1e-5, np.float32)
+    low = table[:, 1]                    # the second block of every request: scores far below zero, the others' are all zero
+    ks[low], vs[low] = 1.0, 1e35
+    q = -torch.ones((requests * new, heads, dim)).to(TYPES[dtype]).cuda()      # (scores of -64 or less, base e, times the scale)
+    c = b.KvCache(requests * n, heads, dim, block)
+    c.load_codes(dev(k), dev(v), dev(ks), dev(vs))
+    cu = (np.arange(requests + 1) * new).astype(np.int32)
+    for scale in (5.0, 100.0, 1e10):
+        out = torch.empty_like(q)
+        b.abft_kv_attention(c, q, dev(table), dev(np.full(requests, length, np.int32)), dev(cu), out, new, length, scale=scale)
+        want, tol, _, _ = o.attention(f64(q), k, v, ks, vs, table, [length] * requests, cu, scale, dtype)
+        within(f64(out), want, tol, f"scale {scale}")
+        # (weights of exactly one, whole numbers of steps, and of zero: a dozen roundings, and as many as there are tiles)
+        within(f64(out), want, np.abs(want) * (2.0 ** -18 + o.UNIT[dtype]) + o.TINY[dtype], f"scale {scale}, all weights alike")
