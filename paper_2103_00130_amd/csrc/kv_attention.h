@@ -413,7 +413,7 @@ __global__ __launch_bounds__(64 * NW, NW > 4 ? NW / 4 : attn_waves(attn_digits(s
                 float to_one = one, worth;   // what makes a numerator a fixed-point number, and what a step of that is worth
                 if constexpr (SMALL) {
                     const float big = max_of_four(own);
-                    to_one = big >= 0x1p-100f ? own / big * one : 0.0f;
+                    to_one = big > 0.0f ? own / big * one : 0.0f;
                     worth = add * big * (1.0f / one);
                 } else {
                     worth = add > 0.0f ? add * vs * (1.0f / one) : add * 0.0f;

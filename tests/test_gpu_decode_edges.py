@@ -150,3 +150,23 @@ def test_attention_with_scales_of_values_far_apart(b, dtype, block, heads, new):
         within(f64(out), want, tol, f"scale {scale}")
         # (weights of exactly one, whole numbers of steps, and of zero: a dozen roundings, and as many as there are tiles)
         within(f64(out), want, np.abs(want) * (2.0 ** -18 + o.UNIT[dtype]) + o.TINY[dtype], f"scale {scale}, all weights alike")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("block", [16, 32, 64])
+def test_attention_of_values_near_the_least(b, dtype, block):
+    """Values down to 2^-103 come back like any others, in blocks of any size."""
+    rng = np.random.default_rng(block)
+    dim, length, heads = 64, 100, 2
+    n = -(-length // block)
+    table = rng.permutation(n).reshape(1, n).astype(np.int32)
+    k, v = (rng.integers(1, 128, (n, heads, block, dim)).astype(np.int8) for _ in range(2))
+    q = torch.from_numpy(rng.standard_normal((1, heads, dim)).astype(np.float32)).to(TYPES[dtype]).cuda()
+    for least in (2.0 ** -99, 2.0 ** -101, 2.0 ** -103):
+        ks, vs = np.full((n, heads), 0.001, np.float32), np.full((n, heads), least, np.float32)
+        c = b.KvCache(n, heads, dim, block)
+        c.load_codes(dev(k), dev(v), dev(ks), dev(vs))
+        out = torch.empty_like(q)
+        b.abft_kv_attention(c, q, dev(table), dev(np.array([length], np.int32)), dev(np.array([0, 1], np.int32)), out, 1, length)
+        want, tol, _, _ = o.attention(f64(q), k, v, ks, vs, table, [length], [0, 1], dim ** -0.5, dtype)
+        within(f64(out), want, tol, f"values of {least}")
