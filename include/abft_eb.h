@@ -201,7 +201,8 @@ int abft_kv_read(const abft_kv_cache_t* cache, const int64_t* slots, int64_t n_t
  *              the work is cut, not what comes out
  *   lse        float32 [n_rows][q_heads] or NULL: the natural logarithm of the sum of exp(scale * Q . K), -inf for a
  *              row that sees nothing
- *   req_flags  int32 [n_req] or NULL: overwritten with ABFT_KV_BAD_BLOCK or 0
+ *   req_flags  int32 [n_req] or NULL: overwritten with ABFT_KV_BAD_BLOCK or 0 (n_rows == 0 is a valid call that does no more than that,
+ *              whatever max_new and max_len are)
  *   workspace  abft_kv_attention_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant; NULL or a smaller one: long
  *              requests are cut into fewer parts
  * Q and the softmax's numerators enter the matrix cores as signed base-256 digits (two of them for 16-bit

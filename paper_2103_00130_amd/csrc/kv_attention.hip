@@ -58,6 +58,11 @@ __global__ __launch_bounds__(256) void kv_clear_flags_kernel(int32_t* flags, int
     const int i = blockIdx.x * 256 + threadIdx.x;
     if (i < n) flags[i] = 0;
 }
+hipError_t clear_flags(int32_t* flags, int n, hipStream_t s) {
+    if (!flags) return hipSuccess;
+    kv_clear_flags_kernel<<<dim3((unsigned)(((int64_t)n + 255) / 256)), dim3(256), 0, s>>>(flags, n);
+    return hipGetLastError();
+}
 
 }  // namespace
 }  // namespace abft
@@ -80,9 +85,14 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
     if (!abft::known_type(type)) return abft::set_error(ABFT_EINVAL, "%s: unknown type %d", fn, type);
     if (n_rows < 0 || n_req < 0 || width < 0) return abft::set_error(ABFT_EINVAL, "%s: negative count", fn);
     if (q_heads < 1 || q_heads % cache->heads != 0) return abft::set_error(ABFT_EINVAL, "%s: q_heads=%d must be a multiple of the cache's %d heads", fn, q_heads, cache->heads);
-    if (max_new < 1 || max_len < 1) return abft::set_error(ABFT_EINVAL, "%s: max_new=%d and max_len=%d must be >= 1", fn, max_new, max_len);
     if (!std::isfinite(scale)) return abft::set_error(ABFT_EINVAL, "%s: scale must be finite", fn);
-    if (n_rows == 0 || n_req == 0) return ABFT_OK;
+    if (n_req == 0) return ABFT_OK;
+    hipStream_t s = (hipStream_t)stream;
+    if (n_rows == 0) {   // nothing to do but to overwrite the flags
+        const hipError_t e = abft::clear_flags(req_flags, n_req, s);
+        return e == hipSuccess ? ABFT_OK : abft::set_error(ABFT_EHIP, "%s: %s", fn, hipGetErrorString(e));
+    }
+    if (max_new < 1 || max_len < 1) return abft::set_error(ABFT_EINVAL, "%s: max_new=%d and max_len=%d must be >= 1", fn, max_new, max_len);
     if (!Q || !O || !table || !seq_len || !cu_new) return abft::set_error(ABFT_EINVAL, "%s: null pointer", fn);
     if (ldt < width) return abft::set_error(ABFT_EINVAL, "%s: ldt=%lld smaller than width=%d", fn, (long long)ldt, width);
     const uintptr_t es = (uintptr_t)abft::type_size(type);
@@ -138,12 +148,7 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
     p.chunk = c.chunk;
     p.scale2 = scale * 1.44269504f;
     p.q_wide = ((reinterpret_cast<uintptr_t>(Q) | (uintptr_t)(q_token_stride * (int64_t)es) | (uintptr_t)(q_head_stride * (int64_t)es) | (uintptr_t)(cache->head_dim * (int64_t)es)) & (4 * es - 1)) == 0;
-    hipStream_t s = (hipStream_t)stream;
-    hipError_t e = hipSuccess;
-    if (req_flags) {
-        abft::kv_clear_flags_kernel<<<dim3((unsigned)((n_req + 255) / 256)), dim3(256), 0, s>>>(req_flags, n_req);
-        e = hipGetLastError();
-    }
+    hipError_t e = abft::clear_flags(req_flags, n_req, s);
     const bool small_blocks = cache->block_tokens < abft::kKvTile;
     if (e == hipSuccess)
         e = type == ABFT_TYPE_F32 ? abft::launch_attention_f32(c.shape, cols, small_blocks, p, (unsigned)workgroups, s)

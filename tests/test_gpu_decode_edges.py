@@ -170,3 +170,12 @@ def test_attention_of_values_near_the_least(b, dtype, block):
         b.abft_kv_attention(c, q, dev(table), dev(np.array([length], np.int32)), dev(np.array([0, 1], np.int32)), out, 1, length)
         want, tol, _, _ = o.attention(f64(q), k, v, ks, vs, table, [length], [0, 1], dim ** -0.5, dtype)
         within(f64(out), want, tol, f"values of {least}")
+
+
+def test_attention_of_no_rows_clears_the_flags(b):
+    c = b.KvCache(4, 2, 64, 16)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
+    q = torch.zeros((0, 4, 64), device="cuda")
+    flags = torch.full((300,), 99, dtype=torch.int32, device="cuda")
+    b.abft_kv_attention(c, q, i32(300, 4), i32(300), i32(301), q.clone(), 0, 0, req_flags=flags)
+    assert not flags.any()
