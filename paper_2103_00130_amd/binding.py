@@ -165,6 +165,17 @@ def _ptr(t, dtype, name):
     return t.data_ptr()
 
 
+def _lent(t, name):
+    """(address, bytes) of the memory that a caller lends: a contiguous device tensor of any type, or none."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _ld(t, name):
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{name} must be 2-D with unit column stride")
@@ -724,11 +735,9 @@ def abft_kv_attention(cache: KvCache, Q, table, seq_len, cu_new, O, max_new: int
         raise TypeError("Q and O must have the same type")
     if table.shape[0] != R:
         raise ValueError("table must have a row for each request")
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib.abft_kv_attention(
         cache.ref, *_kv_rows(Q, cache, n_rows, "Q", q_heads), q_type, n_rows, q_heads, _ptr(table, torch.int32, "table"),
         max(_ld(table, "table"), table.shape[1]), table.shape[1], _entries(seq_len, torch.int32, R, "seq_len"),
         _entries(cu_new, torch.int32, R + 1, "cu_new"), R, int(max_new), int(max_len), float(scale),
         *_kv_rows(O, cache, n_rows, "O", q_heads), None if lse is None else _entries(lse, torch.float32, n_rows * q_heads, "lse"),
-        None if req_flags is None else _entries(req_flags, torch.int32, R, "req_flags"), None if workspace is None else workspace.data_ptr(),
-        ws_bytes, _stream(stream)))
+        None if req_flags is None else _entries(req_flags, torch.int32, R, "req_flags"), *_lent(workspace, "workspace"), _stream(stream)))

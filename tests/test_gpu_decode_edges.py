@@ -179,3 +179,28 @@ def test_attention_of_no_rows_clears_the_flags(b):
     flags = torch.full((300,), 99, dtype=torch.int32, device="cuda")
     b.abft_kv_attention(c, q, i32(300, 4), i32(300), i32(301), q.clone(), 0, 0, req_flags=flags)
     assert not flags.any()
+
+
+# ------------------------------------------------------------------------------------------------------ memory of the caller
+def no_launch(b, monkeypatch, *names):
+    """From here on a call of these library functions fails the test."""
+    for name in names:
+        monkeypatch.setattr(b.lib, name, lambda *a, name=name: pytest.fail(f"{name} was called"))
+
+
+def test_attention_refuses_a_workspace_that_is_not_its_own_memory(b, monkeypatch):
+    rng = np.random.default_rng(1)
+    c = b.KvCache(64, 1, 64, 16)
+    q = torch.zeros((1, 1, 64), device="cuda")
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    table = torch.arange(64, dtype=torch.int32, device="cuda").reshape(1, 64)
+    call = lambda ws: b.abft_kv_attention(c, q, table, i32([1000]), i32([0, 1]), torch.empty_like(q), 1, 1000, workspace=ws)
+    size = b.abft_kv_attention_workspace_bytes(c, 1, 1, 1, 1000) // 4
+    assert size > 0
+    call(torch.empty(size, device="cuda"))
+    no_launch(b, monkeypatch, "abft_kv_attention")
+    with pytest.raises(TypeError):
+        call(torch.empty(size))
+    for ws in (torch.empty(1, device="cuda").expand(size), torch.empty(2 * size, device="cuda")[::2], torch.empty((size, 2), device="cuda").t()):
+        with pytest.raises(ValueError):
+            call(ws)
