@@ -253,7 +253,7 @@ def abft_gemm_workspace_bytes(M: int, Bp: PackedB) -> int:
 
 
 def abft_workspace_init(workspace: torch.Tensor, stream=None):
-    _check(lib.abft_workspace_init(workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
+    _check(lib.abft_workspace_init(*_lent(workspace, "workspace"), _stream(stream)))
 
 
 def make_requant(zA: int, zC: int, mult: torch.Tensor, bias: torch.Tensor | None = None) -> abft_requant_t:
@@ -289,14 +289,13 @@ def abft_gemm_u8s8s32_checked(A, Bp: PackedB, C, row_flags, err_count, rq=None, 
         raise ValueError("row_flags shorter than M")
     if inj is not None and inj.numel() < 3 * n_inj:
         raise ValueError("injection tensor shorter than n_inj entries")
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib.abft_gemm_u8s8s32_checked(
         _ptr(A, torch.uint8, "A"), _ld(A, "A"), M, Bp.handle,
         _ptr(C, torch.int32, "C"), 0 if C is None else _ld(C, "C"),
         _ptr(row_flags, torch.int32, "row_flags"), _ptr(err_count, torch.int32, "err_count"),
         None if rq is None else ctypes.byref(rq), _ptr(Cq, torch.uint8, "Cq"), 0 if Cq is None else _ld(Cq, "Cq"),
         _ptr(inj, torch.int32, "inj"), int(n_inj), int(flags),
-        None if workspace is None else workspace.data_ptr(), ws_bytes, _stream(stream)))
+        *_lent(workspace, "workspace"), _stream(stream)))
 
 
 ABFT_STATIC_WS_MAX_M = 131072
@@ -358,7 +357,7 @@ def abft_recompute_flagged_rows(A, Bp: PackedB, C, row_flags, err_count=None, rq
         _ptr(C, torch.int32, "C"), _ld(C, "C") if C is not None else 0,
         _ptr(row_flags, torch.int32, "row_flags"), _ptr(err_count, torch.int32, "err_count"),
         ctypes.byref(rq) if rq is not None else None, _ptr(Cq, torch.uint8, "Cq"), _ld(Cq, "Cq") if Cq is not None else 0,
-        max_rows_per_pass, scratch.data_ptr(), scratch.numel(), _stream(stream), ctypes.byref(before), ctypes.byref(after)))
+        max_rows_per_pass, *_lent(scratch, "scratch"), _stream(stream), ctypes.byref(before), ctypes.byref(after)))
     return before.value, after.value
 
 
@@ -376,7 +375,7 @@ def abft_recompute_flagged_rows_async(A, Bp: PackedB, C, row_flags, err_count=No
         _ptr(C, torch.int32, "C"), _ld(C, "C") if C is not None else 0,
         _ptr(row_flags, torch.int32, "row_flags"), _ptr(err_count, torch.int32, "err_count"),
         ctypes.byref(rq) if rq is not None else None, _ptr(Cq, torch.uint8, "Cq"), _ld(Cq, "Cq") if Cq is not None else 0,
-        max_rows, scratch.data_ptr(), scratch.numel(), _ptr(status, torch.int32, "status"), _stream(stream)))
+        max_rows, *_lent(scratch, "scratch"), _ptr(status, torch.int32, "status"), _stream(stream)))
     return status
 
 
@@ -400,7 +399,7 @@ def abft_locate_correct(A, Bp: PackedB, C, row_flags, err_count=None, rq=None, C
         _ptr(row_flags, torch.int32, "row_flags"), _ptr(err_count, torch.int32, "err_count"),
         ctypes.byref(rq) if rq is not None else None, _ptr(Cq, torch.uint8, "Cq"), _ld(Cq, "Cq") if Cq is not None else 0,
         _ptr(col_flags, torch.int32, "col_flags"), _ptr(report, torch.int32, "report"),
-        scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)))
+        *_lent(scratch, "scratch"), _stream(stream)))
     return report
 
 

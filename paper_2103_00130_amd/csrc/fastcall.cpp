@@ -130,6 +130,7 @@ PyObject* gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         size_t ws_bytes = 0;
         if (a[12] != Py_None) {
             const at::Tensor& w = tensor(a[12]);
+            if (!w.is_cuda() || !w.is_contiguous()) throw Leave{};
             ws = w.data_ptr();
             ws_bytes = (size_t)w.numel() * w.element_size();
         }

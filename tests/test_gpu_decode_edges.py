@@ -204,3 +204,21 @@ def test_attention_refuses_a_workspace_that_is_not_its_own_memory(b, monkeypatch
     for ws in (torch.empty(1, device="cuda").expand(size), torch.empty(2 * size, device="cuda")[::2], torch.empty((size, 2), device="cuda").t()):
         with pytest.raises(ValueError):
             call(ws)
+
+
+def test_checked_products_refuse_memory_that_is_not_lent_whole(b, monkeypatch):
+    """The workspace of the checked GEMM and the scratch of its repairs, as attention's."""
+    A = torch.zeros((8, 64), dtype=torch.uint8, device="cuda")
+    Bp = b.abft_pack_b_checksum(torch.ones((64, 32), dtype=torch.int8, device="cuda"))
+    C, flags = torch.zeros((8, 32), dtype=torch.int32, device="cuda"), torch.zeros(8, dtype=torch.int32, device="cuda")
+    ws = b.Workspace(8, Bp).tensor
+    b.abft_gemm_u8s8s32_checked(A, Bp, C, flags, None, workspace=ws)
+    torch.cuda.synchronize()
+    no_launch(b, monkeypatch, "abft_gemm_u8s8s32_checked", "abft_workspace_init", "abft_recompute_flagged_rows", "abft_recompute_flagged_rows_async", "abft_locate_correct")
+    n = ws.numel()
+    for bad, error in ((torch.zeros(n, dtype=torch.int32), TypeError), (ws[:1].expand(n), ValueError), (torch.zeros(2 * n, dtype=torch.int32, device="cuda")[::2], ValueError)):
+        for call in (lambda: b.abft_gemm_u8s8s32_checked(A, Bp, C, flags, None, workspace=bad), lambda: b.abft_workspace_init(bad),
+                     lambda: b.abft_recompute_flagged_rows(A, Bp, C, flags, scratch=bad), lambda: b.abft_recompute_flagged_rows_async(A, Bp, C, flags, scratch=bad),
+                     lambda: b.abft_locate_correct(A, Bp, C, flags, scratch=bad)):
+            with pytest.raises(error):
+                call()
