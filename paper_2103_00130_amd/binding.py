@@ -617,6 +617,8 @@ class KvCache:
         if not lib.abft_kv_code_bytes(ctypes.byref(abft_kv_cache_t(None, None, None, None, *self._sizes()))):
             raise ValueError(f"no cache of {n_blocks} blocks of {block_tokens} tokens, {heads} heads of {head_dim}: block_tokens must be 16, 32, 64 or 128, "
                              "head_dim 1..256, and there must be blocks and heads")
+        if torch.device(device).type != "cuda":
+            raise TypeError(f"a cache lies on a device, not on {device}: its addresses go to kernels")
         cols = (self.head_dim + 63) // 64 * 64
         self.k_codes = torch.zeros((self.n_blocks, self.heads, self.block_tokens, cols), dtype=torch.int8, device=device)
         self.v_codes = torch.zeros((self.n_blocks, self.heads, self.block_tokens // 16, cols, 16), dtype=torch.int8, device=device)

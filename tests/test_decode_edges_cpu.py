@@ -26,3 +26,9 @@ def test_memory_that_is_lent_is_contiguous_and_on_the_device(b):
     for t in (host[::2], host[:1].expand(6), host.reshape(2, 3).t()):
         with pytest.raises(ValueError):
             b._lent(OnDevice(t), "x")
+
+
+def test_a_cache_of_the_host_is_refused(b):
+    for device in ("cpu", torch.device("cpu"), "meta"):
+        with pytest.raises(TypeError):
+            b.KvCache(4, 2, 64, 16, device=device)
