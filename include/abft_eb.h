@@ -203,7 +203,8 @@ int abft_kv_read(const abft_kv_cache_t* cache, const int64_t* slots, int64_t n_t
  *              row that sees nothing
  *   req_flags  int32 [n_req] or NULL: overwritten with ABFT_KV_BAD_BLOCK or 0 (n_rows == 0 is a valid call that does no more than that,
  *              whatever max_new and max_len are)
- *   workspace  abft_kv_attention_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant; NULL or a smaller one: long
+ *   workspace  abft_kv_attention_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant: enough for every call on up to n_req
+ *              requests of up to max_new new tokens and max_len tokens (fewer or shorter ones want more parts).  NULL or a smaller one: long
  *              requests are cut into fewer parts
  * Q and the softmax's numerators enter the matrix cores as signed base-256 digits (two of them for 16-bit
  * types, three for binary32; numerators relative to the largest of their 64 tokens), so that the products

@@ -37,6 +37,7 @@
 #include <type_traits>
 
 #include "kv_cache.h"
+#include "kv_cut.h"
 #include "values.h"
 
 namespace abft {
@@ -64,15 +65,6 @@ struct AttnParams {
     bool q_wide;        // rows of Q are whole aligned pieces of four columns
 };
 
-// which kernel (one for each of them and each type, number of columns and kind of block)
-enum AttnShape {
-    kAttnTokens,    // 16 rows, tokens split among four wavefronts
-    kAttnTokens8,   // among eight (up to 128 columns)
-    kAttnRows       // rows split among four wavefronts
-};
-// Most rows of a wavefront, in sixteens.  More do not fit its registers, and a kernel that spills is not to be had: the compiler has put
-// the copy of a spilled register before the end of a divergent branch, where not every lane made it.
-constexpr int attn_rows_tiles(int cols) { return cols <= 64 ? 2 : 1; }
 // Wavefronts that are to share a SIMD's registers (512): what the kernels fit without spilling.
 constexpr int attn_waves(int digits, int cols, int row_tiles) { return cols == 256 ? 1 : digits == 2 && cols <= 128 && row_tiles == 1 ? 3 : 2; }
 constexpr int attn_digits(int type_size) { return type_size == 4 ? 3 : 2; }

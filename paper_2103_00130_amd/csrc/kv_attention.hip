@@ -6,54 +6,6 @@
 namespace abft {
 namespace {
 
-// How a call is cut, by what the host knows of it.  Rows of a request and cached head: new tokens times the query heads that share the
-// head.  All figures in us; heads "32 / 8" are 32 query heads over 8 cached ones, lengths ragged unless said otherwise.
-//
-// Which kernel.  Tokens split among the wavefronts, 16 rows to a workgroup: work of many small pieces, evenly dealt.  Rows split,
-// 64 (or 128) to a workgroup: less joining, fewer rows worked out twice; that wins where there are so many workgroups that pieces need not
-// be small, and loses where there are not (tokens / rows split; workgroups of the latter: 32 + 32 heads of 128, prompts of 2000,
-// 2048: 146 / 110; 16 + 16 of 64, 8 of 1024, 1024: 94 / 67; 32 / 8 of 128, 512 new of 4096, 512: 124 / 115; 40 / 8, 300 new of 6000,
-// 576: 176 / 326; 32 / 8, 150 new of 600, 480: 34 / 42; 12 + 12 of 64, 512 new of 4500, 192: 58 / 130, in 5 parts 66; 16 / 4, 64 new of
-// 2000, 128: 25 / 58, in 4 parts 37).
-// Eight wavefronts for a workgroup instead of four where that spares the cut and the join: a tile for each, or as many workgroups as fit at once
-// (eight / four, 32 / 8 of 128, single tokens: 1 request of 500 8.5 / 10.6, of 1000 11.1 / 10.7, of 200 7.2 / 7.1; 8 up to 1500
-// 14.5 / 12.7; 32 up to 1000 12.7 / 15.9, up to 2000 19.4 / 22.5, up to 3000 25.5 / 27.1).
-//
-// Parts, where tokens are split: enough for 512 workgroups, of no fewer tokens than a pass of the four wavefronts, or two if it is long (parts:
-// 1 / 4 / 16 / 64; 32 / 8 of 128, one of 8000 55.6 / 22.2 / 13.3 / 12.3; 8 up to 2000 18.9 / 13.7 / 13.3 / 13.4; 16 up to 30000,
-// 64 workgroups 237 / 77 / 63 / 61; 4 up to 200000, 32 workgroups 1465 / 411 / 196 / 187; 32 of up to 2000 19.4 / 28.5 / 37 / 37).
-// And of no more than 2048 tokens while that makes no more than 2048 workgroups, so that a long request does not run on alone (64 up
-// to 8000: 108 / 96 / 100 / 113; all of 4000: 96 / 106 / 121 / 121).
-struct AttnCut {
-    AttnShape shape;
-    int groups;   // workgroups for the rows of a request and head
-    int parts, chunk;
-};
-AttnCut cut(int cols, int n_req, int heads, int group, int max_new, int max_len) {
-    AttnCut c;
-    const int64_t rows = (int64_t)max_new * group, pairs = (int64_t)n_req * heads, by_rows = 64 * attn_rows_tiles(cols);
-    c.shape = pairs * ((rows + by_rows - 1) / by_rows) >= 1000 && rows > 16 ? kAttnRows : kAttnTokens;
-    const int64_t per = c.shape == kAttnRows ? by_rows : 16, groups = (rows + per - 1) / per;
-    c.groups = (int)(groups > 4096 ? 4096 : groups);   // (they take rows in turn)
-    const int64_t whole = pairs * c.groups;
-    int64_t parts = 1;
-    if (c.shape == kAttnTokens) {
-        auto limited = [](int64_t x, int64_t most) { return x < most ? x : most; };
-        if (cols <= 128 && max_len > 256 && (max_len <= 512 || (whole > 128 && whole <= 256 && max_len <= 4096))) {
-            c.shape = kAttnTokens8;
-        } else {
-            const int64_t least = max_len > 16384 ? 512 : 256;
-            const int64_t fill = limited((512 + whole / 2) / whole, (max_len + least - 1) / least), even = limited(2048 / whole, max_len / 2048);
-            parts = fill > even ? fill : even;
-            if (parts < 1) parts = 1;
-        }
-    }
-    c.chunk = (int)((((int64_t)max_len + parts - 1) / parts + 255) / 256 * 256);
-    c.parts = (int)(((int64_t)max_len + c.chunk - 1) / c.chunk);
-    return c;
-}
-size_t part_bytes(int64_t rows, int cols) { return (size_t)rows * ((size_t)cols + 2) * sizeof(float); }
-
 __global__ __launch_bounds__(256) void kv_clear_flags_kernel(int32_t* flags, int n) {
     const int i = blockIdx.x * 256 + threadIdx.x;
     if (i < n) flags[i] = 0;
@@ -71,9 +23,7 @@ extern "C" {
 
 size_t abft_kv_attention_workspace_bytes(const abft_kv_cache_t* cache, int n_req, int q_heads, int max_new, int max_len) {
     if (abft::kv_wrong_sizes(cache) || n_req < 1 || q_heads < 1 || q_heads % cache->heads != 0 || max_new < 1 || max_len < 1 || max_len > 0x7ffffe00) return 0;
-    const int cols = abft::kv_columns(cache->head_dim);
-    const abft::AttnCut c = abft::cut(cols, n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
-    return c.parts <= 1 ? 0 : c.parts * abft::part_bytes((int64_t)n_req * max_new * q_heads, cols);
+    return abft::attn_workspace_bytes(abft::kv_columns(cache->head_dim), n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
 }
 
 int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_token_stride, int64_t q_head_stride, int type,
@@ -104,8 +54,8 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
     if (n_rows > 0x7fffffffll / q_heads) return abft::set_error(ABFT_EUNSUPPORTED, "%s: n_rows=%lld too large for one launch", fn, (long long)n_rows);
 
     const int cols = abft::kv_columns(cache->head_dim);
-    abft::AttnCut c = abft::cut(cols, n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
-    const size_t each = abft::part_bytes(n_rows * q_heads, cols);
+    abft::AttnCut c = abft::attn_cut(cols, n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
+    const size_t each = abft::attn_part_bytes(n_rows * q_heads, cols);
     if (c.parts > 1 && (!workspace || workspace_bytes / each < (size_t)c.parts)) {
         const size_t fit = workspace ? workspace_bytes / each : 0;
         const int64_t parts = fit < 2 ? 1 : (int64_t)fit;

@@ -222,3 +222,39 @@ def test_checked_products_refuse_memory_that_is_not_lent_whole(b, monkeypatch):
                      lambda: b.abft_locate_correct(A, Bp, C, flags, scratch=bad)):
             with pytest.raises(error):
                 call()
+
+
+def test_a_layer_whose_single_tokens_are_cut_after_its_prompts_were_not(b):
+    """The workspace of a layer is made for its prompts; the steps of single tokens that follow are cut into parts and find room for them."""
+    from paper_2103_00130_amd import decode_step
+    rng = np.random.default_rng(21)
+    heads, group, dim, block, hidden = 8, 4, 64, 32, 64
+    rows = (heads * group + 2 * heads) * dim
+    plain, handles = [], []
+    for n, k in ((rows, hidden), (hidden, heads * group * dim)):
+        W = rng.integers(0, 256, (n, k // 2), dtype=np.uint8)
+        scale = torch.full((n, -(-k // 32)), (21.25 * k) ** -0.5)
+        handles.append(b.abft_w4_pack(dev(W), scale.cuda(), (scale * -7.5).cuda(), K=k, group=32))
+        plain.append((W, f64(scale), f64(scale * -7.5)))
+    prompts = [1100, 900, 40, 700]
+    layer = decode_step.DecodeLayer(*handles, heads * group, heads, dim, 4, 1200, sum(prompts), block, torch.float32)
+    x = torch.from_numpy(rng.standard_normal((sum(prompts), hidden)).astype(np.float32)).cuda()
+    layer.step(x, prompts)
+    assert layer.workspace is not None
+    parts = [t.cpu().numpy() for t in layer.cache.codes()]
+    scales = [t.cpu().numpy() for t in (layer.cache.k_scale, layer.cache.v_scale)]
+    for replayed in (False, True):
+        if replayed:
+            layer.record()
+        layer.workspace.fill_(float("nan"))
+        x = torch.from_numpy(rng.standard_normal((4, hidden)).astype(np.float32)).cuda()
+        y = layer.replay(x) if replayed else layer.step(x, [1] * 4)
+        assert not torch.isnan(layer.workspace).all(), "no parts were written"
+        qkv, split = f64(layer.qkv[:4]), heads * group * dim
+        slots, table = layer.slots[:4].cpu().numpy(), layer.table.cpu().numpy()
+        for i in range(2):
+            o.append(parts[i], scales[i], qkv[:, split + i * heads * dim:split + (i + 1) * heads * dim].reshape(4, heads, dim).astype(np.float32), slots)
+        mid = f64(layer.mid[:4])
+        want, tol, _, _ = o.attention(qkv[:, :split].reshape(4, heads * group, dim), *parts, *scales, table, layer.lengths, np.arange(5), dim ** -0.5, "f32")
+        within(mid, want, tol, "attention")
+        within(f64(y), *o.w4_product(mid.reshape(4, -1), *plain[1], 32, "f32"), "second projection")
