@@ -54,7 +54,9 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
     if (n_rows > 0x7fffffffll / q_heads) return abft::set_error(ABFT_EUNSUPPORTED, "%s: n_rows=%lld too large for one launch", fn, (long long)n_rows);
 
     const int cols = abft::kv_columns(cache->head_dim);
-    abft::AttnCut c = abft::attn_cut(cols, n_req, cache->heads, q_heads / cache->heads, max_new, max_len);
+    const int64_t pairs = (int64_t)n_req * cache->heads;
+    if (pairs > abft::kAttnMostWorkgroups) return abft::set_error(ABFT_EUNSUPPORTED, "%s: n_req=%d requests of %d heads are too many for one launch", fn, n_req, cache->heads);
+    abft::AttnCut c = abft::attn_cut(cols, n_req, cache->heads, q_heads / cache->heads, (int)abft::attn_at_most(max_new, n_rows), max_len);
     const size_t each = abft::attn_part_bytes(n_rows * q_heads, cols);
     if (c.parts > 1 && (!workspace || workspace_bytes / each < (size_t)c.parts)) {
         const size_t fit = workspace ? workspace_bytes / each : 0;
@@ -62,8 +64,7 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
         c.chunk = (int)((((int64_t)max_len + parts - 1) / parts + 255) / 256 * 256);
         c.parts = (int)(((int64_t)max_len + c.chunk - 1) / c.chunk);
     }
-    const int64_t pairs = (int64_t)n_req * cache->heads, workgroups = pairs * c.groups * c.parts;
-    if (workgroups > 0xffffff) return abft::set_error(ABFT_EUNSUPPORTED, "%s: n_req=%d requests of %d heads and %d new tokens are too many for one launch", fn, n_req, cache->heads, max_new);
+    const int64_t workgroups = pairs * c.groups * c.parts;
     abft::AttnParams p;
     p.k_codes = cache->k_codes;
     p.v_codes = cache->v_codes;

@@ -48,12 +48,13 @@ inline int64_t attn_parts(int64_t whole, int max_len) {
     return parts < 1 ? 1 : parts;
 }
 constexpr int64_t kAttnCutWholes = 1024;   // more workgroups than this have one part
+constexpr int64_t kAttnMostWorkgroups = 0xffffff;   // of a launch; requests times heads are no more
 inline AttnCut attn_cut(int cols, int n_req, int heads, int group, int max_new, int max_len) {
     AttnCut c;
     const int64_t rows = (int64_t)max_new * group, pairs = (int64_t)n_req * heads, by_rows = 64 * attn_rows_tiles(cols);
     c.shape = pairs * ((rows + by_rows - 1) / by_rows) >= 1000 && rows > 16 ? kAttnRows : kAttnTokens;
     const int64_t per = c.shape == kAttnRows ? by_rows : 16, groups = (rows + per - 1) / per;
-    c.groups = (int)attn_at_most(groups, 4096);   // (they take rows in turn)
+    c.groups = (int)attn_at_most(attn_at_most(groups, 4096), kAttnMostWorkgroups / pairs);   // (they take rows in turn)
     const int64_t whole = pairs * c.groups;
     if (c.shape == kAttnTokens && attn_eight(cols, whole, max_len)) c.shape = kAttnTokens8;
     const int64_t parts = c.shape == kAttnTokens ? attn_parts(whole, max_len) : 1;

@@ -81,6 +81,16 @@ def test_every_cut_holds_all_rows_and_tokens(cut):
         assert kernel != TOKENS8 or cols <= 128
 
 
+def test_no_estimate_makes_a_launch_too_large(cut):
+    rng = random.Random(3)
+    for _ in range(20000):
+        cols, n, heads = rng.choice((64, 128, 192, 256)), log(rng, 65535), log(rng, 65535)
+        if n * heads > 0xffffff:
+            continue
+        kernel, groups, parts, chunk = cut(cols, n, heads, log(rng, 128), log(rng, 2 ** 31 - 1), log(rng, 2 ** 31 - 512))
+        assert groups >= 1 and n * heads * groups * parts <= 0xffffff
+
+
 def log(rng, most):
     return max(1, min(most, int(most ** rng.random())))
 

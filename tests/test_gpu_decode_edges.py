@@ -258,3 +258,28 @@ def test_a_layer_whose_single_tokens_are_cut_after_its_prompts_were_not(b):
         want, tol, _, _ = o.attention(qkv[:, :split].reshape(4, heads * group, dim), *parts, *scales, table, layer.lengths, np.arange(5), dim ** -0.5, "f32")
         within(mid, want, tol, "attention")
         within(f64(y), *o.w4_product(mid.reshape(4, -1), *plain[1], 32, "f32"), "second projection")
+
+
+@pytest.mark.parametrize("requests,heads,group,estimate", [(3, 2, 4, 1), (3, 2, 4, 2 ** 31 - 1), (25, 40, 1, 17), (25, 40, 1, 2 ** 31 - 1), (300, 250, 1, 2 ** 20)])
+def test_attention_with_any_estimate_of_new_tokens(b, requests, heads, group, estimate):
+    """max_new is an estimate: with one that is far too small rows are taken in turn, one that is far too large is no reason to refuse."""
+    rng = np.random.default_rng(requests)
+    dim, block, length, new = 16, 16, 90 if requests < 300 else 5, 80 if requests < 300 else 1
+    n = -(-length // block)
+    n_blocks = 3 * n
+    k, v = (rng.integers(-127, 128, (n_blocks, heads, block, dim)).astype(np.int8) for _ in range(2))
+    ks, vs = ((rng.random((n_blocks, heads)) * 0.03 + 0.01).astype(np.float32) for _ in range(2))
+    c = b.KvCache(n_blocks, heads, dim, block)
+    c.load_codes(dev(k), dev(v), dev(ks), dev(vs))
+    some = min(requests, 3)     # (requests share blocks, and those past the third have one new token: the oracle takes its time)
+    table = np.stack([np.arange(n) + n * (r % some) for r in range(requests)]).astype(np.int32)
+    fresh = np.array([new if r < some else 1 for r in range(requests)])
+    cu = np.concatenate([[0], np.cumsum(fresh)]).astype(np.int32)
+    q = torch.from_numpy(rng.standard_normal((int(cu[-1]), heads * group, dim)).astype(np.float32)).to(torch.bfloat16).cuda()
+    out = torch.full_like(q, 9.0)
+    b.abft_kv_attention(c, q, dev(table), dev(np.full(requests, length, np.int32)), dev(cu), out, estimate, length,
+                        workspace=b.KvWorkspace(c, requests, heads * group, estimate, length).tensor)
+    last = min(requests, 6)
+    rows = int(cu[last])
+    want, tol, _, _ = o.attention(f64(q[:rows]), k, v, ks, vs, table[:last], [length] * last, cu[:last + 1], dim ** -0.5, "bf16")
+    within(f64(out[:rows]), want, tol, f"{requests} requests, max_new {estimate}")
