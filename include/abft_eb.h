@@ -165,6 +165,7 @@ size_t abft_kv_code_bytes(const abft_kv_cache_t* cache);
  *                its seq_len is ctx_len; its rows stay counted in cu_new.  Requests behind one that found no
  *                free blocks are refused too if they need any.
  *   taken        int32 [1]: blocks taken; the caller drops them from free_blocks
+ * ctx_len, new_len and free_blocks do not overlap what is written: seq_len goes back to ctx_len by a copy behind the call.
  * Calling it again with the same lengths and free blocks gives the same again.  n_req 0..16384,
  * n_slots below 2^31; block_tokens 1 or more. */
 int abft_kv_plan(const int32_t* ctx_len, const int32_t* new_len, int n_req, int block_tokens, int32_t* table, int64_t ldt, int width,

@@ -83,6 +83,15 @@ __device__ inline int first_above(const uint32_t* sums, int n, uint32_t v) {
     return lo;
 }
 
+struct Range {
+    uintptr_t at, bytes;
+    bool overlaps(const Range& o) const { return bytes > 0 && o.bytes > 0 && at < o.at + o.bytes && o.at < at + bytes; }
+};
+template <typename T>
+Range range(const T* p, int64_t n) {
+    return {reinterpret_cast<uintptr_t>(p), p ? (uintptr_t)n * sizeof(T) : 0};
+}
+
 // NT threads, each of which takes up to PER neighbouring requests.
 template <int NT, int PER>
 __global__ __launch_bounds__(NT) void kv_plan_kernel(const PlanParams p) {
@@ -197,6 +206,13 @@ extern "C" int abft_kv_plan(const int32_t* ctx_len, const int32_t* new_len, int 
     if (ldt < width) return abft::set_error(ABFT_EINVAL, "%s: ldt=%lld smaller than width=%d", fn, (long long)ldt, width);
     if (n_req > abft::kMaxRequests) return abft::set_error(ABFT_EUNSUPPORTED, "%s: n_req=%d (at most %d)", fn, n_req, abft::kMaxRequests);
     if (n_slots >= 0x7fffffffll) return abft::set_error(ABFT_EUNSUPPORTED, "%s: n_slots=%lld too large", fn, (long long)n_slots);
+    // (every workgroup reads all lengths while others write: an update in place would come out in parts)
+    const abft::Range inputs[] = {abft::range(ctx_len, n_req), abft::range(new_len, n_req), abft::range(free_blocks, n_free)};
+    const abft::Range outputs[] = {abft::range(seq_len, n_req), abft::range(cu_new, (int64_t)n_req + 1), abft::range(req_flags, n_req), abft::range(taken, 1),
+                                   abft::range(slots, n_slots), abft::range(table, n_req > 0 ? (n_req - 1) * ldt + width : 0)};
+    for (const abft::Range& in : inputs)
+        for (const abft::Range& out : outputs)
+            if (in.overlaps(out)) return abft::set_error(ABFT_EINVAL, "%s: the lengths or free blocks overlap what is written", fn);
     abft::PlanParams p{ctx_len, new_len, free_blocks, table, seq_len, cu_new, slots, req_flags, taken, ldt, n_slots, ~0ull / (uint64_t)block_tokens + 1, n_req, block_tokens, -1, width, n_free};
     for (int k = 0; k < 31; ++k)
         if (block_tokens == 1 << k) p.shift = k;

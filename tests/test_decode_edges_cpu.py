@@ -115,3 +115,17 @@ def test_a_workspace_serves_all_smaller_calls(b, cut):
             assert parts == 1 or parts * small[0] * small[1] * heads * group * (cols + 2) * 4 <= most, (cols, n, heads, group, fresh, length, small)
             cut_ones += parts > 1
     assert cut_ones > 1000
+
+
+def test_a_plan_in_place_is_refused(b):
+    """Lengths and free blocks that overlap anything that the plan writes."""
+    at = {name: 0x100000 * (i + 1) for i, name in enumerate(("ctx", "new", "table", "free", "seq", "cu", "slots", "flags", "taken"))}
+
+    def call(**kw):
+        p = {k: ctypes.c_void_p(v) for k, v in (at | kw).items()}
+        return b.lib.abft_kv_plan(p["ctx"], p["new"], 4, 16, p["table"], 8, 6, p["free"], 5, p["seq"], p["cu"], p["slots"], 9, p["flags"], p["taken"], None)
+    inputs, outputs = {"ctx": 16, "new": 16, "free": 20}, {"seq": 16, "cu": 20, "slots": 72, "flags": 16, "taken": 4, "table": 4 * (3 * 8 + 6)}
+    for i, n in inputs.items():
+        for out, m in outputs.items():
+            for where in (at[i], at[i] + n - 4, at[i] - m + 4):
+                assert call(**{out: where}) == b.ABFT_EINVAL and b"overlap" in b.lib.abft_last_error(), (i, out)
