@@ -35,7 +35,8 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
     if (!abft::known_type(type)) return abft::set_error(ABFT_EINVAL, "%s: unknown type %d", fn, type);
     if (n_rows < 0 || n_req < 0 || width < 0) return abft::set_error(ABFT_EINVAL, "%s: negative count", fn);
     if (q_heads < 1 || q_heads % cache->heads != 0) return abft::set_error(ABFT_EINVAL, "%s: q_heads=%d must be a multiple of the cache's %d heads", fn, q_heads, cache->heads);
-    if (!std::isfinite(scale)) return abft::set_error(ABFT_EINVAL, "%s: scale must be finite", fn);
+    const float scale2 = scale * 1.44269504f;
+    if (!std::isfinite(scale2)) return abft::set_error(ABFT_EINVAL, "%s: scale must be finite, as must be scale * log2(e)", fn);
     if (n_req == 0) return ABFT_OK;
     hipStream_t s = (hipStream_t)stream;
     if (n_rows == 0) {   // nothing to do but to overwrite the flags
@@ -97,7 +98,7 @@ int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_tok
     p.parts = c.parts;
     p.stride = (int)(pairs * 382 / 1000 / 8 * 8 + 1);   // (far, by no simple fraction, and on to the next eighth of the chip)
     p.chunk = c.chunk;
-    p.scale2 = scale * 1.44269504f;
+    p.scale2 = scale2;
     p.q_wide = ((reinterpret_cast<uintptr_t>(Q) | (uintptr_t)(q_token_stride * (int64_t)es) | (uintptr_t)(q_head_stride * (int64_t)es) | (uintptr_t)(cache->head_dim * (int64_t)es)) & (4 * es - 1)) == 0;
     hipError_t e = abft::clear_flags(req_flags, n_req, s);
     const bool small_blocks = cache->block_tokens < abft::kKvTile;

@@ -129,3 +129,11 @@ def test_a_plan_in_place_is_refused(b):
         for out, m in outputs.items():
             for where in (at[i], at[i] + n - 4, at[i] - m + 4):
                 assert call(**{out: where}) == b.ABFT_EINVAL and b"overlap" in b.lib.abft_last_error(), (i, out)
+
+
+def test_attention_refuses_a_scale_that_overflows_in_base_two(b):
+    at = ctypes.c_void_p(0x1000)
+    c = b.abft_kv_cache_t(0x1000, 0x1000, 0x1000, 0x1000, 4, 2, 64, 16)
+    for scale in (2.4e38, -3.4e38):
+        assert b.lib.abft_kv_attention(ctypes.byref(c), at, 256, 64, 2, 3, 4, at, 8, 8, at, at, 3, 1, 100, scale, at, 256, 64, None, None, None, 0, None) == b.ABFT_EINVAL
+        assert b"scale" in b.lib.abft_last_error()
