@@ -62,6 +62,13 @@ class DecodeLayer:
             self.lengths[r] += m
         return first
 
+    def _check_rows(self, x, rows):
+        # (before anything is counted: a step that is refused leaves the layer as it was)
+        if tuple(x.shape) != (rows, self.wqkv.K) or (x.shape[1] > 1 and x.stride(1) != 1):
+            raise ValueError(f"x is {tuple(x.shape)}, a step of {rows} new tokens takes {rows} x {self.wqkv.K} with unit column stride")
+        if not x.is_cuda or x.dtype != self.qkv.dtype:
+            raise TypeError(f"x must be {self.qkv.dtype} on the device")
+
     def _launch(self, x, new, free, y, max_new, max_len):
         rows, split = x.shape[0], self.q_heads * self.head_dim
         b.abft_kv_plan(self.ctx, new, self.block, self.table, free, self.seq, self.cu, self.slots[:rows], self.flags, self.taken)
@@ -77,8 +84,7 @@ class DecodeLayer:
 
     def step(self, x, new):
         """x: a row for each new token, those of request 0 first; new: how many each request has (a list).  Returns the rows' output."""
-        if x.shape[0] != sum(new):
-            raise ValueError(f"{x.shape[0]} rows for {sum(new)} new tokens")
+        self._check_rows(x, sum(new))
         first = self._take(new)
         y = torch.empty((x.shape[0], self.wo.N), dtype=x.dtype, device=x.device)
         if x.shape[0]:
@@ -97,6 +103,10 @@ class DecodeLayer:
 
     def replay(self, x):
         """The step of one token for each request, as `record` recorded it; the output is overwritten by the next replay."""
+        if self.graph is None:
+            raise RuntimeError("nothing is recorded")
+        if tuple(x.shape) != self.x1.shape:
+            raise ValueError(f"x is {tuple(x.shape)}, a replay takes {tuple(self.x1.shape)}")
         first = self._take([1] * self.requests)
         self.x1.copy_(x)
         self.free1.copy_(self.pool[first:first + self.requests])

@@ -283,3 +283,23 @@ def test_attention_with_any_estimate_of_new_tokens(b, requests, heads, group, es
     rows = int(cu[last])
     want, tol, _, _ = o.attention(f64(q[:rows]), k, v, ks, vs, table[:last], [length] * last, cu[:last + 1], dim ** -0.5, "bf16")
     within(f64(out[:rows]), want, tol, f"{requests} requests, max_new {estimate}")
+
+
+def test_a_step_that_is_refused_leaves_the_layer_as_it_was(b):
+    from paper_2103_00130_amd import decode_step
+    g = torch.Generator("cuda").manual_seed(1)
+    handles = [decode_step.random_weight(n, 64, 32, torch.float32, g) for n in (192, 64)]
+    layer = decode_step.DecodeLayer(*handles, 1, 1, 64, 2, 30, 20, 16, torch.float32)
+    x = torch.zeros((2, 64), device="cuda")
+    with pytest.raises(RuntimeError):
+        layer.replay(x)
+    layer.record()
+    for bad, error in ((x.half(), TypeError), (x.cpu(), TypeError), (x[:, :63], ValueError), (x[:1], ValueError), (torch.zeros((64, 2), device="cuda").t(), ValueError)):
+        with pytest.raises(error):
+            layer.step(bad, [1, 1])
+    for bad in (x[:1], x[:, :63]):
+        with pytest.raises(ValueError):
+            layer.replay(bad)
+    assert layer.lengths == [0, 0] and layer.used == 0 and not layer.ctx.any()
+    layer.step(x, [1, 1])
+    assert layer.lengths == [1, 1] and layer.used == 2 and layer.ctx.tolist() == [1, 1]
