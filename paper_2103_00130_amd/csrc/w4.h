@@ -22,6 +22,7 @@
 #include "../../include/abft_gemm.h"
 #include "abft_internal.h"
 #include "values.h"
+#include "w4_shape.h"
 
 namespace abft {
 
@@ -274,12 +275,6 @@ __global__ __launch_bounds__(NW * 64) void w4_gemv_kernel(const W4Params p) {
         if (m < p.M && n < p.N) static_cast<T*>(p.Y)[(int64_t)m * p.ldy + n] = from_f32<T>(y);
     }
 }
-
-struct W4Shape {
-    int tiles, waves;   // NT, NW
-};
-// The most tiles of a wavefront that fit its registers.
-constexpr int w4_most_tiles(bool f32, int group, int ct) { return ct == 2 || (f32 && group == 32) ? 2 : 4; }
 
 template <typename T, bool WIDE, bool BIAS, int GROUP, int CT, int RI>
 hipError_t launch_w4_shape(W4Shape shape, const W4Params& p, hipStream_t s) {

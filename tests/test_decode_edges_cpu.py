@@ -137,3 +137,30 @@ def test_attention_refuses_a_scale_that_overflows_in_base_two(b):
     for scale in (2.4e38, -3.4e38):
         assert b.lib.abft_kv_attention(ctypes.byref(c), at, 256, 64, 2, 3, 4, at, 8, 8, at, at, 3, 1, 100, scale, at, 256, 64, None, None, None, 0, None) == b.ABFT_EINVAL
         assert b"scale" in b.lib.abft_last_error()
+
+
+# ------------------------------------------------------------------------------------- how 4-bit products are cut (csrc/w4_shape.h)
+@pytest.fixture(scope="module")
+def shape(tmp_path_factory):
+    """(rows, tiles of the weight, chunks of K) -> (tiles of a workgroup, its wavefronts)"""
+    lib = str(tmp_path_factory.mktemp("shape") / "shape.so")
+    src = ('#include "w4_shape.h"\nextern "C" void shape(int M, long long tiles, int chunks, int* out) {\n'
+           '    const abft::W4Shape s = abft::w4_shape(M, tiles, chunks);\n    out[0] = s.tiles; out[1] = s.waves;\n}\n')
+    subprocess.run([os.environ.get("CXX", "g++"), "-std=c++17", "-Wall", "-Werror", "-shared", "-fPIC", f"-I{CSRC}", "-x", "c++", "-", "-o", lib],
+                   input=src, text=True, check=True)
+    so = ctypes.CDLL(lib)
+
+    def call(M, N, K):
+        out = (ctypes.c_int * 2)()
+        so.shape(M, ctypes.c_longlong(-(-N // 16)), -(-K // 128), out)
+        return tuple(out)
+    return call
+
+
+# the sizes that the rule's comment has figures of, and those on either side of where it changes
+@pytest.mark.parametrize("sizes,want", [
+    ((1, 4096, 4096), (1, 8)), ((16, 4096, 4096), (1, 8)), ((16, 8192, 8192), (2, 8)), ((16, 16384, 4096), (4, 8)), ((32, 16384, 4096), (4, 8)),
+    ((1, 16384, 4096), (2, 8)), ((1, 4096, 16384), (1, 16)), ((4, 16384, 100), (2, 8)), ((5, 16384, 100), (4, 8)), ((1, 4096, 8064), (1, 8)),
+    ((1, 4096, 8065), (1, 16)), ((1, 4097, 16384), (2, 8)), ((33, 2048, 100), (1, 8)), ((33, 2049, 100), (2, 8)), ((33, 4097, 100), (4, 8))])
+def test_how_products_are_cut(shape, sizes, want):
+    assert shape(*sizes) == want

@@ -303,3 +303,25 @@ def test_a_step_that_is_refused_leaves_the_layer_as_it_was(b):
     assert layer.lengths == [0, 0] and layer.used == 0 and not layer.ctx.any()
     layer.step(x, [1, 1])
     assert layer.lengths == [1, 1] and layer.used == 2 and layer.ctx.tolist() == [1, 1]
+
+
+# ----------------------------------------------------------------------------------------------------------- 4-bit weights
+@pytest.mark.parametrize("dtype,scale_dtype", [("bf16", "bf16"), ("f16", "f16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "f16"), ("f16", "bf16")])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_products_of_wide_and_of_long_weights(b, dtype, scale_dtype, group):
+    """Sizes on both sides of every change of the cut: several tiles of the weight to a workgroup, the last one with fewer; sixteen wavefronts; many rows."""
+    sizes = [(1, 4100, 100), (4, 4161, 131), (5, 4100, 257), (16, 4113, 1300), (17, 4100, 129), (33, 4099, 65), (1, 8300, 33), (5, 8300, 300), (16, 8241, 129),
+             (33, 2050, 130), (1, 40, 8065), (4, 17, 8200), (5, 33, 8191), (16, 16, 8320), (20, 16, 8200), (200, 50, 300), (513, 17, 260)]
+    for case, (M, N, K) in enumerate(sizes):
+        rng = np.random.default_rng(1000 * group + case)
+        G = -(-K // group)
+        W = rng.integers(0, 256, (N, (K + 1) // 2), dtype=np.uint8)
+        scale = torch.from_numpy((np.exp(rng.standard_normal((N, G)) * 0.5) * 0.05).astype(np.float32)).to(TYPES[scale_dtype])
+        shift = torch.from_numpy((rng.standard_normal((N, G)) * 0.5).astype(np.float32)).to(TYPES[scale_dtype]) if (case + group // 32) % 2 else None
+        x = torch.from_numpy(rng.standard_normal((M, K + 1)).astype(np.float32)).to(TYPES[dtype]).cuda()[:, case % 2:][:, :K]
+        y = torch.full((M, N + 1), 7.0, dtype=TYPES[dtype], device="cuda")
+        Wp = b.abft_w4_pack(dev(W), scale.cuda(), None if shift is None else shift.cuda(), K=K, group=group)
+        b.abft_w4_gemv(x, Wp, y[:, :N])
+        want, tol = o.w4_product(f64(x), W, f64(scale), None if shift is None else f64(shift), group, dtype)
+        within(f64(y[:, :N]), want, tol, f"{M}x{N}x{K} group {group}")
+        assert (y[:, N:] == 7.0).all()
