@@ -325,3 +325,50 @@ def test_products_of_wide_and_of_long_weights(b, dtype, scale_dtype, group):
         want, tol = o.w4_product(f64(x), W, f64(scale), None if shift is None else f64(shift), group, dtype)
         within(f64(y[:, :N]), want, tol, f"{M}x{N}x{K} group {group}")
         assert (y[:, N:] == 7.0).all()
+
+
+# ------------------------------------------------------------------------------------------- kernels and batches of attention
+def held(b, rng, lengths, fresh, heads, group, dim, block, dtype):
+    """(cache, its parts, table, cu_new, q) of requests whose blocks lie in no order"""
+    n = [-(-int(x) // block) for x in lengths]
+    n_blocks = sum(n) + 2
+    k, v = (rng.integers(-127, 128, (n_blocks, heads, block, dim)).astype(np.int8) for _ in range(2))
+    ks, vs = ((rng.random((n_blocks, heads)) * 0.03 + 0.01).astype(np.float32) for _ in range(2))
+    c = b.KvCache(n_blocks, heads, dim, block)
+    c.load_codes(dev(k), dev(v), dev(ks), dev(vs))
+    ids, table, at = rng.permutation(n_blocks), np.full((len(lengths), max(n)), -1, np.int32), 0
+    for r, m in enumerate(n):
+        table[r, :m] = ids[at:at + m]
+        at += m
+    cu = np.concatenate([[0], np.cumsum(fresh)]).astype(np.int32)
+    q = torch.from_numpy(rng.standard_normal((int(cu[-1]), heads * group, dim)).astype(np.float32)).to(TYPES[dtype]).cuda()
+    return c, (k, v, ks, vs), table, cu, q
+
+
+@pytest.mark.parametrize("dim,block", [(64, 64), (128, 16), (90, 32)])
+def test_eight_wavefronts_in_binary16(b, dim, block):
+    rng = np.random.default_rng(dim)
+    lengths = rng.integers(1, 1000, 13)
+    lengths[3] = 1000
+    c, parts, table, cu, q = held(b, rng, lengths, [1] * 13, 10, 2, dim, block, "f16")
+    out = torch.empty_like(q)
+    b.abft_kv_attention(c, q, dev(table), dev(lengths.astype(np.int32)), dev(cu), out, 1, 1000)
+    want, tol, _, _ = o.attention(f64(q), *parts, table, lengths, cu, dim ** -0.5, "f16")
+    within(f64(out), want, tol, "eight wavefronts")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("heads,group,block", [(2, 4, 64), (40, 1, 16), (3, 7, 32)])
+def test_prompts_and_single_tokens_in_one_call(b, dtype, heads, group, block):
+    """One prompt, a part of one, a request that waits and single tokens of long and short requests."""
+    rng = np.random.default_rng(heads)
+    lengths = np.array([700, 130, 1, 0, 64, 90, 65, 333] + [40] * (18 if heads == 40 else 0))
+    fresh = np.array([1, 130, 1, 0, 1, 37, 0, 1] + [1] * (len(lengths) - 8))
+    c, parts, table, cu, q = held(b, rng, lengths, fresh, heads, group, 32, block, dtype)
+    want, tol, want_lse, lse_tol = o.attention(f64(q), *parts, table, lengths, cu, 32 ** -0.5, dtype)
+    for estimate in (130, 1):
+        out, lse = torch.full_like(q, 9.0), torch.full(q.shape[:2], 9.0, device="cuda")
+        ws = b.KvWorkspace(c, len(lengths), heads * group, 130, 700).tensor
+        b.abft_kv_attention(c, q, dev(table), dev(lengths.astype(np.int32)), dev(cu), out, estimate, 700, lse=lse, workspace=ws)
+        within(f64(out), want, tol, f"estimate {estimate}")
+        within(f64(lse), want_lse, lse_tol, f"lse, estimate {estimate}")
