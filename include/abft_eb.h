@@ -209,8 +209,13 @@ int abft_kv_read(const abft_kv_cache_t* cache, const int64_t* slots, int64_t n_t
  *              requests are cut into fewer parts
  * Q and the softmax's numerators enter the matrix cores as signed base-256 digits (two of them for 16-bit
  * types, three for binary32; numerators relative to the largest of their 64 tokens), so that the products
- * with the codes are exact; everything else is binary32, rounded once to `type`.  A row of Q that holds an infinity or
- * a NaN gives NaN.  The same bits every time. */
+ * with the codes are exact; everything else is binary32, rounded once to `type`.  What the digits leave out: of an element of Q up
+ * to 1.6e-5 (16-bit types; 1.3e-7 for binary32) of the row's largest, so that small elements beside a much larger one keep fewer bits, and
+ * a row whose largest is below 2^-100 counts as zeros; of a numerator up to 1.6e-5 (6.1e-8) of the largest of its 64 tokens - in blocks of
+ * fewer tokens each times the scale of its values - while the sum of the numerators has them whole.  A row of Q that holds an
+ * infinity or a NaN gives NaN; finite scores of any size are taken.  The same bits every time.
+ * A batch is cut by its largest request: max_new and max_len hold for all.  Beside a long prompt single tokens are cut into fewer parts, or
+ * none, than in a call of their own. */
 size_t abft_kv_attention_workspace_bytes(const abft_kv_cache_t* cache, int n_req, int q_heads, int max_new, int max_len);
 int abft_kv_attention(const abft_kv_cache_t* cache, const void* Q, int64_t q_token_stride, int64_t q_head_stride, int type,
                       int64_t n_rows, int q_heads, const int32_t* table, int64_t ldt, int width, const int32_t* seq_len,

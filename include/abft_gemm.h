@@ -382,8 +382,12 @@ void abft_w4_destroy(abft_w4* Wp);
  *       Any alignment of an element; rows of X that are multiples of 16 bytes are read faster.
  * The products are exact and are summed in binary32 (16-bit types: X enters the matrix
  * cores as it is; binary32: as three bfloat16 parts that add up to it), a group's sum is
- * scaled in binary32, and the result is rounded once, to `type`.  A row of X that holds
- * an infinity or a NaN gives NaN.  M == 0 is a valid call that does nothing.
+ * scaled in binary32, and the result is rounded once, to `type`.  A group's sum is of
+ * x * (16 + code), from which the sum of x times 16 is taken again: what cancels is some
+ * five times the result, so that for few groups the error of binary32 rows is up to some
+ * seven times that of a sum of x * W (1e-6 of the result; for long K it is no larger), and
+ * elements from 2^115 on may overflow where W would make them small.  A row of X that holds
+ * an infinity or a NaN gives no finite number.  M == 0 is a valid call that does nothing.
  * No workspace, no host synchronisation, the same bits every time. */
 int abft_w4_gemv(const void* X, int64_t ldx, int type, int M, const abft_w4* Wp, void* Y, int64_t ldy, void* stream);
 

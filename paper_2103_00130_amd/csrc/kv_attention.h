@@ -2,7 +2,7 @@
 // instantiates them.
 //
 // What bounds it: with a new token or a few for each request every code is used for a handful of products, so the time is that of
-// reading the codes; with long prompts, the vector instructions of the softmax.  Both want the codes to go from memory to the matrix
+// reading the codes; with long prompts, vector instructions, and an uneven end (figures below).  Both want the codes to go from memory to the matrix
 // cores as they are:
 //
 //  * The matrix cores multiply 8-bit integers, so Q and the softmax's numerators are brought to them instead: as signed base-256
@@ -24,13 +24,16 @@
 // neighbouring tokens, so of one block), which are then relative to the largest numerator times scale.
 //
 // The vector instructions that are left for each score: two to make it a float, one for the maximum, one multiply-add and an exp2,
-// one for the sum, 2.75 to make it digits; for each sum of values two to make it a float and one multiply-add.  The sums are
+// one for the sum, 2.75 to make it digits; for each sum of values two to make it a float and one multiply-add.  (That is 11.75 for 64
+// columns.  Counted by the chip, for 512 new of up to 4500 in blocks of 32, 12 heads of 64, f16, are 20.9, with rows made digits, masks,
+// exchanges and addresses; vector units are busy for 81 % of the time in which a compute unit has work and for half of the kernel's,
+// matrix cores for 9 %: compute units have no work for a third of it, at the ends of the longest requests.)  The sums are
 // relative to a maximum that is only moved when a row's largest score has grown by more than 2^kSlack, which spares their
 // multiplication for nearly every tile.
 //
 // Measured, bf16, 32 query heads over 8 cached ones of 128, blocks of 64: a token each for 64 requests of 4000 96 us (5.5 TB/s), of uneven
-// lengths up to 8000 98 us (4.4 TB/s: what is left of the last long ones); for one of 100 6.4 us, of 8000 12.4.  512 new tokens each for two of up to 4096 115
-// us, 330e12 operations of the definition a second (the matrix cores do twice as many: two digits).
+// lengths up to 8000 98 us (4.4 TB/s: what is left of the last long ones); for one of 100 6.5 us, of 8000 12.7.  512 new tokens each for two of up to 4096 124
+// us, 305e12 operations of the definition a second (the matrix cores do twice as many: two digits).
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -587,7 +590,11 @@ hipError_t launch_attention_cols(AttnShape shape, bool small_blocks, const AttnP
     const hipError_t e = small_blocks ? launch_attention_block<T, COLS, true>(shape, p, grid, s) : launch_attention_block<T, COLS, false>(shape, p, grid, s);
     if (e != hipSuccess || p.parts <= 1) return e;
     const int64_t rows = (p.n_rows + p.n_req - 1) / p.n_req * p.q_heads;
-    if (p.parts > 8 || (p.parts > 2 && rows * p.n_req <= 2048)) {   // many parts, few rows: the wavefronts of a workgroup share a row's
+    // Many parts, few rows: the wavefronts of a workgroup share a row's.  (us with the attention ahead, shared / not, single tokens, 32 heads over 8
+    // of 128 unless said otherwise: 61 parts, 64 heads, 4 requests up to 200000 185 / 206; 32 parts, one of 8000 11.9 / 21.6; 14 parts, 16 up to
+    // 30000 105 / 109; 4 parts, 8 up to 2000 12.7 / 14.6, one of 777 10.1 / 10.6; 3 parts, 64 up to 8000 98.6 / 98.0, 100 up to 6000 70.6 / 69.9, 16 up to
+    // 8000 with 4 new 41.3 / 41.1; 2 requests with 64 new of 8000, 16 heads 35.5 / 34.1.)
+    if (p.parts > 8 || (p.parts > 2 && rows * p.n_req <= 2048)) {
         kv_attention_join_kernel<T, COLS, true><<<dim3((unsigned)(rows < 4096 ? rows : 4096), (unsigned)p.n_req), dim3(256), 0, s>>>(p);
     } else {
         constexpr int kTake = COLS <= 64 ? 16 : COLS <= 128 ? 8 : 4;

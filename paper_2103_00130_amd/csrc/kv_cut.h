@@ -22,7 +22,10 @@ constexpr int attn_rows_tiles(int cols) { return cols <= 64 ? 2 : 1; }
 // be small, and loses where there are not (tokens / rows split; workgroups of the latter: 32 + 32 heads of 128, prompts of 2000,
 // 2048: 146 / 110; 16 + 16 of 64, 8 of 1024, 1024: 94 / 67; 32 / 8 of 128, 512 new of 4096, 512: 124 / 115; 40 / 8, 300 new of 6000,
 // 576: 176 / 326; 32 / 8, 150 new of 600, 480: 34 / 42; 12 + 12 of 64, 512 new of 4500, 192: 58 / 130, in 5 parts 66; 16 / 4, 64 new of
-// 2000, 128: 25 / 58, in 4 parts 37).
+// 2000, 128: 25 / 58, in 4 parts 37).  Between some 600 and 950 workgroups of rows split either may win, and tokens are split there: one
+// causal prompt goes faster so (16 + 16 of 128, prompts of 2500, 3000, 3600: 78 / 95, 103 / 120, 143 / 152; 32 / 8, 300 new of 3000 for 4
+// 91 / 106), many that are alike do not (32 / 8, 4 prompts of 450 107 / 47; 16 + 16 of 64, 6 of 1024 72 / 58; 12 + 12 of 64, 8 of 1000
+// 70 / 59; 40 / 8, 4 with 300 new of 6000 201 / 183).
 // Eight wavefronts for a workgroup instead of four where that spares the cut and the join: a tile for each, or as many workgroups as fit at once
 // (eight / four, 32 / 8 of 128, single tokens: 1 request of 500 8.5 / 10.6, of 1000 11.1 / 10.7, of 200 7.2 / 7.1; 8 up to 1500
 // 14.5 / 12.7; 32 up to 1000 12.7 / 15.9, up to 2000 19.4 / 22.5, up to 3000 25.5 / 27.1).

@@ -7,7 +7,9 @@
 //  * The matrix cores multiply 16 rows of the weight with up to 16 rows of X at once (16x16x32), and 16 rows of ones as well: the
 //    sums of X over a group come out in the same lanes as the products, and with them sum x*code = sum x*(16 + code) - 16 sum x and
 //    the group's bias are one fused multiply-add.  16-bit products are exact in binary32; a binary32 X enters as three bfloat16
-//    parts (truncated, so that they add up to it bit for bit).
+//    parts (truncated, so that they add up to it bit for bit).  The 16 costs accuracy that no 16-bit result shows, but a binary32 one: rms error
+//    over rms result, normal rows, against a binary32 product with the weight written out, K = 32 2.7e-7 / 0.9e-7, 128 8.6e-7 / 1.2e-7,
+//    512 6.4e-7 / 2.1e-7, 4096 6.4e-7 to 1.1e-6 / 5.6e-7.  Codes brought to the matrix cores as they are would take conversions.
 //  * A tile of 16 rows x 128 columns of codes is 1 KiB, 16 bytes a lane; a workgroup owns 16 rows of the weight, its wavefronts
 //    take chunks along K in turn and their sums meet in LDS in a fixed order.
 //
