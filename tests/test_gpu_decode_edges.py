@@ -372,3 +372,25 @@ def test_prompts_and_single_tokens_in_one_call(b, dtype, heads, group, block):
         b.abft_kv_attention(c, q, dev(table), dev(lengths.astype(np.int32)), dev(cu), out, estimate, 700, lse=lse, workspace=ws)
         within(f64(out), want, tol, f"estimate {estimate}")
         within(f64(lse), want_lse, lse_tol, f"lse, estimate {estimate}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("group", [32, 128])
+def test_products_of_large_elements(b, dtype, group):
+    """Elements just below 2^115, all of one sign, and rows with an infinity beside a weight that is positive everywhere."""
+    rng = np.random.default_rng(group)
+    M, N, K = 5, 40, 256
+    W = rng.integers(0, 256, (N, K // 2), dtype=np.uint8)
+    scale = torch.full((N, K // group), 0.01)
+    for bias in (None, torch.full((N, K // group), -0.075), torch.full((N, K // group), 0.5)):
+        Wp = b.abft_w4_pack(dev(W), scale.cuda(), None if bias is None else bias.cuda(), K=K, group=group)
+        x = torch.from_numpy((rng.uniform(1, 1.99, (M, K)) * 2.0 ** 114).astype(np.float32)).to(TYPES[dtype]).cuda()
+        y = torch.empty((M, N), dtype=TYPES[dtype], device="cuda")
+        b.abft_w4_gemv(x, Wp, y)
+        want, tol = o.w4_product(f64(x), W, f64(scale), None if bias is None else f64(bias), group, dtype)
+        within(f64(y), want, tol, "large elements")
+        x = torch.ones((M, K), dtype=TYPES[dtype], device="cuda")
+        x[1, 3], x[4, 255] = float("inf"), float("nan")
+        b.abft_w4_gemv(x, Wp, y)
+        finite = np.isfinite(f64(y)).all(1)
+        assert finite.tolist() == [True, False, True, True, False] and not np.isfinite(f64(y)[[1, 4]]).any()
