@@ -186,6 +186,27 @@ int abft_kv_plan(const int32_t* ctx_len, const int32_t* new_len, int n_req, int 
 int abft_kv_append(const abft_kv_cache_t* cache, const void* K, int64_t k_token_stride, int64_t k_head_stride, const void* V,
                    int64_t v_token_stride, int64_t v_head_stride, int type, const int64_t* slots, int64_t n_tokens, void* stream);
 
+/* The same with the rotation of a token's position applied on the way, to keys and to queries (rotary position embedding).
+ * Of a head the first rot_dim columns turn, in pairs (a, b): columns i and rot_dim / 2 + i (ABFT_ROTARY_HALVES), or 2 i and 2 i + 1
+ * (ABFT_ROTARY_NEIGHBOURS), i < rot_dim / 2:
+ *     a becomes a * cos - b * sin,   b becomes b * cos + a * sin,
+ * in binary32, the products and their sum or difference rounded one by one; the other columns stay.
+ *   Q, QR      n_tokens x q_heads x head_dim of `type`: queries, and where they go, rounded once to `type`.  QR may be Q (the
+ *              same pointer and strides), or does not overlap it.  q_heads 0: no queries, and both may be NULL
+ *   K, V, slots   as above; what a key turns into goes to its code without being rounded to `type`
+ *   positions  int32 [n_tokens]
+ *   table      float32 [n_positions][rot_dim]: for each position the cosines of the pairs, then their sines, any scaling of
+ *              frequencies and of the result being the caller's
+ *   rot_dim    even, 2..head_dim
+ * A token whose position is outside the table is left out: the cache and QR stay as they are there.  One whose slot is outside the cache has
+ * its queries turned and is not appended. */
+#define ABFT_ROTARY_HALVES 0
+#define ABFT_ROTARY_NEIGHBOURS 1
+int abft_kv_append_rotary(const abft_kv_cache_t* cache, const void* Q, int64_t q_token_stride, int64_t q_head_stride, int q_heads, void* QR,
+                          int64_t qr_token_stride, int64_t qr_head_stride, const void* K, int64_t k_token_stride, int64_t k_head_stride, const void* V,
+                          int64_t v_token_stride, int64_t v_head_stride, int type, const int64_t* slots, const int32_t* positions, int64_t n_tokens,
+                          const float* table, int64_t n_positions, int rot_dim, int pairs, void* stream);
+
 /* The tokens at `slots` as values, code * scale rounded to `type`; a slot outside the cache gives zeros.  Either of
  * K and V may be NULL.  Strides as above. */
 int abft_kv_read(const abft_kv_cache_t* cache, const int64_t* slots, int64_t n_tokens, void* K, int64_t k_token_stride,

@@ -32,7 +32,8 @@
  *     alpha_A beta_B (A_I e_k) e_n^T of Eq. 1 is not part of this library.
  *
  * At the end of this header: products with 4-bit weights for a handful of rows
- * (abft_w4_*), the weight format of a decoding step.  They carry no check.
+ * (abft_w4_*), the weight format of a decoding step, low-rank adapters beside them
+ * (abft_lora_*) and log probabilities of what they give (abft_logprobs).  They carry no check.
  */
 #ifndef ABFT_GEMM_H
 #define ABFT_GEMM_H
@@ -390,6 +391,74 @@ void abft_w4_destroy(abft_w4* Wp);
  * an infinity or a NaN gives no finite number.  M == 0 is a valid call that does nothing.
  * No workspace, no host synchronisation, the same bits every time. */
 int abft_w4_gemv(const void* X, int64_t ldx, int type, int M, const abft_w4* Wp, void* Y, int64_t ldy, void* stream);
+
+/* ------------------------------------------------------------------------- */
+/* Low-rank adapters of many requests at once, beside a projection that they share:
+ *     Y[m] = base[m] + scale[a] * up[a] (down[a] X[m]),    a = ids[m],
+ * down[a] of rank[a] x K, up[a] of N x rank[a].  Not part of the paper; no check.
+ *
+ * A pool holds up to `adapters` of them.  HOST struct; the pointers are device memory
+ * of the caller, down and up 16-byte aligned, of the sizes that abft_lora_bytes gives.
+ * What stands in a slot into which no adapter was loaded does not matter as long
+ * as no row names it. */
+typedef struct {
+    void* down;
+    void* up;
+    float* scale;      /* float32 [adapters] */
+    int32_t* rank;     /* int32 [adapters] */
+    int32_t adapters;
+    int32_t max_rank;  /* 1..128; kept in sixteens */
+    int32_t K;
+    int32_t N;
+    int32_t type;      /* ABFT_TYPE_*, of the adapters and of the rows that go through them */
+} abft_lora_t;
+
+/* bytes of `down` and of `up` (host out-pointers, either may be NULL; the pointers in the pool are not looked at) */
+int abft_lora_bytes(const abft_lora_t* pool, size_t* down, size_t* up);
+
+/* Load an adapter into a slot, in stream order.
+ *   A  rank x K, lda >= K;  B  N x rank, ldb >= rank (elements of the pool's type)
+ *   rank  0..max_rank (0: the slot adds nothing; A and B may be NULL)
+ * The inputs must stay valid until the kernel has run. */
+int abft_lora_load(const abft_lora_t* pool, int slot, const void* A, int64_t lda, const void* B, int64_t ldb, int rank, float scale, void* stream);
+
+/* Y = base + the rows' adapters.
+ *   X     M x K of the pool's type, ldx >= K
+ *   ids   int32 [M]: the slot of each row's adapter, in any order; -1, or anything outside the pool: none
+ *   base  M x N, ldb >= N;  Y  M x N, ldy >= N, both of the pool's type.  Y may be base (the same pointer and leading
+ *         dimension; rows without an adapter are then left alone), or overlaps nothing
+ *   workspace  16-byte aligned, contents irrelevant: abft_lora_workspace_bytes(pool, M) bytes are enough for every
+ *         call on up to M rows.  With less, K is cut into fewer parts; at least M * (max_rank rounded up to 16) floats.
+ *         Calls that may run at the same time need workspaces of their own
+ * Any alignment of an element; rows of 16-byte pieces are faster.  Both sums are binary32 (16-bit types: products of X with
+ * `down` are exact; what is summed over K meets `up` in binary32), and base plus scale times the sum is rounded once.  A row of X with an
+ * infinity or a NaN gives no finite number if its adapter has a rank, and no other row is touched by it.
+ * M == 0 is a valid call that does nothing.  No host synchronisation; the same bits every time. */
+size_t abft_lora_workspace_bytes(const abft_lora_t* pool, int M);
+int abft_lora_gemv(const void* X, int64_t ldx, int M, const abft_lora_t* pool, const int32_t* ids, const void* base, int64_t ldb, void* Y, int64_t ldy,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------- */
+/* What rows of logits say about tokens.  With p = softmax(scale * logits[row]):
+ *   logits   n_rows x vocab of `type`, ldl >= vocab; scale > 0 (one over the temperature), scale * log2(e) finite
+ *   targets  int64 [n_rows] or NULL: a token of each row; outside 0..vocab-1: none
+ *   logprob  float32 [n_rows] or NULL: ln p[target]; 0 where there is no target
+ *   rank     int32 [n_rows] or NULL: tokens ahead of the target, those with a larger logit, or an equal one and a
+ *            lower index; -1 where there is no target
+ *   entropy  float32 [n_rows] or NULL: -sum p ln p
+ *   lse      float32 [n_rows] or NULL: the natural logarithm of the sum of exp(scale * logits)
+ *   top_logprob, top_index   float32 and int64 [n_rows][top], top 0..64 (0: both may be NULL): the most probable tokens in order, of equal
+ *            logits the lower index first; -inf and -1 where there are no more (a logit of -inf is no token)
+ *   workspace  16-byte aligned, contents irrelevant: abft_logprobs_workspace_bytes(...) bytes are enough for every call on up to n_rows rows
+ *            of up to vocab tokens and up to `top` of them (0: none is needed).  NULL or a smaller one: few rows are cut into
+ *            fewer parts.  Calls that may run at the same time need workspaces of their own
+ * A row of -inf alone has logprob and lse -inf and entropy 0.  A row that holds a NaN or +inf gives NaN (logprob 0 where it has no
+ * target) and -1 in rank and top_index.  Sums are binary32; order and ranks are those of the logits themselves.
+ * n_rows == 0 is a valid call that does nothing.  No host synchronisation; the same bits every time. */
+size_t abft_logprobs_workspace_bytes(int64_t n_rows, int vocab, int top);
+int abft_logprobs(const void* logits, int64_t ldl, int type, int64_t n_rows, int vocab, float scale, const int64_t* targets, float* logprob,
+                  int32_t* rank, float* entropy, float* lse, int top, float* top_logprob, int64_t* top_index, void* workspace,
+                  size_t workspace_bytes, void* stream);
 
 /* Message for the last non-OK return on this host thread. */
 const char* abft_last_error(void);

@@ -34,18 +34,20 @@ EXPORTS = (
     "abft_recompute_flagged_rows_async",
     "abft_locate_scratch_bytes", "abft_locate_correct", "abft_calib_copy", "abft_clock_probe", "abft_mfma_peak_probe", "abft_clock_trace", "abft_last_error",
     "abft_w4_pack", "abft_w4_dims", "abft_w4_destroy", "abft_w4_gemv",
+    "abft_lora_bytes", "abft_lora_load", "abft_lora_workspace_bytes", "abft_lora_gemv", "abft_logprobs_workspace_bytes", "abft_logprobs",
 )
 ABFT_LOCATE_CLEAN, ABFT_LOCATE_CORRECTED, ABFT_LOCATE_NOT_ONE_ELEMENT = 0, 1, 2
 EXPORTS_EB = (
     "abft_eb_pack_rowsum", "abft_eb_table_dims", "abft_eb_table_get_rowsums", "abft_eb_table_flip_bit",
     "abft_eb_table_destroy", "abft_eb_u8_checked",
-    "abft_kv_code_bytes", "abft_kv_plan", "abft_kv_append", "abft_kv_read", "abft_kv_attention_workspace_bytes", "abft_kv_attention",
+    "abft_kv_code_bytes", "abft_kv_plan", "abft_kv_append", "abft_kv_append_rotary", "abft_kv_read", "abft_kv_attention_workspace_bytes", "abft_kv_attention",
 )
 ABFT_EB_CHECK, ABFT_EB_NOCHECK = 0, 1
 ABFT_EB_VARIANT_BATCH, ABFT_EB_VARIANT_GROUP = 0x100, 0x200
 ABFT_EB_ERR, ABFT_EB_BAD_INDEX = 1, 2
 ABFT_EB_PACK_COMPACT, ABFT_EB_PACK_LINE_ALIGNED, ABFT_EB_PACK_INT4 = 0, 1, 2
 ABFT_TYPE_F32, ABFT_TYPE_F16, ABFT_TYPE_BF16 = 0, 1, 2
+ABFT_ROTARY_HALVES, ABFT_ROTARY_NEIGHBOURS = 0, 1
 ABFT_KV_NO_BLOCK, ABFT_KV_TABLE_FULL, ABFT_KV_NO_ROW, ABFT_KV_BAD_LENGTH, ABFT_KV_BAD_BLOCK = 1, 2, 4, 8, 16
 
 
@@ -61,6 +63,11 @@ class abft_inject_t(ctypes.Structure):
 class abft_kv_cache_t(ctypes.Structure):
     _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("n_blocks", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block_tokens", ctypes.c_int32)]
+
+
+class abft_lora_t(ctypes.Structure):
+    _fields_ = [("down", ctypes.c_void_p), ("up", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rank", ctypes.c_void_p),
+                ("adapters", ctypes.c_int32), ("max_rank", ctypes.c_int32), ("K", ctypes.c_int32), ("N", ctypes.c_int32), ("type", ctypes.c_int32)]
 
 
 class AbftError(RuntimeError):
@@ -121,11 +128,21 @@ def _load() -> ctypes.CDLL:
     L.abft_w4_destroy.argtypes = [vp]
     L.abft_w4_destroy.restype = None
     L.abft_w4_gemv.argtypes = [vp, i64, i32, i32, vp, vp, i64, vp]
+    lora = ctypes.POINTER(abft_lora_t)
+    L.abft_lora_bytes.argtypes = [lora, ctypes.POINTER(sz), ctypes.POINTER(sz)]
+    L.abft_lora_load.argtypes = [lora, i32, vp, i64, vp, i64, i32, ctypes.c_float, vp]
+    L.abft_lora_workspace_bytes.argtypes = [lora, i32]
+    L.abft_lora_workspace_bytes.restype = sz
+    L.abft_lora_gemv.argtypes = [vp, i64, i32, lora, vp, vp, i64, vp, i64, vp, sz, vp]
+    L.abft_logprobs_workspace_bytes.argtypes = [i64, i32, i32]
+    L.abft_logprobs_workspace_bytes.restype = sz
+    L.abft_logprobs.argtypes = [vp, i64, i32, i64, i32, ctypes.c_float, vp, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
     kv = ctypes.POINTER(abft_kv_cache_t)
     L.abft_kv_code_bytes.argtypes = [kv]
     L.abft_kv_code_bytes.restype = sz
     L.abft_kv_plan.argtypes = [vp, vp, i32, i32, vp, i64, i32, vp, i32, vp, vp, vp, i64, vp, vp, vp]
     L.abft_kv_append.argtypes = [kv, vp, i64, i64, vp, i64, i64, i32, vp, i64, vp]
+    L.abft_kv_append_rotary.argtypes = [kv, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, i32, vp, vp, i64, vp, i64, i32, i32, vp]
     L.abft_kv_read.argtypes = [kv, vp, i64, vp, i64, i64, vp, i64, i64, i32, vp]
     L.abft_kv_attention_workspace_bytes.argtypes = [kv, i32, i32, i32, i32]
     L.abft_kv_attention_workspace_bytes.restype = sz
@@ -140,7 +157,8 @@ try:
 except ImportError as e:
     raise ImportError(f"{e}: build it with `python -m paper_2103_00130_amd.build`") from e
 _fastcall.bind([ctypes.cast(f, ctypes.c_void_p).value for f in (lib.abft_gemm_u8s8s32_checked, lib.abft_eb_u8_checked, lib.abft_w4_gemv, lib.abft_kv_plan,
-                                                                 lib.abft_kv_append, lib.abft_kv_read, lib.abft_kv_attention)],
+                                                                 lib.abft_kv_append, lib.abft_kv_read, lib.abft_kv_attention, lib.abft_kv_append_rotary,
+                                                                 lib.abft_lora_gemv, lib.abft_logprobs)],
                torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
 
 
@@ -519,7 +537,7 @@ def abft_eb_u8_checked(Tp: EbTable, indices: torch.Tensor, offsets: torch.Tensor
 
 
 # ---------------------------------------------------------------------------------------------
-# Operators of a decoding step: 4-bit weights (abft_gemm.h), the 8-bit key/value cache (abft_eb.h)
+# Operators of a decoding step: 4-bit weights, low-rank adapters and log probabilities (abft_gemm.h), the 8-bit key/value cache (abft_eb.h)
 
 _TYPES = {torch.float32: ABFT_TYPE_F32, torch.float16: ABFT_TYPE_F16, torch.bfloat16: ABFT_TYPE_BF16}
 
@@ -608,6 +626,111 @@ def abft_w4_gemv(X: torch.Tensor, Wp: W4Weight, Y: torch.Tensor, stream=None):
     _check(lib.abft_w4_gemv(x_ptr, ldx, x_type, X.shape[0], Wp.handle, y_ptr, ldy, _stream(stream)))
 
 
+class LoraPool:
+    """The buffers of a pool of low-rank adapters (abft_lora_t), none of which adds anything until it is loaded."""
+
+    def __init__(self, adapters: int, K: int, N: int, max_rank: int, dtype=torch.bfloat16, device="cuda"):
+        if dtype not in _TYPES:
+            raise TypeError(f"adapters are float32, float16 or bfloat16, not {dtype}")
+        self.adapters, self.K, self.N, self.max_rank, self.dtype = int(adapters), int(K), int(N), int(max_rank), dtype
+        sizes = (self.adapters, self.max_rank, self.K, self.N, _TYPES[dtype])
+        down, up = ctypes.c_size_t(), ctypes.c_size_t()
+        if lib.abft_lora_bytes(ctypes.byref(abft_lora_t(None, None, None, None, *sizes)), ctypes.byref(down), ctypes.byref(up)) != ABFT_OK:
+            raise ValueError(f"no pool of {adapters} adapters of {K} to {N} columns and rank {max_rank}: {lib.abft_last_error().decode()}")
+        if torch.device(device).type != "cuda":
+            raise TypeError(f"a pool lies on a device, not on {device}: its addresses go to kernels")
+        self.down = torch.empty(down.value // dtype.itemsize, dtype=dtype, device=device)
+        self.up = torch.empty(up.value // dtype.itemsize, dtype=dtype, device=device)
+        self.scale = torch.zeros(self.adapters, dtype=torch.float32, device=device)
+        self.rank = torch.zeros(self.adapters, dtype=torch.int32, device=device)
+        self.struct = abft_lora_t(self.down.data_ptr(), self.up.data_ptr(), self.scale.data_ptr(), self.rank.data_ptr(), *sizes)
+        self.ref = ctypes.byref(self.struct)
+        self.address = ctypes.addressof(self.struct)
+
+    def load(self, slot: int, A: torch.Tensor | None, B: torch.Tensor | None, scale: float = 1.0, stream=None):
+        """abft_lora_load: A rank x K and B N x rank of the pool's type into a slot; None for both empties it."""
+        abft_lora_load(self, slot, A, B, scale, stream)
+
+
+def abft_lora_load(pool: LoraPool, slot: int, A: torch.Tensor | None, B: torch.Tensor | None, scale: float = 1.0, stream=None):
+    if (A is None) != (B is None):
+        raise ValueError("an adapter has both A and B, or neither")
+    if A is None:
+        _check(lib.abft_lora_load(pool.ref, int(slot), None, 0, None, 0, 0, float(scale), _stream(stream)))
+        return
+    lda, ldb = _ld(A, "A"), _ld(B, "B")
+    rank = A.shape[0]
+    if tuple(A.shape) != (rank, pool.K) or tuple(B.shape) != (pool.N, rank):
+        raise ValueError(f"A is {tuple(A.shape)} and B {tuple(B.shape)}, the pool takes rank x {pool.K} and {pool.N} x rank")
+    _check(lib.abft_lora_load(pool.ref, int(slot), _ptr(A, pool.dtype, "A"), lda, _ptr(B, pool.dtype, "B"), ldb, rank, float(scale), _stream(stream)))
+
+
+def abft_lora_workspace_bytes(pool: LoraPool, M: int) -> int:
+    return int(lib.abft_lora_workspace_bytes(pool.ref, int(M)))
+
+
+class LoraWorkspace:
+    """A workspace tensor for abft_lora_gemv on up to M rows."""
+
+    def __init__(self, pool: LoraPool, M: int):
+        self.tensor = torch.empty(max(1, abft_lora_workspace_bytes(pool, M) // 4), dtype=torch.float32, device=pool.down.device)
+
+
+def abft_lora_gemv(X: torch.Tensor, pool: LoraPool, ids: torch.Tensor, Y: torch.Tensor, base: torch.Tensor | None = None, workspace=None, stream=None):
+    """Y = base + the rows' adapters: X M x K, Y and base M x N of the pool's type, ids int32 [M] (-1: none).  base: Y itself unless given."""
+    if base is None:
+        base = Y
+    rc = _fastcall.lora(X, pool.address, pool.K, pool.N, pool.struct.type, ids, base, Y, workspace, stream)
+    if rc is not None:
+        if rc != ABFT_OK:
+            _check(rc)
+        return
+    ldx, ldb, ldy = _ld(X, "X"), _ld(base, "base"), _ld(Y, "Y")
+    M = X.shape[0]
+    if X.shape[1] != pool.K or tuple(Y.shape) != (M, pool.N) or tuple(base.shape) != (M, pool.N):
+        raise ValueError(f"X is {tuple(X.shape)}, base {tuple(base.shape)} and Y {tuple(Y.shape)}, the pool has K={pool.K}, N={pool.N}")
+    _check(lib.abft_lora_gemv(_ptr(X, pool.dtype, "X"), ldx, M, pool.ref, _entries(ids, torch.int32, M, "ids"), _ptr(base, pool.dtype, "base"), ldb,
+                              _ptr(Y, pool.dtype, "Y"), ldy, *_lent(workspace, "workspace"), _stream(stream)))
+
+
+def abft_logprobs_workspace_bytes(n_rows: int, vocab: int, top: int) -> int:
+    return int(lib.abft_logprobs_workspace_bytes(int(n_rows), int(vocab), int(top)))
+
+
+class LogprobsWorkspace:
+    """A workspace tensor for abft_logprobs on up to n_rows rows of up to vocab tokens and up to `top` alternatives (None where none is needed)."""
+
+    def __init__(self, n_rows: int, vocab: int, top: int, device="cuda"):
+        size = abft_logprobs_workspace_bytes(n_rows, vocab, top)
+        self.tensor = torch.empty(size // 4, dtype=torch.float32, device=device) if size else None
+
+
+def abft_logprobs(logits: torch.Tensor, targets=None, logprob=None, rank=None, entropy=None, lse=None, top_logprob=None, top_index=None,
+                  scale: float = 1.0, workspace=None, stream=None):
+    """Of each row of logits: logprob and rank of its target (int64), entropy, lse, and as many of the most probable tokens as
+    top_logprob (float32) and top_index (int64) have columns.  Results that are None are not computed."""
+    rc = _fastcall.logprobs(logits, targets, logprob, rank, entropy, lse, top_logprob, top_index, scale, workspace, stream)
+    if rc is not None:
+        if rc != ABFT_OK:
+            _check(rc)
+        return
+    ldl = _ld(logits, "logits")
+    at, kind = _typed(logits, "logits")
+    n_rows, vocab = logits.shape
+    top = 0
+    if (top_logprob is None) != (top_index is None):
+        raise ValueError("top_logprob and top_index come together")
+    if top_index is not None:
+        if top_index.dim() != 2 or top_index.shape[0] != n_rows or tuple(top_logprob.shape) != tuple(top_index.shape):
+            raise ValueError(f"top_logprob and top_index must be {n_rows} x alternatives")
+        top = top_index.shape[1]
+    each = lambda t, dtype, n, name: None if t is None else _entries(t, dtype, n, name)
+    _check(lib.abft_logprobs(at, ldl, kind, n_rows, vocab, float(scale), each(targets, torch.int64, n_rows, "targets"), each(logprob, torch.float32, n_rows, "logprob"),
+                             each(rank, torch.int32, n_rows, "rank"), each(entropy, torch.float32, n_rows, "entropy"), each(lse, torch.float32, n_rows, "lse"), top,
+                             each(top_logprob, torch.float32, n_rows * top, "top_logprob"), each(top_index, torch.int64, n_rows * top, "top_index"),
+                             *_lent(workspace, "workspace"), _stream(stream)))
+
+
 class KvCache:
     """The buffers of an 8-bit key/value cache (abft_kv_cache_t): k_codes [n_blocks][heads][block_tokens][columns], v_codes
     [n_blocks][heads][block_tokens / 16][columns][16], k_scale and v_scale [n_blocks][heads]; columns is head_dim rounded up to 64."""
@@ -684,6 +807,48 @@ def abft_kv_append(cache: KvCache, K, V, slots, stream=None):
         raise TypeError("K and V must have the same type")
     _check(lib.abft_kv_append(cache.ref, *_kv_rows(K, cache, T, "K"), *_kv_rows(V, cache, T, "V"), k_type, _entries(slots, torch.int64, T, "slots"),
                               T, _stream(stream)))
+
+
+def rotary_table(n_positions: int, rot_dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """float32 [n_positions][rot_dim]: cosines, then sines, of position * base ** (-2 i / rot_dim), whose angles are taken in 64 bits."""
+    if rot_dim < 2 or rot_dim % 2 or n_positions < 0:
+        raise ValueError(f"no table of {n_positions} positions and {rot_dim} columns: they turn in pairs")
+    i = torch.arange(0, rot_dim, 2, dtype=torch.float64, device=device)
+    angle = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * float(base) ** (-i / rot_dim)
+    return torch.cat([angle.cos(), angle.sin()], 1).float()
+
+
+def abft_kv_append_rotary(cache: KvCache, Q, K, V, slots, positions, table, QR=None, neighbours: bool = False, stream=None):
+    """Turns Q (tokens x query heads x head_dim, or None) into QR (Q itself unless given) and K by the tokens' positions (int32), rows of
+    `table` (float32, positions x columns that turn: cosines, then sines), and quantizes K and V into the cache at `slots`."""
+    if QR is None:
+        QR = Q
+    rc = _fastcall.append_rotary(cache.address, cache.heads, cache.head_dim, Q, K, V, slots, positions, table, QR, neighbours, stream)
+    if rc is not None:
+        if rc != ABFT_OK:
+            _check(rc)
+        return
+    T = slots.numel()
+    _, k_type = _typed(K, "K")
+    _, v_type = _typed(V, "V")
+    q_heads, none = 0, (None, 0, 0)
+    if Q is not None:
+        if Q.dim() != 3:
+            raise ValueError("Q must be tokens x query heads x head_dim")
+        q_heads = Q.shape[1]
+        if _typed(Q, "Q")[1] != k_type or _typed(QR, "QR")[1] != k_type:
+            raise TypeError("Q, QR, K and V must have the same type")
+    elif QR is not None:
+        raise ValueError("QR without Q")
+    if k_type != v_type:
+        raise TypeError("K and V must have the same type")
+    if table.dim() != 2:
+        raise ValueError("table must be positions x columns that turn")
+    q, r = ((none if t is None else _kv_rows(t, cache, T, name, q_heads)) for t, name in ((Q, "Q"), (QR, "QR")))
+    _check(lib.abft_kv_append_rotary(cache.ref, *q, q_heads, *r, *_kv_rows(K, cache, T, "K"), *_kv_rows(V, cache, T, "V"), k_type,
+                                     _entries(slots, torch.int64, T, "slots"), _entries(positions, torch.int32, T, "positions"), T,
+                                     _entries(table, torch.float32, 0, "table"), table.shape[0], table.shape[1],
+                                     ABFT_ROTARY_NEIGHBOURS if neighbours else ABFT_ROTARY_HALVES, _stream(stream)))
 
 
 def abft_kv_read(cache: KvCache, slots, K=None, V=None, stream=None):

@@ -1,6 +1,6 @@
 // The calls that a serving loop makes for every layer, every lookup and every decoding step, marshalled natively: the operands of
-// abft_gemm_u8s8s32_checked, abft_eb_u8_checked, abft_w4_gemv, abft_kv_plan, abft_kv_append, abft_kv_read and abft_kv_attention
-// are unpacked from torch tensors here and handed to the C ABI, whose addresses bind() receives.  What binding.py checks is checked here too, and whatever does not pass - another type, a wrong
+// abft_gemm_u8s8s32_checked, abft_eb_u8_checked, abft_w4_gemv, abft_kv_plan, abft_kv_append, abft_kv_append_rotary, abft_kv_read,
+// abft_kv_attention, abft_lora_gemv and abft_logprobs are unpacked from torch tensors here and handed to the C ABI, whose addresses bind() receives.  What binding.py checks is checked here too, and whatever does not pass - another type, a wrong
 // shape, a tensor subclass - is left to it: the function returns None, and the Python code that follows raises what it
 // always raised.  A call took 9.3-10 us of host time through ctypes, more than most of the kernels it launches run.
 // The interpreter lock is released around the library call, as ctypes does.
@@ -18,6 +18,9 @@ decltype(&abft_kv_plan) g_plan = nullptr;
 decltype(&abft_kv_append) g_append = nullptr;
 decltype(&abft_kv_read) g_read = nullptr;
 decltype(&abft_kv_attention) g_attention = nullptr;
+decltype(&abft_kv_append_rotary) g_append_rotary = nullptr;
+decltype(&abft_lora_gemv) g_lora = nullptr;
+decltype(&abft_logprobs) g_logprobs = nullptr;
 PyObject* g_current_device = nullptr;  // () -> int
 PyObject* g_raw_stream = nullptr;      // (device) -> the current stream of that device, as an integer
 PyObject* g_cuda_stream = nullptr;     // the attribute name of an explicit stream
@@ -362,6 +365,116 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
+// memory that a caller lends: a contiguous device tensor of any type, or none
+struct Lent {
+    void* at = nullptr;
+    size_t bytes = 0;
+};
+Lent lent(PyObject* o) {
+    Lent l;
+    if (o == Py_None) return l;
+    const at::Tensor& w = tensor(o);
+    if (!w.is_cuda() || !w.is_contiguous()) throw Leave{};
+    l.at = w.data_ptr();
+    l.bytes = (size_t)w.numel() * w.element_size();
+    return l;
+}
+
+// append_rotary(cache struct, heads, head_dim, Q, K, V, slots, positions, table, QR, neighbours, stream) -> return code, or None
+PyObject* append_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    int rc = 0;
+    try {
+        if (n != 12 || !g_append_rotary || !PyBool_Check(a[10])) throw Leave{};
+        const int64_t heads = integer(a[1]), dim = integer(a[2]), T = needed(a[6], at::kLong).numel();
+        const Rows k = rows(a[4], T, heads, dim), v = rows(a[5], T, heads, dim);
+        Rows q = {nullptr, 0, 0, k.type}, r = q;
+        int64_t q_heads = 0;
+        if (a[3] != Py_None) {
+            const at::Tensor& Q = tensor(a[3]);
+            if (Q.dim() != 3 || Q.size(1) > 0x7fffffff) throw Leave{};
+            q_heads = Q.size(1);
+            q = rows(a[3], T, q_heads, dim);
+            r = rows(a[9], T, q_heads, dim);
+        } else if (a[9] != Py_None) {
+            throw Leave{};
+        }
+        if (k.type != v.type || q.type != k.type || r.type != k.type) throw Leave{};
+        const at::Tensor& table = needed(a[8], at::kFloat);
+        if (table.dim() != 2 || !table.is_contiguous() || table.size(1) > 0x7fffffff) throw Leave{};
+        const int64_t* const slots = vec<int64_t>(a[6], at::kLong, T);
+        const int32_t* const positions = vec<int32_t>(a[7], at::kInt, T);
+        const abft_kv_cache_t* const cache = static_cast<const abft_kv_cache_t*>(handle(a[0]));
+        const float* const angles = ptr<float>(&table);
+        const int64_t n_positions = table.size(0), rot = table.size(1);
+        const int pairs = a[10] == Py_True ? ABFT_ROTARY_NEIGHBOURS : ABFT_ROTARY_HALVES;
+        void* const s = stream(a[11]);
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_append_rotary(cache, q.at, q.token, q.head, (int)q_heads, r.at, r.token, r.head, k.at, k.token, k.head, v.at, v.token, v.head, k.type, slots,
+                             positions, T, angles, n_positions, (int)rot, pairs, s);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    return PyLong_FromLong(rc);
+}
+
+// lora(X, pool struct, K, N, type, ids, base, Y, workspace, stream) -> return code, or None
+PyObject* lora(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    int rc = 0;
+    try {
+        if (n != 10 || !g_lora) throw Leave{};
+        const at::Tensor &X = tensor(a[0]), &base = tensor(a[6]), &Y = tensor(a[7]);
+        const int64_t K = integer(a[2]), N = integer(a[3]), type = integer(a[4]);
+        if (value_type(X) != type || value_type(base) != type || value_type(Y) != type) throw Leave{};
+        const int64_t ldx = leading(X), ldb = leading(base), ldy = leading(Y), M = X.size(0);
+        if (X.size(1) != K || base.size(0) != M || base.size(1) != N || Y.size(0) != M || Y.size(1) != N || M > 0x7fffffff) throw Leave{};
+        const int32_t* const ids = vec<int32_t>(a[5], at::kInt, M);
+        const Lent ws = lent(a[8]);
+        const abft_lora_t* const pool = static_cast<const abft_lora_t*>(handle(a[1]));
+        void* const s = stream(a[9]);
+        void *const x = X.data_ptr(), *const b = base.data_ptr(), *const y = Y.data_ptr();
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_lora(x, ldx, (int)M, pool, ids, b, ldb, y, ldy, ws.at, ws.bytes, s);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    return PyLong_FromLong(rc);
+}
+
+// logprobs(logits, targets, logprob, rank, entropy, lse, top_logprob, top_index, scale, workspace, stream) -> return code, or None
+PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    int rc = 0;
+    try {
+        if (n != 11 || !g_logprobs || !PyFloat_CheckExact(a[8]) || (a[6] == Py_None) != (a[7] == Py_None)) throw Leave{};
+        const at::Tensor& x = tensor(a[0]);
+        const int type = value_type(x);
+        const int64_t ldl = leading(x), M = x.size(0), V = x.size(1);
+        if (V > 0x7fffffff) throw Leave{};
+        int64_t top = 0;
+        if (a[7] != Py_None) {
+            const at::Tensor &value = needed(a[6], at::kFloat), &index = needed(a[7], at::kLong);
+            if (index.dim() != 2 || index.size(0) != M || value.sizes() != index.sizes() || index.size(1) > 0x7fffffff) throw Leave{};
+            top = index.size(1);
+        }
+        const auto f = [&](PyObject* o, int64_t count) { return o == Py_None ? nullptr : vec<float>(o, at::kFloat, count); };
+        const int64_t* const targets = a[1] == Py_None ? nullptr : vec<int64_t>(a[1], at::kLong, M);
+        float *const logprob = f(a[2], M), *const entropy = f(a[4], M), *const lse = f(a[5], M), *const top_logprob = f(a[6], M * top);
+        int32_t* const rank = a[3] == Py_None ? nullptr : vec<int32_t>(a[3], at::kInt, M);
+        int64_t* const top_index = a[7] == Py_None ? nullptr : vec<int64_t>(a[7], at::kLong, M * top);
+        const float scale = (float)PyFloat_AS_DOUBLE(a[8]);
+        const Lent ws = lent(a[9]);
+        void* const s = stream(a[10]);
+        void* const logits = x.data_ptr();
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_logprobs(logits, ldl, type, M, (int)V, scale, targets, logprob, rank, entropy, lse, (int)top, top_logprob, top_index, ws.at, ws.bytes, s);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    return PyLong_FromLong(rc);
+}
+
 template <typename F>
 bool address(PyObject* list, Py_ssize_t i, F* f) {
     PyObject* const o = PyList_GetItem(list, i);
@@ -371,13 +484,14 @@ bool address(PyObject* list, Py_ssize_t i, F* f) {
     return true;
 }
 
-// bind([addresses of abft_gemm_u8s8s32_checked, abft_eb_u8_checked, abft_w4_gemv, abft_kv_plan, abft_kv_append, abft_kv_read, abft_kv_attention],
-// current_device, raw_stream)
+// bind([addresses of abft_gemm_u8s8s32_checked, abft_eb_u8_checked, abft_w4_gemv, abft_kv_plan, abft_kv_append, abft_kv_read, abft_kv_attention,
+// abft_kv_append_rotary, abft_lora_gemv, abft_logprobs], current_device, raw_stream)
 PyObject* bind(PyObject*, PyObject* args) {
     PyObject *list, *device, *raw;
     if (!PyArg_ParseTuple(args, "O!OO", &PyList_Type, &list, &device, &raw)) return nullptr;
     if (!address(list, 0, &g_gemm) || !address(list, 1, &g_eb) || !address(list, 2, &g_w4) || !address(list, 3, &g_plan) ||
-        !address(list, 4, &g_append) || !address(list, 5, &g_read) || !address(list, 6, &g_attention))
+        !address(list, 4, &g_append) || !address(list, 5, &g_read) || !address(list, 6, &g_attention) ||
+        !address(list, 7, &g_append_rotary) || !address(list, 8, &g_lora) || !address(list, 9, &g_logprobs))
         return nullptr;
     Py_INCREF(device);
     Py_INCREF(raw);
@@ -395,6 +509,9 @@ PyMethodDef g_methods[] = {
     ABFT_FAST(append, "abft_kv_append"),
     ABFT_FAST(read, "abft_kv_read"),
     ABFT_FAST(attention, "abft_kv_attention"),
+    ABFT_FAST(append_rotary, "abft_kv_append_rotary"),
+    ABFT_FAST(lora, "abft_lora_gemv"),
+    ABFT_FAST(logprobs, "abft_logprobs"),
 #undef ABFT_FAST
     {"bind", bind, METH_VARARGS, "addresses of the library's functions, and where to ask for the current device and stream"},
     {nullptr, nullptr, 0, nullptr}};

@@ -11,313 +11,22 @@
 // (64 of them: 4.3 us).
 #include <hip/hip_runtime.h>
 
-#include "kv_cache.h"
-#include "values.h"
+#include "kv_append.h"
 
 namespace abft {
 namespace {
 
-typedef uint32_t v2u __attribute__((ext_vector_type(2)));
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-
-struct Side {   // keys or values
-    int8_t* codes;
-    float* scale;
-    const void* x;
-    void* out;
-    int64_t token_stride, head_stride;
-    bool wide;   // rows of x (or out) are whole pieces of 8 columns, 16-byte aligned
-};
-struct CacheParams {
-    Side side[2];
-    const int64_t* slots;
-    int64_t n_tokens, limit;   // limit: slots of the cache
-    int heads, dim, cols, block, shift;   // shift: of a slot to its block
-    int window;                // append: tokens in which a workgroup looks for the beginning of runs
-    int read_heads[2];         // read: heads of a workgroup, for keys and for values
-};
-
-constexpr int kNT = 256;
-constexpr int kMaxWindow = 16, kMaxBlock = 128;
-
-// Eight columns of a token, as they are stored.
-template <typename T>
-struct Eight {
-    static constexpr int kWords = 2 * sizeof(T);
-    uint32_t w[kWords];
-};
-// From column d on; those past the head are zero.  WIDE: rows are whole aligned pieces of 8 columns.
-template <typename T, bool WIDE>
-__device__ inline void load_eight(Eight<T>& e, const T* row, int d, int dim) {
-    constexpr int PER = 4 / sizeof(T);
-    if constexpr (WIDE) {
-#pragma unroll
-        for (int h = 0; h < Eight<T>::kWords / 4; ++h) {
-            const v4u v = reinterpret_cast<const v4u*>(row + d)[h];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e.w[4 * h + i] = v[i];
-        }
-    } else {
-#pragma unroll
-        for (int h = 0; h < Eight<T>::kWords; ++h) {
-            e.w[h] = 0;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int c = d + h * PER + i;
-                const T x = row[min(c, dim - 1)];
-                if constexpr (sizeof(T) == 4) e.w[h] = c < dim ? __builtin_bit_cast(uint32_t, x) : 0u;
-                else e.w[h] |= (c < dim ? (uint32_t)__builtin_bit_cast(uint16_t, x) : 0u) << (16 * i);
-            }
-        }
-    }
-}
-template <typename T>
-__device__ inline float value_of(const Eight<T>& e, int i) {
-    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, e.w[i]);
-    else return to_f32(__builtin_bit_cast(T, (uint16_t)(e.w[i / 2] >> (16 * (i % 2)))));
-}
-
-// rne(x * inv) in the low byte of what comes back: what is added leaves a whole number, rounded to nearest even.  A finite x is no
-// larger than 127 scales (and a rounding); of others an infinity becomes 127 and a NaN 0.
-template <bool FINITE>
-__device__ inline uint32_t code_of(float x, float inv) {
-    float y = x * inv;
-    if (!FINITE) y = __builtin_amdgcn_fmed3f(y == y ? y : 0.0f, -127.0f, 127.0f);
-    return __builtin_bit_cast(uint32_t, y + 12582912.0f);
-}
-__device__ inline uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
-}
-__device__ inline uint32_t rescale_word(uint32_t w, float ratio) {
-    uint32_t r = 0;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-        const float y = __builtin_rintf((float)(int8_t)(w >> (8 * b)) * ratio);
-        r |= ((uint32_t)(int)__builtin_amdgcn_fmed3f(y, -127.0f, 127.0f) & 255u) << (8 * b);   // (a code of -128 is brought into range)
-    }
-    return r;
-}
-
-__device__ inline float wave_max(float v) {
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) v = fmaxf(v, __shfl_xor(v, m));
-    return v;
-}
-// The largest |x|, as bits that order like the numbers: two halves at a time for 16-bit types.
-template <typename T>
-__device__ inline uint32_t max_bits(uint32_t most, const Eight<T>& e) {
-    typedef uint16_t half2 __attribute__((ext_vector_type(2)));
-#pragma unroll
-    for (int h = 0; h < Eight<T>::kWords; ++h) {
-        if constexpr (sizeof(T) == 4) most = max(most, e.w[h] & 0x7fffffffu);
-        else most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(half2, most), __builtin_bit_cast(half2, e.w[h] & 0x7fff7fffu)));
-    }
-    return most;
-}
-template <typename T>
-__device__ inline float from_bits(uint32_t most) {
-    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, most);
-    else return to_f32(__builtin_bit_cast(T, (uint16_t)max(most & 0xffffu, most >> 16)));
-}
-// the largest finite one
-template <typename T>
-__device__ inline float finite_max(float peak, const Eight<T>& e) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float a = fabsf(value_of(e, i));
-        peak = a < INFINITY ? fmaxf(peak, a) : peak;
-    }
-    return peak;
-}
-// the run's scale, from the largest value and what the block had
-struct Settled {
-    float scale, inv, ratio;
-    bool grew;
-};
-__device__ inline Settled settle(float peak, float old, int first) {
-    Settled r;
-    r.scale = fmaxf(old, peak > 0.0f ? fmaxf(peak / 127.0f, 0x1p-126f) : 0.0f);
-    r.inv = r.scale > 0.0f ? 1.0f / r.scale : 0.0f;
-    r.grew = first > 0 && r.scale > old;
-    r.ratio = r.grew ? old / r.scale : 1.0f;
-    return r;
-}
-
-// Codes of U tokens of 8 columns (those that are the run's), to where they stand.
-template <typename T, bool VALUES, bool FINITE, int U>
-__device__ inline void store_unit(const CacheParams& p, const Eight<T> (&v)[U], int8_t* codes, int o, int d, int first, int n, const Settled& r) {
-    if constexpr (!VALUES) {
-#pragma unroll
-        for (int j = 0; j < U; ++j) {
-            uint32_t c[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) c[k] = code_of<FINITE>(value_of(v[j], k), r.inv);
-            if (o + j >= first && o + j < first + n)
-                *reinterpret_cast<v2u*>(codes + (o + j) * p.cols + d) = v2u{low_bytes(c[0], c[1], c[2], c[3]), low_bytes(c[4], c[5], c[6], c[7])};
-        }
-    } else {
-        typedef uint32_t words __attribute__((ext_vector_type(U / 4)));
-        const bool whole = o >= first && o + U <= first + n;
-        int8_t* const at = codes + ((int64_t)o / kKvGroup * p.cols + d) * kKvGroup + o % kKvGroup;
-        words mask;
-#pragma unroll
-        for (int q = 0; q < U / 4; ++q) {
-            mask[q] = 0;
-#pragma unroll
-            for (int j = 4 * q; j < 4 * q + 4; ++j) mask[q] |= o + j >= first && o + j < first + n ? 255u << (8 * (j % 4)) : 0u;
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            words* const to = reinterpret_cast<words*>(at + k * kKvGroup);
-            words w;
-#pragma unroll
-            for (int q = 0; q < U / 4; ++q)
-                w[q] = low_bytes(code_of<FINITE>(value_of(v[4 * q], k), r.inv), code_of<FINITE>(value_of(v[4 * q + 1], k), r.inv),
-                                 code_of<FINITE>(value_of(v[4 * q + 2], k), r.inv), code_of<FINITE>(value_of(v[4 * q + 3], k), r.inv));
-            if (!whole) {   // (what else stands there: tokens before the run, already at its scale, and what is past it, of no token)
-                const words was = *to;
-                w = (w & mask) | (was & ~mask);
-            }
-            *to = w;
-        }
-    }
-}
-
-// A run of n tokens from x on, whose slots begin at token `first` of a block, by one wavefront.  codes: of the block and head.
-// U: tokens of a lane's units where the run is no short one.
-template <typename T, bool VALUES, bool WIDE, int U>
-__device__ inline void append_run(const CacheParams& p, const T* x, int64_t stride, int8_t* codes, float* scale_at, int first, int n) {
-    const int lane = threadIdx.x & 63, pieces = (p.dim + 7) / 8, items = n * pieces;
-    const float old = first > 0 ? *scale_at : 0.0f;
-    const bool few = !WIDE || items <= 64;
-    // Few tokens (and rows that are read by elements): a lane has 8 columns of a token, as often as it takes.  Else it has units of U
-    // tokens of a group and 8 columns, mostly one.
-    const int units = p.block / U * pieces;
-    Eight<T> e, v[U];
-    // (every token of a unit is loaded, from rows that exist, so that the loads go out together)
-    auto load = [&](int o, int d) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < U; ++j) load_eight<T, WIDE>(v[j], x + (int64_t)min(max(o + j - first, 0), n - 1) * stride, d, p.dim);
-    };
-    uint32_t most = 0;
-    if (few) {
-#pragma unroll 1
-        for (int u = lane; u < items; u += 64) {
-            load_eight<T, WIDE>(e, x + (int64_t)(u / pieces) * stride, u % pieces * 8, p.dim);
-            most = max_bits(most, e);
-        }
-    } else if constexpr (WIDE) {
-#pragma unroll 1
-        for (int u = lane; u < units; u += 64) {
-            const int o = u / pieces * U, d = u % pieces * 8;
-            if (o + U <= first || o >= first + n) continue;
-            load(o, d);
-#pragma unroll
-            for (int j = 0; j < U; ++j) most = max_bits(most, v[j]);
-        }
-    }
-    // (as bits: those of an infinity or a NaN are above all others, where a maximum of floats would pass a NaN by)
-    most = __builtin_bit_cast(uint32_t, from_bits<T>(most));
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, m));
-    float peak = __builtin_bit_cast(float, most);
-    const bool finite = most < 0x7f800000u;
-    if (!finite) {
-        peak = 0.0f;
-#pragma unroll 1
-        for (int u = lane; u < items; u += 64) {
-            load_eight<T, WIDE>(e, x + (int64_t)(u / pieces) * stride, u % pieces * 8, p.dim);
-            peak = finite_max(peak, e);
-        }
-        peak = wave_max(peak);
-    }
-    const Settled r = settle(peak, old, first);
-    if (lane == 0) *scale_at = r.scale;
-    if (r.grew) {
-        // all rows of keys before the run, all groups of values that hold any: what stands past them is of no token, or the run's and
-        // written below
-        const int words = VALUES ? (first + kKvGroup - 1) / kKvGroup * p.cols : first * p.cols / 16;
-#pragma unroll 1
-        for (int u = lane; u < words; u += 64) {
-            v4u w = reinterpret_cast<v4u*>(codes)[u];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = rescale_word(w[k], r.ratio);
-            reinterpret_cast<v4u*>(codes)[u] = w;
-        }
-        // (other lanes read and write those groups: their stores are done first)
-        __builtin_amdgcn_s_waitcnt(0);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-    }
-    if (few) {
-#pragma unroll 1
-        for (int u = lane; u < items; u += 64) {
-            const int o = first + u / pieces, d = u % pieces * 8;
-            if (items > 64 || !finite) load_eight<T, WIDE>(e, x + (int64_t)(u / pieces) * stride, d, p.dim);   // (else it is there)
-            uint32_t c[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) c[k] = code_of<false>(value_of(e, k), r.inv);
-            if constexpr (!VALUES) {
-                *reinterpret_cast<v2u*>(codes + o * p.cols + d) = v2u{low_bytes(c[0], c[1], c[2], c[3]), low_bytes(c[4], c[5], c[6], c[7])};
-            } else {
-                int8_t* const at = codes + (o / kKvGroup * p.cols + d) * kKvGroup + o % kKvGroup;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) at[k * kKvGroup] = (int8_t)c[k];   // (columns are padded to 64)
-            }
-        }
-    } else if constexpr (WIDE) {
-#pragma unroll 1
-        for (int u = lane; u < units; u += 64) {
-            const int o = u / pieces * U, d = u % pieces * 8;
-            if (o + U <= first || o >= first + n) continue;
-            if (units > 64) load(o, d);   // (with one unit to a lane it is there)
-            if (finite) store_unit<T, VALUES, true, U>(p, v, codes, o, d, first, n, r);
-            else store_unit<T, VALUES, false, U>(p, v, codes, o, d, first, n, r);
-        }
-    }
-}
-
-constexpr int kAppendHeads = 2, kAppendWaves = 2 * kAppendHeads;
 template <typename T, bool WIDE, int U>
 __global__ __launch_bounds__(kAppendWaves * 64) void kv_append_kernel(const CacheParams p) {
-    __shared__ int64_t s_slot[kMaxWindow + kMaxBlock + 1];   // of the token before the window, the window, and what a run can reach
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t t0 = (int64_t)blockIdx.x * p.window;
-    const int ahead = p.window + p.block + 1;
-    for (int i = threadIdx.x; i < ahead; i += kAppendWaves * 64) {
-        const int64_t t = t0 - 1 + i;
-        const int64_t v = t >= 0 && t < p.n_tokens ? p.slots[t] : -1;
-        s_slot[i] = v >= 0 && v < p.limit ? v : -1;
-    }
-    __syncthreads();
-    // the tokens of the window that begin a run: those that do not continue the slot before them within its block
-    bool begins = false;
-    if (lane < p.window) {
-        const int64_t slot = s_slot[lane + 1];
-        begins = slot >= 0 && (((int)slot & (p.block - 1)) == 0 || s_slot[lane] != slot - 1);
-    }
-    unsigned long long left = __ballot(begins);
-    const int side = wave & 1, head = blockIdx.y * kAppendHeads + (wave >> 1);
-    if (head >= p.heads) return;
-    for (; left; left &= left - 1) {
-        const int w = __builtin_ctzll(left);
-        const int64_t slot = s_slot[w + 1], block = slot >> p.shift;
-        const int first = (int)slot & (p.block - 1);
-        // the run's length: how many slots count up from here without leaving the block
-        int n = 0;
-#pragma unroll
-        for (int h = 0; h < kMaxBlock / 64; ++h) {
-            const int j = h * 64 + lane;
-            const bool on = j < p.block - first && s_slot[w + 1 + j] == slot + j;
-            const unsigned long long b = __ballot(on);
-            if (n == h * 64) n += b == ~0ull ? 64 : __builtin_ctzll(~b);
-        }
+    __shared__ int64_t s_slot[kMaxAhead];
+    append_runs(p, s_slot, blockIdx.y, [&](int64_t t, int) { return p.slots[t]; }, [&](int side, int head, int64_t t, int, int64_t block, int first, int n) {
         const Side& s = p.side[side];
-        const T* const x = static_cast<const T*>(s.x) + (t0 + w) * s.token_stride + head * s.head_stride;
+        const Rows<T, WIDE> src = {static_cast<const T*>(s.x) + t * s.token_stride + head * s.head_stride, s.token_stride};
         int8_t* const codes = s.codes + (block * p.heads + head) * p.block * p.cols;
         float* const scale_at = s.scale + block * p.heads + head;
-        if (side == 0) append_run<T, false, WIDE, U>(p, x, s.token_stride, codes, scale_at, first, n);
-        else append_run<T, true, WIDE, U>(p, x, s.token_stride, codes, scale_at, first, n);
-    }
+        if (side == 0) append_run<Rows<T, WIDE>, false, U>(p, src, codes, scale_at, first, n);
+        else append_run<Rows<T, WIDE>, true, U>(p, src, codes, scale_at, first, n);
+    });
 }
 
 // Reading: a workgroup has 16 tokens and p.read_heads of their heads.  Of keys a thread has 8 columns of two tokens.  Of values, which
@@ -445,42 +154,10 @@ __global__ __launch_bounds__(kNT) void kv_read_kernel(const CacheParams p, int s
     }
 }
 
-bool pieces_aligned(const void* x, int64_t token_stride, int64_t head_stride, int dim, int type) {
-    const int64_t es = type_size(type);
-    return dim % 8 == 0 && ((reinterpret_cast<uintptr_t>(x) | (uintptr_t)(token_stride * es) | (uintptr_t)(head_stride * es)) & 15) == 0;
-}
-
-// what append and read have in common; 0, or an error code
-int fill(CacheParams& p, const char* fn, const abft_kv_cache_t* c, const void* K, int64_t kt, int64_t kh, const void* V, int64_t vt, int64_t vh,
-         int type, const int64_t* slots, int64_t n_tokens) {
-    if (const char* w = kv_wrong(c)) return set_error(ABFT_EINVAL, "%s: %s", fn, w);
-    if (!known_type(type)) return set_error(ABFT_EINVAL, "%s: unknown type %d", fn, type);
-    if (n_tokens < 0) return set_error(ABFT_EINVAL, "%s: n_tokens=%lld must be >= 0", fn, (long long)n_tokens);
-    if (n_tokens > 0 && !slots) return set_error(ABFT_EINVAL, "%s: null pointer", fn);
-    const uintptr_t es = (uintptr_t)type_size(type);
-    if (reinterpret_cast<uintptr_t>(K) % es || reinterpret_cast<uintptr_t>(V) % es) return set_error(ABFT_EINVAL, "%s: K or V is not aligned to its type", fn);
-    if (n_tokens > 0xffffffll) return set_error(ABFT_EUNSUPPORTED, "%s: n_tokens=%lld too large for one launch", fn, (long long)n_tokens);
-    p.side[0] = {c->k_codes, c->k_scale, K, const_cast<void*>(K), kt, kh, pieces_aligned(K, kt, kh, c->head_dim, type)};
-    p.side[1] = {c->v_codes, c->v_scale, V, const_cast<void*>(V), vt, vh, pieces_aligned(V, vt, vh, c->head_dim, type)};
-    p.slots = slots;
-    p.n_tokens = n_tokens;
-    p.limit = (int64_t)c->n_blocks * c->block_tokens;
-    p.heads = c->heads;
-    p.dim = c->head_dim;
-    p.cols = kv_columns(c->head_dim);
-    p.block = c->block_tokens;
-    p.shift = p.block == 16 ? 4 : p.block == 32 ? 5 : p.block == 64 ? 6 : 7;
-    p.window = 1;
-    return ABFT_OK;
-}
-
 template <typename T>
 void launch_append(const CacheParams& p, hipStream_t s) {
     const dim3 grid((unsigned)((p.n_tokens + p.window - 1) / p.window), (unsigned)((p.heads + kAppendHeads - 1) / kAppendHeads)), threads(kAppendWaves * 64);
-    // So few tokens to a lane's units that a block has one for every lane, if it can (us with the read behind, 16 tokens / the rule: 6000 tokens of
-    // one request, 8 heads of 128, blocks of 16 24.3 / 20.8, of 32 22.2 / 20.2; 40 requests of up to 300, 5 heads of 80, blocks of 16 15.7 / 12.8;
-    // 30 of up to 200, 8 heads of 64, binary32, blocks of 16 18.1 / 13.0).
-    const int pieces = (p.dim + 7) / 8, unit = p.block / 4 * pieces <= 64 ? 4 : p.block / 8 * pieces <= 64 ? 8 : 16;
+    const int unit = append_unit(p);
     if (!p.side[0].wide || !p.side[1].wide) kv_append_kernel<T, false, 4><<<grid, threads, 0, s>>>(p);
     else if (unit == 4) kv_append_kernel<T, true, 4><<<grid, threads, 0, s>>>(p);
     else if (unit == 8) kv_append_kernel<T, true, 8><<<grid, threads, 0, s>>>(p);
@@ -505,12 +182,7 @@ int abft_kv_append(const abft_kv_cache_t* cache, const void* K, int64_t k_token_
     if (rc != ABFT_OK) return rc;
     if (n_tokens == 0) return ABFT_OK;
     if (!K || !V) return abft::set_error(ABFT_EINVAL, "%s: null pointer", fn);
-    // A workgroup looks for runs among so many tokens: few, so that single tokens do not wait for each other, while that makes up to 2048
-    // workgroups; of more tokens most lie inside runs, and the workgroups that find none would hold up the others (us, 1 / 2 / 4 / 8 /
-    // 16 tokens: 6000 of one request 94 / 86 / 30 / 16 / 11, 64 single tokens 4.2 / 4.8 / 7.3 / 11.8 / 21, 1169 of 40 requests 8.8 / 8.2 / 8.7 /
-    // 10.6 / 12.6).
-    const int64_t all = n_tokens * ((p.heads + abft::kAppendHeads - 1) / abft::kAppendHeads);
-    while (p.window < abft::kMaxWindow && all > 2048ll * p.window) p.window *= 2;
+    p.window = abft::append_window(p);
     hipStream_t s = (hipStream_t)stream;
     if (type == ABFT_TYPE_F32) abft::launch_append<float>(p, s);
     else if (type == ABFT_TYPE_F16) abft::launch_append<abft::f16>(p, s);

@@ -1,0 +1,281 @@
+// New tokens' queries and keys rotated by their positions, keys and values quantized into the 8-bit cache on the way (abft_kv_append_rotary in
+// include/abft_eb.h).
+//
+// A pair of columns (a, b) of a head becomes (a cos - b sin, b cos + a sin), with the cosines and sines of the token's position from the
+// caller's table.  Keys and values go the way of an append (kv_append.h): a lane that loads 8 columns of a key loads the 8 that they turn with,
+// and keeps what they turn into in 32 bits until it is a code, so that a key is rounded once, to its code.  Queries are dealt to workgroups of
+// their own: a thread has 8 pairs (or 8 columns that do not turn) of up to four heads of a token, whose cosines and sines it loads once.
+#include <hip/hip_runtime.h>
+
+#include "kv_append.h"
+
+namespace abft {
+namespace {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+struct RotaryParams {
+    CacheParams cache;
+    const void* q;
+    void* qr;
+    int64_t q_token, q_head, r_token, r_head;
+    int q_heads, key_groups;      // key_groups: workgroups of a window for keys and values; those for queries follow
+    const int32_t* positions;
+    const float* table;           // [position][cosines of rot / 2 pairs, then sines]
+    int64_t n_positions;
+    int rot;
+    bool in_place;                // columns that do not turn are where they belong
+};
+
+constexpr int kQueryHeads = 4;   // of a thread
+
+// Eight columns of each of the two sides of pairs; or, of neighbours, sixteen columns.
+__device__ inline void load_angles(float (&cs)[8], float (&sn)[8], const float* angles, int half, int i) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const v4f c = *reinterpret_cast<const v4f*>(angles + i + 4 * h), s = *reinterpret_cast<const v4f*>(angles + half + i + 4 * h);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            cs[4 * h + k] = c[k];
+            sn[4 * h + k] = s[k];
+        }
+    }
+}
+
+// The keys of a run, turned.  WIDE: rows of keys are whole aligned pieces of 8 columns, and so are the columns that turn (either half of them,
+// unless neighbours turn).
+template <typename T, bool WIDE, bool NEIGHBOURS>
+struct Turned {
+    typedef float Kept;
+    static constexpr bool kWide = WIDE;
+    const T* x;
+    int64_t stride;
+    const float* table;
+    const int32_t* positions;   // of the run's tokens, in LDS
+    int rot;
+    __device__ inline void load(Eight<float>& e, int token, int d, int dim) const {
+        const T* const row = x + (int64_t)token * stride;
+        const float* const angles = table + (int64_t)positions[token] * rot;
+        const int half = rot / 2;
+        float y[8];
+        if constexpr (WIDE) {
+            Eight<T> mine;
+            load_eight<T, true>(mine, row, d, dim);
+            if (d >= rot) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) y[k] = value_of(mine, k);
+            } else if constexpr (NEIGHBOURS) {
+                const v4f c = *reinterpret_cast<const v4f*>(angles + d / 2), s = *reinterpret_cast<const v4f*>(angles + half + d / 2);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float cs = c[k], sn = s[k], a = value_of(mine, 2 * k), b = value_of(mine, 2 * k + 1);
+                    y[2 * k] = a * cs - b * sn;
+                    y[2 * k + 1] = b * cs + a * sn;
+                }
+            } else {
+                const bool front = d < half;
+                const int i = front ? d : d - half;
+                Eight<T> other;
+                load_eight<T, true>(other, row, front ? d + half : i, dim);
+                float cs[8], sn[8];
+                load_angles(cs, sn, angles, half, i);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float turn = value_of(other, k) * sn[k], stay = value_of(mine, k) * cs[k];
+                    y[k] = front ? stay - turn : stay + turn;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int c = min(d + k, dim - 1);
+                const bool turns = c < rot, front = NEIGHBOURS ? (c & 1) == 0 : c < half;
+                const int other = !turns ? c : NEIGHBOURS ? c ^ 1 : front ? c + half : c - half, i = !turns ? 0 : NEIGHBOURS ? c / 2 : front ? c : c - half;
+                const float v = to_f32(row[c]);
+                y[k] = v;
+                if (turns) {
+                    const float turn = to_f32(row[other]) * angles[half + i], stay = v * angles[i];
+                    y[k] = front ? stay - turn : stay + turn;
+                }
+                if (d + k >= dim) y[k] = 0.0f;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e.w[k] = __builtin_bit_cast(uint32_t, y[k]);
+    }
+};
+
+template <typename T>
+__device__ inline void store_eight(T* out, const float (&y)[8]) {
+    typedef T piece __attribute__((ext_vector_type(8)));
+    piece v;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = from_f32<T>(y[k]);
+    *reinterpret_cast<piece*>(out) = v;
+}
+
+// Queries of a window's tokens: an item is 8 pairs (16 columns), or 8 columns that do not turn, of up to four heads of a token; by elements (not WIDE), one
+// pair or column of a head.
+template <typename T, bool WIDE, bool NEIGHBOURS>
+__device__ inline void turn_queries(const RotaryParams& p, int group) {
+    const int half = p.rot / 2, unit = WIDE ? 8 : 1, pairs = half / unit, rest = p.in_place ? 0 : (p.cache.dim - p.rot) / unit;
+    const int pieces = pairs + rest, head_groups = WIDE ? (p.q_heads + kQueryHeads - 1) / kQueryHeads : p.q_heads;
+    const int64_t t0 = (int64_t)blockIdx.x * p.cache.window;
+    const int tokens = (int)min((int64_t)p.cache.window, p.cache.n_tokens - t0), items = tokens * head_groups * pieces, groups = gridDim.y - p.key_groups;
+    for (int u = group * kAppendWaves * 64 + threadIdx.x; u < items; u += groups * kAppendWaves * 64) {
+        const int piece = u % pieces, head0 = u / pieces % head_groups * (WIDE ? kQueryHeads : 1);
+        const int64_t t = t0 + u / pieces / head_groups;
+        const int position = p.positions[t];
+        if (position < 0 || position >= p.n_positions) continue;
+        const float* const angles = p.table + (int64_t)position * p.rot;
+        const T* const q = static_cast<const T*>(p.q) + t * p.q_token;
+        T* const r = static_cast<T*>(p.qr) + t * p.r_token;
+        if (piece < pairs) {
+            const int i = piece * unit, a0 = NEIGHBOURS ? 2 * i : i, b0 = NEIGHBOURS ? 2 * i + unit : half + i;   // (neighbours: the sixteen columns from a0 on)
+            if constexpr (WIDE) {
+                float cs[8], sn[8];
+                load_angles(cs, sn, angles, half, i);
+                Eight<T> a[kQueryHeads], b[kQueryHeads];
+#pragma unroll
+                for (int h = 0; h < kQueryHeads; ++h) {
+                    const T* const row = q + (int64_t)min(head0 + h, p.q_heads - 1) * p.q_head;
+                    load_eight<T, true>(a[h], row, a0, p.cache.dim);
+                    load_eight<T, true>(b[h], row, b0, p.cache.dim);
+                }
+#pragma unroll
+                for (int h = 0; h < kQueryHeads; ++h) {
+                    if (head0 + h >= p.q_heads) break;
+                    float y[8], z[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if constexpr (NEIGHBOURS) {
+                            const Eight<T>& e = k < 4 ? a[h] : b[h];
+                            const float u0 = value_of(e, 2 * (k % 4)), u1 = value_of(e, 2 * (k % 4) + 1), y0 = u0 * cs[k] - u1 * sn[k], y1 = u1 * cs[k] + u0 * sn[k];
+                            (k < 4 ? y : z)[2 * (k % 4)] = y0;
+                            (k < 4 ? y : z)[2 * (k % 4) + 1] = y1;
+                        } else {
+                            const float u0 = value_of(a[h], k), u1 = value_of(b[h], k);
+                            y[k] = u0 * cs[k] - u1 * sn[k];
+                            z[k] = u1 * cs[k] + u0 * sn[k];
+                        }
+                    }
+                    T* const out = r + (int64_t)(head0 + h) * p.r_head;
+                    store_eight(out + a0, y);
+                    store_eight(out + b0, z);
+                }
+            } else {
+                const float c = angles[i], s = angles[half + i], u0 = to_f32(q[head0 * p.q_head + a0]), u1 = to_f32(q[head0 * p.q_head + b0]);
+                r[head0 * p.r_head + a0] = from_f32<T>(u0 * c - u1 * s);
+                r[head0 * p.r_head + b0] = from_f32<T>(u1 * c + u0 * s);
+            }
+        } else {
+            const int d = p.rot + (piece - pairs) * unit;
+            for (int h = head0; h < min(head0 + (WIDE ? kQueryHeads : 1), p.q_heads); ++h) {
+                if constexpr (WIDE) *reinterpret_cast<Eight<T>*>(r + (int64_t)h * p.r_head + d) = *reinterpret_cast<const Eight<T>*>(q + (int64_t)h * p.q_head + d);
+                else r[h * p.r_head + d] = q[h * p.q_head + d];
+            }
+        }
+    }
+}
+
+template <typename T, bool WIDE, bool WIDE_Q, bool NEIGHBOURS, int U>
+__global__ __launch_bounds__(kAppendWaves * 64) void kv_append_rotary_kernel(const RotaryParams p) {
+    __shared__ int64_t s_slot[kMaxAhead];
+    __shared__ int32_t s_position[kMaxAhead];
+    if ((int)blockIdx.y >= p.key_groups) {
+        turn_queries<T, WIDE_Q, NEIGHBOURS>(p, blockIdx.y - p.key_groups);
+        return;
+    }
+    const CacheParams& c = p.cache;
+    append_runs(
+        c, s_slot, blockIdx.y,
+        [&](int64_t t, int i) {
+            const int position = p.positions[t];
+            s_position[i] = position;
+            return position >= 0 && position < p.n_positions ? c.slots[t] : (int64_t)-1;
+        },
+        [&](int side, int head, int64_t t, int at, int64_t block, int first, int n) {
+            const Side& s = c.side[side];
+            const T* const x = static_cast<const T*>(s.x) + t * s.token_stride + head * s.head_stride;
+            int8_t* const codes = s.codes + (block * c.heads + head) * c.block * c.cols;
+            float* const scale_at = s.scale + block * c.heads + head;
+            if (side == 0) append_run<Turned<T, WIDE, NEIGHBOURS>, false, (U < 8 ? U : 8)>(c, Turned<T, WIDE, NEIGHBOURS>{x, s.token_stride, p.table, s_position + at, p.rot}, codes, scale_at, first, n);
+            else append_run<Rows<T, WIDE>, true, U>(c, Rows<T, WIDE>{x, s.token_stride}, codes, scale_at, first, n);
+        });
+}
+
+template <typename T, bool NEIGHBOURS>
+void launch_rotary(const RotaryParams& p, bool wide, bool wide_q, int groups, hipStream_t s) {
+    const dim3 grid((unsigned)((p.cache.n_tokens + p.cache.window - 1) / p.cache.window), (unsigned)groups), threads(kAppendWaves * 64);
+    const int unit = append_unit(p.cache);
+    if (!wide && !wide_q) kv_append_rotary_kernel<T, false, false, NEIGHBOURS, 4><<<grid, threads, 0, s>>>(p);
+    else if (!wide) kv_append_rotary_kernel<T, false, true, NEIGHBOURS, 4><<<grid, threads, 0, s>>>(p);
+    else if (!wide_q) kv_append_rotary_kernel<T, true, false, NEIGHBOURS, 4><<<grid, threads, 0, s>>>(p);
+    else if (unit == 4) kv_append_rotary_kernel<T, true, true, NEIGHBOURS, 4><<<grid, threads, 0, s>>>(p);
+    else if (unit == 8) kv_append_rotary_kernel<T, true, true, NEIGHBOURS, 8><<<grid, threads, 0, s>>>(p);
+    else kv_append_rotary_kernel<T, true, true, NEIGHBOURS, 16><<<grid, threads, 0, s>>>(p);
+}
+
+}  // namespace
+}  // namespace abft
+
+extern "C" int abft_kv_append_rotary(const abft_kv_cache_t* cache, const void* Q, int64_t q_token_stride, int64_t q_head_stride, int q_heads, void* QR,
+                                     int64_t qr_token_stride, int64_t qr_head_stride, const void* K, int64_t k_token_stride, int64_t k_head_stride, const void* V,
+                                     int64_t v_token_stride, int64_t v_head_stride, int type, const int64_t* slots, const int32_t* positions, int64_t n_tokens,
+                                     const float* table, int64_t n_positions, int rot_dim, int pairs, void* stream) {
+    const char* fn = "abft_kv_append_rotary";
+    abft::RotaryParams p;
+    abft::CacheParams& c = p.cache;
+    const int rc = abft::fill(c, fn, cache, K, k_token_stride, k_head_stride, V, v_token_stride, v_head_stride, type, slots, n_tokens);
+    if (rc != ABFT_OK) return rc;
+    if (q_heads < 0) return abft::set_error(ABFT_EINVAL, "%s: q_heads=%d must be >= 0", fn, q_heads);
+    if (pairs != ABFT_ROTARY_HALVES && pairs != ABFT_ROTARY_NEIGHBOURS) return abft::set_error(ABFT_EINVAL, "%s: pairs=%d is neither halves nor neighbours", fn, pairs);
+    if (rot_dim < 2 || rot_dim % 2 || rot_dim > cache->head_dim) return abft::set_error(ABFT_EINVAL, "%s: rot_dim=%d must be even, 2 to head_dim", fn, rot_dim);
+    if (n_positions < 0) return abft::set_error(ABFT_EINVAL, "%s: n_positions=%lld must be >= 0", fn, (long long)n_positions);
+    if (n_positions > 0x7fffffffll + 1) return abft::set_error(ABFT_EUNSUPPORTED, "%s: n_positions=%lld too large", fn, (long long)n_positions);
+    if (q_heads > 65535) return abft::set_error(ABFT_EUNSUPPORTED, "%s: too many query heads", fn);
+    if (n_tokens == 0) return ABFT_OK;
+    if (!K || !V || !positions || (n_positions > 0 && !table) || (q_heads > 0 && (!Q || !QR))) return abft::set_error(ABFT_EINVAL, "%s: null pointer", fn);
+    const uintptr_t es = (uintptr_t)abft::type_size(type);
+    if (reinterpret_cast<uintptr_t>(table) & 3) return abft::set_error(ABFT_EINVAL, "%s: table is not aligned to its type", fn);
+    if (q_heads > 0 && (reinterpret_cast<uintptr_t>(Q) % es || reinterpret_cast<uintptr_t>(QR) % es)) return abft::set_error(ABFT_EINVAL, "%s: Q or QR is not aligned to its type", fn);
+    if (q_heads > 0 && Q == QR && (q_token_stride != qr_token_stride || q_head_stride != qr_head_stride))
+        return abft::set_error(ABFT_EINVAL, "%s: QR is Q, with other strides", fn);
+    p.q = Q;
+    p.qr = QR;
+    p.q_token = q_token_stride;
+    p.q_head = q_head_stride;
+    p.r_token = qr_token_stride;
+    p.r_head = qr_head_stride;
+    p.q_heads = q_heads;
+    p.positions = positions;
+    p.table = table;
+    p.n_positions = n_positions;
+    p.rot = rot_dim;
+    p.in_place = Q == QR;
+    c.window = abft::append_window(c);
+    const bool neighbours = pairs == ABFT_ROTARY_NEIGHBOURS;
+    const bool angles = (reinterpret_cast<uintptr_t>(table) & 15) == 0 && rot_dim % 8 == 0;   // pieces of four of a row's cosines and sines, aligned
+    const bool wide = c.side[0].wide && c.side[1].wide && angles && (neighbours || rot_dim % 16 == 0);
+    const bool wide_q = q_heads > 0 && abft::pieces_aligned(Q, q_token_stride, q_head_stride, c.dim, type) &&
+                        abft::pieces_aligned(QR, qr_token_stride, qr_head_stride, c.dim, type) && angles && rot_dim % 16 == 0;
+    p.key_groups = (c.heads + abft::kAppendHeads - 1) / abft::kAppendHeads;
+    // so many workgroups for the queries of a window that a thread has one item, or a few
+    const int64_t unit = wide_q ? 8 : 1, items = (int64_t)c.window * (wide_q ? (q_heads + abft::kQueryHeads - 1) / abft::kQueryHeads : q_heads) * (rot_dim / 2 / unit + (p.in_place ? 0 : (c.dim - rot_dim) / unit));
+    int64_t groups = (items + abft::kAppendWaves * 64 - 1) / (abft::kAppendWaves * 64);
+    if (groups > 32) groups = 32;
+    groups += p.key_groups;
+    if (groups > 65535) return abft::set_error(ABFT_EUNSUPPORTED, "%s: too many heads", fn);
+    hipStream_t s = (hipStream_t)stream;
+    auto launch = [&](auto one) {
+        typedef decltype(one) T;
+        if (neighbours) abft::launch_rotary<T, true>(p, wide, wide_q, (int)groups, s);
+        else abft::launch_rotary<T, false>(p, wide, wide_q, (int)groups, s);
+    };
+    if (type == ABFT_TYPE_F32) launch(0.0f);
+    else if (type == ABFT_TYPE_F16) launch((abft::f16)0.0f);
+    else launch((abft::bf16)0.0f);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return abft::set_error(ABFT_EHIP, "%s: %s", fn, hipGetErrorString(e));
+    return ABFT_OK;
+}
