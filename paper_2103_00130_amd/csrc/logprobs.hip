@@ -52,30 +52,40 @@ __device__ inline float value_of(const Piece<T>& e, int i) {
     if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, e.w[i]);
     else return to_f32(__builtin_bit_cast(T, (uint16_t)(e.w[i / 2] >> (16 * (i % 2)))));
 }
-// Logits i..i + 7 of a row, whose address is a multiple of 8 elements'; those that the row does not have are -inf.
+// A row as pieces: whole ones of eight logits that begin at multiples of 8 elements in memory, then those ahead of them and behind them, one to a piece.
+struct Pieces {
+    int head, whole, count;   // logits ahead of the whole pieces; pieces
+    __device__ inline Pieces(int offset, int vocab) {   // offset: of the row's first logit from such a multiple
+        head = min((8 - offset) & 7, vocab);
+        whole = (vocab - head) / 8;
+        count = whole + vocab - 8 * whole;
+    }
+    // where piece q begins
+    __device__ inline int index(int q) const { return q < whole ? q * 8 + head : q - whole < head ? q - whole : whole * 8 + q - whole; }
+};
 template <typename T>
-__device__ inline void load_piece(Piece<T>& e, const T* row, int64_t i, int vocab) {
-    if (i >= 0 && i + 8 <= vocab) {
+__device__ inline void load_whole(Piece<T>& e, const T* at) {
 #pragma unroll
-        for (int h = 0; h < Piece<T>::kWords / 4; ++h) {
-            const v4u v = reinterpret_cast<const v4u*>(row + i)[h];
+    for (int h = 0; h < Piece<T>::kWords / 4; ++h) {
+        const v4u v = reinterpret_cast<const v4u*>(at)[h];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) e.w[4 * h + k] = v[k];
-        }
+        for (int k = 0; k < 4; ++k) e.w[4 * h + k] = v[k];
+    }
+}
+// Piece q; logits that it does not have are -inf.
+template <typename T>
+__device__ inline void load_piece(Piece<T>& e, const T* row, const Pieces& pieces, int q, int end) {
+    if (q < min(end, pieces.whole)) {
+        load_whole(e, row + pieces.index(q));
     } else {
         constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, f16>::value ? 0xfc00u : 0xff80u;
-        uint32_t v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int64_t at = i + k;
-            v[k] = kNone;
-            if (at >= 0 && at < vocab) {
-                if constexpr (sizeof(T) == 4) v[k] = __builtin_bit_cast(uint32_t, row[at]);
-                else v[k] = __builtin_bit_cast(uint16_t, row[at]);
-            }
+        for (int h = 0; h < Piece<T>::kWords; ++h) e.w[h] = sizeof(T) == 4 ? kNone : kNone * 0x10001u;
+        if (q < end) {
+            const T x = row[pieces.index(q)];
+            if constexpr (sizeof(T) == 4) e.w[0] = __builtin_bit_cast(uint32_t, x);
+            else e.w[0] = __builtin_bit_cast(uint16_t, x) | kNone << 16;
         }
-#pragma unroll
-        for (int k = 0; k < Piece<T>::kWords; ++k) e.w[k] = sizeof(T) == 4 ? v[k] : v[2 * k % 8] | v[(2 * k + 1) % 8] << 16;
     }
 }
 
@@ -107,45 +117,75 @@ __device__ inline float value_of_key(uint64_t k) {
     return __builtin_bit_cast(float, b & 0x80000000u ? b ^ 0x80000000u : ~b);
 }
 __device__ inline uint32_t index_of_key(uint64_t k) { return ~(uint32_t)k; }
-__device__ inline uint64_t from_lane(uint64_t k, int lane) {
-    return (uint64_t)(uint32_t)__shfl((int)(k >> 32), lane) << 32 | (uint32_t)__shfl((int)k, lane);
+// The value of the lane whose number differs by D, without a trip through LDS.
+template <int CTRL>
+__device__ inline uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
+template <int D>
+__device__ inline uint32_t across(uint32_t v, int lane) {
+    if constexpr (D == 1) return dpp<0xB1>(v);            // quad_perm 1 0 3 2
+    else if constexpr (D == 2) return dpp<0x4E>(v);       // quad_perm 2 3 0 1
+    else if constexpr (D == 3) return dpp<0x1B>(v);       // quad_perm 3 2 1 0
+    else if constexpr (D == 7) return dpp<0x141>(v);      // half a row mirrored
+    else if constexpr (D == 15) return dpp<0x140>(v);     // a row mirrored
+    else if constexpr (D == 4) return dpp<0x1B>(dpp<0x141>(v));
+    else if constexpr (D == 8) return dpp<0x128>(v);      // a row turned by 8
+    else if constexpr (D == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);   // rows 0 0 2 2 and 1 1 3 3
+        return lane & 16 ? r[0] : r[1];
+    } else if constexpr (D == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return lane & 32 ? r[0] : r[1];
+    } else if constexpr (D == 31) return across<16>(dpp<0x140>(v), lane);
+    else return across<32>(across<31>(v, lane), lane);    // 63
 }
-// the larger of a pair goes to the lane that wants it
-__device__ inline uint64_t exchange(uint64_t k, int other, bool larger) {
-    const uint64_t o = from_lane(k, other);
+// The larger of a pair of lanes, of numbers that differ by D, goes to the lane that wants it.
+template <int D>
+__device__ inline uint64_t exchange(uint64_t k, int lane, bool larger) {
+    const uint64_t o = (uint64_t)across<D>((uint32_t)(k >> 32), lane) << 32 | across<D>((uint32_t)k, lane);
     return (k > o) == larger ? k : o;
 }
-// A list that rises and falls (or falls and rises) put in order.
+// A list that rises and falls (or falls and rises) within every N lanes put in order, the largest first.
+template <int N>
 __device__ inline uint64_t ordered(uint64_t k, int lane) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) k = exchange(k, lane ^ d, (lane & d) == 0);
-    return k;
+    if constexpr (N > 1) return ordered<N / 2>(exchange<N / 2>(k, lane, (lane & (N / 2)) == 0), lane);
+    else return k;
 }
+// (lists of N / 2 in order, two and two: the second of each meets the first from its end)
+template <int N = 2>
 __device__ inline uint64_t sorted(uint64_t k, int lane) {
-#pragma unroll
-    for (int n = 2; n <= 64; n *= 2) {
-#pragma unroll
-        for (int d = n / 2; d; d >>= 1) k = exchange(k, lane ^ d, ((lane & d) == 0) == ((lane & n) == 0));
-    }
-    return k;   // (with n = 64 lane & n is 0: the largest first)
+    k = ordered<N / 2>(exchange<N - 1>(k, lane, (lane & (N / 2)) == 0), lane);
+    if constexpr (N < 64) return sorted<2 * N>(k, lane);
+    else return k;
 }
 // the 64 largest of two lists
 __device__ inline uint64_t merged(uint64_t a, uint64_t b, int lane) {
-    const uint64_t r = from_lane(b, 63 - lane);
-    return ordered(a > r ? a : r, lane);
+    const uint64_t r = (uint64_t)across<63>((uint32_t)(b >> 32), lane) << 32 | across<63>((uint32_t)b, lane);
+    return ordered<64>(a > r ? a : r, lane);
+}
+__device__ inline uint64_t of_lane(uint64_t k, int lane) {   // (the same for all)
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
+}
+
+// A row's target and its logit.
+struct Target {
+    int at;     // -1: none
+    float x;
+};
+template <typename T>
+__device__ inline Target target_of(const LogprobsParams& p, int64_t row, const T* logits) {
+    const int64_t t = p.targets ? p.targets[row] : -1;
+    const bool inside = t >= 0 && t < p.vocab;
+    return {inside ? (int)t : -1, inside ? to_f32(logits[t]) : INFINITY};
 }
 
 // What a row gives, from its sums: by one wavefront, whose lanes hold the list.
-template <typename T>
-__device__ inline void finish(const LogprobsParams& p, int64_t row, const T* logits, Sums r, int ahead, uint64_t list, int lane) {
+__device__ inline void finish(const LogprobsParams& p, int64_t row, Target target, Sums r, int ahead, uint64_t list, int lane) {
     const bool bad = !(r.s == r.s), none = r.s == 0.0f;   // (a NaN or a +inf among the logits; nothing but -inf)
     const float nan = __builtin_nanf(""), ln = none ? 0.0f : logf(r.s);
     auto log_p = [&](float x) { return bad ? nan : none ? -INFINITY : (x - r.m) * p.scale - ln; };
     if (lane == 0) {
-        const int64_t t = p.targets ? p.targets[row] : -1;
-        const bool inside = t >= 0 && t < p.vocab;
-        if (p.logprob) p.logprob[row] = inside ? log_p(to_f32(logits[inside ? t : 0])) : 0.0f;
-        if (p.rank) p.rank[row] = inside && !bad ? ahead : -1;
+        if (p.logprob) p.logprob[row] = target.at >= 0 ? log_p(target.x) : 0.0f;
+        if (p.rank) p.rank[row] = target.at >= 0 && !bad ? ahead : -1;
         if (p.entropy) p.entropy[row] = bad ? nan : none ? 0.0f : __builtin_fmaf(-kLn2, r.u / r.s, ln);
         if (p.lse) p.lse[row] = bad ? nan : none ? -INFINITY : __builtin_fmaf(p.scale, r.m, ln);
     }
@@ -156,98 +196,176 @@ __device__ inline void finish(const LogprobsParams& p, int64_t row, const T* log
     }
 }
 
+// Sums and counts of all lanes.
+__device__ inline void join_lanes(Sums& r, int& ahead, float c, int lane) {
+    auto step = [&](auto d) __attribute__((always_inline)) {
+        constexpr int D = decltype(d)::value;
+        auto of = [&](float v) __attribute__((always_inline)) { return __builtin_bit_cast(float, across<D>(__builtin_bit_cast(uint32_t, v), lane)); };
+        join(r, Sums{of(r.m), of(r.s), of(r.u)}, c);
+        ahead += (int)across<D>((uint32_t)ahead, lane);
+    };
+    step(std::integral_constant<int, 1>());
+    step(std::integral_constant<int, 2>());
+    step(std::integral_constant<int, 4>());
+    step(std::integral_constant<int, 8>());
+    step(std::integral_constant<int, 16>());
+    step(std::integral_constant<int, 32>());
+}
+
+// The least of the largest of every `group` lanes (a power of two).
+__device__ inline float least_of_groups(float v, int group, int lane) {
+    auto step = [&](auto d, int size) __attribute__((always_inline)) {   // (lanes that differ by D below `size` hold the same by then)
+        const float o = __builtin_bit_cast(float, across<decltype(d)::value>(__builtin_bit_cast(uint32_t, v), lane));
+        const float most = fmaxf(v, o), least = fminf(v, o);
+        v = size < group ? most : least;
+    };
+    step(std::integral_constant<int, 1>(), 1);
+    step(std::integral_constant<int, 2>(), 2);
+    step(std::integral_constant<int, 7>(), 4);
+    step(std::integral_constant<int, 15>(), 8);
+    step(std::integral_constant<int, 16>(), 16);
+    step(std::integral_constant<int, 32>(), 32);
+    return v;
+}
+
 template <typename T, bool TOP>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobsParams p) {
     __shared__ Sums s_sums[kWaves];
     __shared__ int s_ahead[kWaves];
-    __shared__ uint64_t s_list[kWaves][128];
+    __shared__ uint64_t s_list[TOP ? kWaves : 1][128];
+    __shared__ volatile float s_bar[kWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row = blockIdx.x;
     const int part = blockIdx.y;
     const T* const logits = static_cast<const T*>(p.logits) + row * p.ldl;
     const float c = p.scale * kLog2e;
-    // pieces of eight begin at multiples of 8 elements in memory: the first may begin ahead of the row, the last end behind it
-    const int ahead0 = (int)(reinterpret_cast<uintptr_t>(logits) / sizeof(T) & 7);
-    const int pieces = (int)(((int64_t)p.vocab + ahead0 + 7) / 8), each = (pieces + p.parts - 1) / p.parts;
-    const int begin = part * each, end = min(pieces, begin + each);
+    const Pieces pieces((int)(reinterpret_cast<uintptr_t>(logits) / sizeof(T) & 7), p.vocab);
+    const int each = (pieces.count + p.parts - 1) / p.parts, begin = min(part * each, pieces.count), end = min(pieces.count, begin + each), whole = min(end, pieces.whole);
 
-    const int64_t target = p.targets ? p.targets[row] : -1;
-    const bool inside = target >= 0 && target < p.vocab;
-    // Tokens ahead of the target: those not <= `bar`, which is the target's logit behind it, and the number below it ahead of it, where
+    constexpr int kBatch = 16 / Piece<T>::kWords;
+    Piece<T> e[kBatch], next[kBatch];
+    auto load = [&](Piece<T> (&to)[kBatch], int q0) __attribute__((always_inline)) {
+        if (q0 + kBatch * kThreads <= whole) {
+            const T* const at = logits + pieces.head + (int64_t)(q0 + (int)threadIdx.x) * 8;
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) load_whole(to[j], at + j * kThreads * 8);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) load_piece(to[j], logits, pieces, q0 + j * kThreads + (int)threadIdx.x, end);
+        }
+    };
+    load(e, begin);
+    const Target target = target_of(p, row, logits);
+    // Tokens ahead of the target: those not <= a bar, which is the target's logit behind it, and the number below it ahead of it, where
     // equal ones count (NaN, which nothing is <= to, if there is no number below).  +inf: nothing counts.
     float bar_behind = INFINITY, bar_ahead = INFINITY;
-    if (inside && p.rank) {
-        bar_behind = to_f32(logits[target]);
+    if (p.rank && target.at >= 0) {
+        bar_behind = target.x;
         const uint32_t b = __builtin_bit_cast(uint32_t, bar_behind + 0.0f);
         bar_ahead = bar_behind == -INFINITY ? __builtin_nanf("") : b == 0 ? -1e-45f : __builtin_bit_cast(float, b & 0x80000000u ? b + 1 : b - 1);
     }
-    const int target_piece = inside ? (int)((target + ahead0) / 8) : -1;
 
     Sums r = {kLowest, 0.0f, 0.0f};
     int ahead = 0;
     uint64_t list = 0;
-    float last = -INFINITY;       // the list's last wanted entry
-    uint32_t last_index = 0;
+    // What a logit has to reach to be gathered: a number, the last wanted entry of the wavefront's list, or what as many lanes' logits reach as
+    // are wanted: lanes in groups, as many groups as tokens are wanted or more, the least of the groups' largest logits.  Groups of the workgroup's lanes (their
+    // bars in s_bar, which only rise: an old one is a lower one) or, where it has fewer pieces than lanes, of the wavefront's.
+    float last = kLowest;
+    uint32_t last_index = 0xffffffffu;
+    int groups = 4;
+    while (groups < p.top) groups *= 2;
+    const bool wide = end - begin >= kThreads;
+    const int group = wide ? kThreads / groups : 64 / groups;
     int gathered = 0;
-    uint64_t* const heap = s_list[wave];
+    uint64_t* const heap = s_list[TOP ? wave : 0];
     auto take = [&](uint64_t key) {   // 64 keys into the list
-        list = merged(list, sorted(key, lane), lane);
-        const uint64_t k = from_lane(list, p.top - 1);
+        key = sorted(key, lane);
+        list = list ? merged(list, key, lane) : key;
+        const uint64_t k = of_lane(list, p.top - 1);
         if (k) {
-            last = value_of_key(k);
-            last_index = index_of_key(k);
-        }
-    };
-    for (int q0 = begin; q0 < end; q0 += kThreads) {
-        const int q = q0 + threadIdx.x;
-        Piece<T> e;
-        const int64_t i0 = (int64_t)q * 8 - ahead0;
-        load_piece(e, logits, q < end ? i0 : -8, p.vocab);
-        float x[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = value_of(e, k);
-        float most = x[0];
-#pragma unroll
-        for (int k = 1; k < 8; ++k) most = fmaxf(most, x[k]);
-        if (__any(most > r.m)) raise(r, fmaxf(r.m, most), c);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float t = (x[k] - r.m) * c, f = __builtin_amdgcn_exp2f(t);
-            r.s += f;
-            r.u = __builtin_fmaf(f, fmaxf(t, kNothing), r.u);
-        }
-        const bool by_index = q < end && (q == target_piece || i0 < 0);   // (the first piece may hold what is not the row's)
-        const float bar = q < target_piece && q < end && !by_index ? bar_ahead : bar_behind;
-        if (p.rank && __any(by_index || !(most <= bar))) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const bool counts = by_index ? i0 + k >= 0 && i0 + k < p.vocab && (x[k] > bar_behind || (x[k] == bar_behind && i0 + k < target)) : !(x[k] <= bar);
-                ahead += counts ? 1 : 0;
+            const float v = value_of_key(k);
+            if (v >= last) {
+                last = v;
+                last_index = index_of_key(k);
             }
         }
-        if constexpr (TOP) {
-            if (__any(most > last || (most == last && (uint32_t)i0 <= last_index))) {
-#pragma unroll 1
-                for (int k = 0; k < 8; ++k) {
-                    float v = x[0];
+    };
+    for (int q0 = begin, n = 0; q0 < end; q0 += kBatch * kThreads, ++n) {
+        if (q0 + kBatch * kThreads < end) load(next, q0 + kBatch * kThreads);
+        float x[kBatch][8], most[kBatch], highest = -INFINITY;
 #pragma unroll
-                    for (int j = 1; j < 8; ++j) v = k == j ? x[j] : v;
-                    const uint32_t i = (uint32_t)(i0 + k);
-                    const bool pass = v > last || (v == last && i < last_index && v > -INFINITY);
-                    const unsigned long long mask = __ballot(pass);
-                    if (!mask) continue;
-                    if (pass) heap[gathered + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = key_of(v, i);
-                    gathered += __builtin_popcountll(mask);
-                    if (gathered >= 64) {
-                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-                        take(heap[lane]);
-                        const uint64_t rest = heap[64 + lane];
-                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-                        heap[lane] = rest;
-                        gathered -= 64;
+        for (int j = 0; j < kBatch; ++j) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[j][k] = value_of(e[j], k);
+            most[j] = fmaxf(fmaxf(fmaxf(x[j][0], x[j][1]), fmaxf(x[j][2], x[j][3])), fmaxf(fmaxf(x[j][4], x[j][5]), fmaxf(x[j][6], x[j][7])));
+            highest = fmaxf(highest, most[j]);
+        }
+        if (__any(highest > r.m)) raise(r, fmaxf(r.m, highest), c);
+        if constexpr (TOP) {
+            if ((n & (n + 1)) == 0) {   // (after 1, 2, 4, 8.. batches)
+                float bar = least_of_groups(r.s > 0.0f || highest >= r.m ? r.m : -INFINITY, group, lane);
+                if (wide) {
+                    if (lane == 0) s_bar[wave] = bar;
+                    if (n == 0) __syncthreads();
+#pragma unroll
+                    for (int w = 0; w < kWaves; ++w) bar = fminf(bar, s_bar[w]);
+                }
+                if (bar > last) {
+                    last = bar;
+                    last_index = 0xffffffffu;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int q = q0 + j * kThreads + (int)threadIdx.x, i0 = pieces.index(q);
+            if (q0 + j * kThreads >= end) break;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float t = (x[j][k] - r.m) * c, f = __builtin_amdgcn_exp2f(t);
+                r.s += f;
+                r.u = __builtin_fmaf(f, fmaxf(t, kNothing), r.u);
+            }
+            // (single logits, and the target's own piece, are counted below)
+            const float bar = q >= whole || (i0 <= target.at && target.at - i0 < 8) ? INFINITY : i0 < target.at ? bar_ahead : bar_behind;
+            if (__any(!(most[j] <= bar))) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) ahead += !(x[j][k] <= bar) ? 1 : 0;
+            }
+            if constexpr (TOP) {
+                if (__any(most[j] > last || (most[j] == last && (uint32_t)i0 <= last_index))) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const uint32_t i = (uint32_t)(i0 + k);
+                        const bool pass = x[j][k] > last || (x[j][k] == last && i < last_index);
+                        const unsigned long long mask = __ballot(pass);
+                        if (!mask) continue;
+                        if (pass) heap[gathered + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = key_of(x[j][k], i);
+                        gathered += __builtin_popcountll(mask);
+                        if (gathered >= 64) {
+                            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+                            take(heap[lane]);
+                            const uint64_t rest = heap[64 + lane];
+                            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+                            heap[lane] = rest;
+                            gathered -= 64;
+                        }
                     }
                 }
             }
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) e[j] = next[j];
+    }
+    if (part == 0 && wave == 0 && p.rank && target.at >= 0) {
+        // single logits at the ends of the row, and the seven beside the target
+        const int single = lane < pieces.count - pieces.whole ? pieces.index(pieces.whole + lane) : -1;
+        const int own = target.at >= pieces.head && target.at < pieces.head + 8 * pieces.whole ? (target.at - pieces.head) / 8 * 8 + pieces.head + lane - 16 : -1;
+        const int i = lane < 16 ? single : lane < 24 ? own : -1;
+        if (i >= 0) {
+            const float v = to_f32(logits[i]);
+            ahead += v > target.x || (v == target.x && i < target.at) ? 1 : 0;
         }
     }
     if constexpr (TOP) {
@@ -256,26 +374,26 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobsParams
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
         heap[lane] = list;
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const Sums o = {__shfl_xor(r.m, d), __shfl_xor(r.s, d), __shfl_xor(r.u, d)};
-        join(r, o, c);
-        ahead += __shfl_xor(ahead, d);
-    }
+    join_lanes(r, ahead, c, lane);
     if (lane == 0) {
         s_sums[wave] = r;
         s_ahead[wave] = ahead;
     }
     __syncthreads();
+    if constexpr (TOP) {
+        if (wave == 2) s_list[2][lane] = merged(list, s_list[3][lane], lane);
+        if (wave == 0) list = merged(list, s_list[1][lane], lane);
+        __syncthreads();
+    }
     if (wave) return;
+    if constexpr (TOP) list = merged(list, s_list[2][lane], lane);
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) {
         join(r, s_sums[w], c);
         ahead += s_ahead[w];
-        if constexpr (TOP) list = merged(list, s_list[w][lane], lane);
     }
     if (p.parts == 1) {
-        finish(p, row, logits, r, ahead, list, lane);
+        finish(p, row, target, r, ahead, list, lane);
         return;
     }
     const int64_t at = row * p.parts + part;
@@ -283,29 +401,64 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobsParams
     if (lane < p.top) p.lists[at * p.top + lane] = list;
 }
 
-// The parts of a row joined, by one wavefront.
+// The parts of a row joined.  Entries of their lists that reach the last wanted one of the first entries (where there are as many parts), or the
+// largest of the last ones, which as many reach as are wanted, are gathered, and taken 64 at a time by the first wavefront.
+constexpr int kJoinThreads = 256;
 template <typename T>
-__global__ __launch_bounds__(64) void logprobs_join_kernel(const LogprobsParams p) {
-    const int lane = threadIdx.x;
+__global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(const LogprobsParams p) {
+    __shared__ uint64_t s_heap[kMostParts * kMostTop];
+    __shared__ int s_gathered;
+    __shared__ uint64_t s_bar;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row = blockIdx.x;
     const float c = p.scale * kLog2e;
+    const uint64_t* const lists = p.lists + row * p.parts * p.top;
+    constexpr int kMine = 4;
+    uint64_t mine[kMine];
+    const int count = p.parts * p.top;
+    Target target = {-1, INFINITY};
     Sums r = {kLowest, 0.0f, 0.0f};
     int ahead = 0;
-    if (lane < p.parts) {   // (at most 64)
-        const v4f v = p.sums[row * p.parts + lane];
-        const float n = v[3];
-        r = {v[0], v[1], v[2]};
-        ahead = __builtin_bit_cast(int, n);
-    }
+    if (p.top) {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const Sums o = {__shfl_xor(r.m, d), __shfl_xor(r.s, d), __shfl_xor(r.u, d)};
-        join(r, o, c);
-        ahead += __shfl_xor(ahead, d);
+        for (int j = 0; j < kMine; ++j) mine[j] = j * kJoinThreads + (int)threadIdx.x < count ? lists[j * kJoinThreads + threadIdx.x] : 0;
+    }
+    if (wave == 0) {
+        target = target_of(p, row, static_cast<const T*>(p.logits) + row * p.ldl);
+        if (lane < p.parts) {   // (at most 64)
+            const v4f v = p.sums[row * p.parts + lane];
+            const float n = v[3];
+            r = {v[0], v[1], v[2]};
+            ahead = __builtin_bit_cast(int, n);
+        }
+        join_lanes(r, ahead, c, lane);
+    } else if (wave == 1 && p.top) {
+        const uint64_t k = lane < p.parts ? lists[lane * p.top + (p.parts >= p.top ? 0 : p.top - 1)] : 0;
+        const uint64_t bar = of_lane(sorted(k, lane), p.parts >= p.top ? p.top - 1 : 0);
+        if (lane == 0) {
+            s_bar = bar ? bar : 1;   // (0 is no entry)
+            s_gathered = 0;
+        }
     }
     uint64_t list = 0;
-    for (int q = 0; q < (p.top ? p.parts : 0); ++q) list = merged(list, lane < p.top ? p.lists[(row * p.parts + q) * p.top + lane] : 0, lane);
-    finish(p, row, static_cast<const T*>(p.logits) + row * p.ldl, r, ahead, list, lane);
+    if (p.top) {
+        __syncthreads();
+        const uint64_t bar = s_bar;
+        auto gather = [&](uint64_t k) {
+            if (k >= bar) s_heap[atomicAdd(&s_gathered, 1)] = k;
+        };
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) gather(mine[j]);
+        for (int i = kMine * kJoinThreads + threadIdx.x; i < count; i += kJoinThreads) gather(lists[i]);
+        __syncthreads();
+        if (wave) return;
+        const int gathered = s_gathered;
+        for (int i = 0; i < gathered; i += 64) {
+            const uint64_t key = sorted(i + lane < gathered ? s_heap[i + lane] : 0, lane);
+            list = i ? merged(list, key, lane) : key;
+        }
+    }
+    if (wave == 0) finish(p, row, target, r, ahead, list, lane);
 }
 
 template <typename T>
@@ -313,7 +466,7 @@ void launch_logprobs(const LogprobsParams& p, hipStream_t s) {
     const dim3 grid((unsigned)p.n_rows, (unsigned)p.parts);
     if (p.top) logprobs_kernel<T, true><<<grid, dim3(kThreads), 0, s>>>(p);
     else logprobs_kernel<T, false><<<grid, dim3(kThreads), 0, s>>>(p);
-    if (p.parts > 1) logprobs_join_kernel<T><<<dim3((unsigned)p.n_rows), dim3(64), 0, s>>>(p);
+    if (p.parts > 1) logprobs_join_kernel<T><<<dim3((unsigned)p.n_rows), dim3(kJoinThreads), 0, s>>>(p);
 }
 
 }  // namespace
