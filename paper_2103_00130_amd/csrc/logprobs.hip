@@ -269,8 +269,8 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobsParams
     int ahead = 0;
     uint64_t list = 0;
     // What a logit has to reach to be gathered: a number, the last wanted entry of the wavefront's list, or what as many lanes' logits reach as
-    // are wanted: lanes in groups, as many groups as tokens are wanted or more, the least of the groups' largest logits.  Groups of the workgroup's lanes (their
-    // bars in s_bar, which only rise: an old one is a lower one) or, where it has fewer pieces than lanes, of the wavefront's.
+    // are wanted: lanes in groups, as many groups as tokens are wanted or more, the least of the groups' largest logits.  Groups of the workgroup's lanes or,
+    // where it has fewer pieces than lanes, of any wavefront's.  (What wavefronts have in s_bar only rises: an old one is a lower one.)
     float last = kLowest;
     uint32_t last_index = 0xffffffffu;
     int groups = 4;
@@ -305,12 +305,10 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobsParams
         if constexpr (TOP) {
             if ((n & (n + 1)) == 0) {   // (after 1, 2, 4, 8.. batches)
                 float bar = least_of_groups(r.s > 0.0f || highest >= r.m ? r.m : -INFINITY, group, lane);
-                if (wide) {
-                    if (lane == 0) s_bar[wave] = bar;
-                    if (n == 0) __syncthreads();
+                if (lane == 0) s_bar[wave] = bar;
+                if (n == 0) __syncthreads();
 #pragma unroll
-                    for (int w = 0; w < kWaves; ++w) bar = fminf(bar, s_bar[w]);
-                }
+                for (int w = 0; w < kWaves; ++w) bar = wide ? fminf(bar, s_bar[w]) : fmaxf(bar, s_bar[w]);
                 if (bar > last) {
                     last = bar;
                     last_index = 0xffffffffu;

@@ -25,11 +25,16 @@ typedef bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef f16 v8h __attribute__((ext_vector_type(8)));
 
 // Layouts.  down: [adapter][rank / 16][chunk of K][lane][16 bytes], lane l of a chunk has row l % 16 of the sixteen and, of the chunk's 64 bytes a
-// row, bytes 16 (l / 16)..: the first operand of a product with rows of X.  up: [adapter][columns / 64][rank / 16][tile 0..3][lane][4 elements]:
-// lane l of a tile has the ranks 4 (l / 16).. of the sixteen for column 16 (i / 4) + 4 tile + i % 4 of the 64, i = l % 16, so that a
-// lane's sums of the four tiles are 16 columns side by side.
+// row, bytes 16 (l / 16)..: the first operand of a product with rows of X.  up: [adapter][columns / 64][rank / 16][lane][tile 0..3][4 elements]:
+// lane l of a tile has the ranks 4 (l / 16).. of the sixteen for column_of(i / 4, 4 tile + i % 4) of the 64, i = l % 16, so that a
+// lane's sums of the four tiles are pieces of 16 bytes of Y, those of four lanes side by side.
 template <typename T>
 constexpr int kChunkOf = 64 / sizeof(T);   // columns of a chunk
+template <typename T>
+constexpr int kPiece = 16 / sizeof(T);     // elements of 16 bytes
+// the place of a lane's f-th sum among 64 columns, kg the lane's sixteen
+template <typename T>
+__device__ inline int column_of(int kg, int f) { return 4 * kPiece<T> * (f / kPiece<T>) + kPiece<T> * kg + f % kPiece<T>; }
 
 struct LoraParams {
     const uint8_t* down;
@@ -42,7 +47,8 @@ struct LoraParams {
     const int32_t* ids;
     float* sums;     // [split][row][ranks]
     int64_t ldx, ldb, ldy;
-    int M, N, K, adapters, max_rank, rank_tiles, chunks, blocks, splits, slots;
+    int M, N, K, adapters, max_rank, rank_tiles, chunks, blocks, splits, tiles, slots;
+    bool by_rows;    // the wavefronts of a workgroup have rows of their own and the same columns
     bool wide;       // rows of base and Y are whole aligned pieces of 16 bytes
 };
 
@@ -93,133 +99,240 @@ __device__ inline int adapter_of(const LoraParams& p, int m0) {
     const int a = m < p.M ? p.ids[m] : -1;
     return a >= 0 && a < p.adapters ? a : -1;
 }
-// (matrix instructions run whatever lanes are active: what decides about them is brought to one register for all)
-__device__ inline int rank_of(const LoraParams& p, int a) { return __builtin_amdgcn_readfirstlane(min(max(p.rank[a], 0), p.max_rank)); }
-
-// Sums over K.  RT: sixteens of ranks that a wavefront holds; an adapter of more is taken in turns.
-template <typename T, int RT>
-__global__ __launch_bounds__(kLoraWaves * 64) void lora_down_kernel(const LoraParams p) {
-    __shared__ v4f s_sum[kLoraWaves][RT][64];
-    constexpr int kStep = RT > 2 ? 2 : 4;   // chunks under way
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = lane >> 4;
-    const int m0 = blockIdx.y * kLoraRows, mine = adapter_of(p, m0);
-    const int each = (p.chunks + p.splits - 1) / p.splits, begin = blockIdx.z * each, end = min(p.chunks, begin + each);
-    const T* const row = static_cast<const T*>(p.X) + (int64_t)min(m0 + (lane & 15), p.M - 1) * p.ldx;
-    uint32_t left = (uint32_t)__ballot(mine >= 0) & 0xffffu;
+// The adapters among a tile's rows (and -1, where `none` says so), dealt to `slots` workgroups: to one for each row that has its adapter first, where there
+// are as many, else in turns.
+template <typename F>
+__device__ inline void for_adapters(int mine, int slot, int slots, bool none, const F& f) {
+    uint32_t left = (uint32_t)__ballot(none || mine >= 0) & 0xffffu;
+    if (slots == kLoraRows) {
+        const int a = __builtin_amdgcn_readlane(mine, slot);
+        const uint32_t same = (uint32_t)__ballot(mine == a) & left;
+        if (same && __builtin_ctz(same) == slot) f(a);
+        return;
+    }
     for (int n = 0; left; ++n) {
         const int a = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
         left &= ~(uint32_t)__ballot(mine == a);
-        if (n % p.slots != (int)blockIdx.x) continue;
-        const int tiles = (rank_of(p, a) + 15) / 16;
+        if (n % slots == slot) f(a);
+    }
+}
+// (matrix instructions run whatever lanes are active: what decides about them is brought to one register for all)
+__device__ inline int rank_of(const LoraParams& p, int a) { return __builtin_amdgcn_readfirstlane(min(max(p.rank[a], 0), p.max_rank)); }
+
+// Sums over K.  RT: sixteens of ranks that a wavefront holds; an adapter of more is taken in turns.  The next step's loads are on their way while
+// this one's are multiplied, without a branch about them, so that what is awaited is what is multiplied: rows that are not the adapter's are
+// read from a row that is, and their sums left.
+template <typename T, int RT>
+__global__ __launch_bounds__(kLoraWaves * 64) void lora_down_kernel(const LoraParams p) {
+    __shared__ v4f s_sum[kLoraWaves][RT][64];
+    constexpr int kStep = RT > 2 ? 2 : 4;   // chunks of a step
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = lane >> 4;
+    const int m0 = blockIdx.y * kLoraRows, mine = adapter_of(p, m0);
+    const int each = (p.chunks + p.splits - 1) / p.splits, begin = min((int)blockIdx.z * each, p.chunks), end = min(p.chunks, begin + each);
+    const int whole = min(end, p.K / kChunkOf<T>);   // (the last chunk may reach past K)
+    for_adapters(mine, blockIdx.x, p.slots, false, [&](int a) __attribute__((always_inline)) {
+        const uint32_t rows = (uint32_t)__ballot(mine == a) & 0xffffu;
+        const int from = mine == a ? lane & 15 : __builtin_ctz(rows);
+        const T* const row = static_cast<const T*>(p.X) + (int64_t)(m0 + from) * p.ldx + kg * kPiece<T>;
         const v4u* const down = reinterpret_cast<const v4u*>(p.down) + (int64_t)a * p.rank_tiles * p.chunks * 64 + lane;
-        for (int t0 = 0; t0 < tiles; t0 += RT) {
-            v4f sum[RT];
+        const int tiles = (rank_of(p, a) + 15) / 16;
+        auto some = [&](auto nt, int t0) __attribute__((always_inline)) {
+            constexpr int NT = decltype(nt)::value;
+            struct Fetched {
+                v4u x[kStep], w[kStep][NT];
+            };
+            v4f sum[NT];
 #pragma unroll
-            for (int t = 0; t < RT; ++t) sum[t] = v4f{0, 0, 0, 0};
-            for (int c0 = begin + wave * kStep; c0 < end; c0 += kLoraWaves * kStep) {
-                v4u x[kStep], w[kStep][RT];
+            for (int t = 0; t < NT; ++t) sum[t] = v4f{0, 0, 0, 0};
+            auto fetch = [&](Fetched& f, int c0) __attribute__((always_inline)) {
 #pragma unroll
                 for (int c = 0; c < kStep; ++c) {
-                    const int ch = c0 + c;
-                    x[c] = v4u{0, 0, 0, 0};
-                    if (mine == a && ch < end) x[c] = load_x<T>(row, ch * kChunkOf<T> + kg * (16 / (int)sizeof(T)), p.K);
+                    const int ch = min(c0 + c, whole - 1);
+                    f.x[c] = *reinterpret_cast<const v4u_any*>(row + ch * kChunkOf<T>);
 #pragma unroll
-                    for (int t = 0; t < RT; ++t)
-                        if (t0 + t < tiles) w[c][t] = down[((int64_t)(t0 + t) * p.chunks + min(ch, end - 1)) * 64];
+                    for (int t = 0; t < NT; ++t) f.w[c][t] = down[((int64_t)(t0 + t) * p.chunks + ch) * 64];
                 }
+            };
+            auto multiply = [&](const Fetched& f, int c0) __attribute__((always_inline)) {
 #pragma unroll
-                for (int c = 0; c < kStep; ++c)
+                for (int c = 0; c < kStep; ++c) {
+                    const v4u x = c0 + c < whole ? f.x[c] : v4u{0, 0, 0, 0}, none = {0, 0, 0, 0};
 #pragma unroll
-                    for (int t = 0; t < RT; ++t)
-                        if (t0 + t < tiles) sum[t] = mma<T>(w[c][t], x[c], sum[t]);
+                    for (int t = 0; t < NT; ++t) sum[t] = mma<T>(c0 + c < whole ? f.w[c][t] : none, x, sum[t]);
+                }
+            };
+            constexpr int kAll = kLoraWaves * kStep;
+            int c0 = begin + wave * kStep;
+            if (c0 < whole) {
+                Fetched one, two;
+                fetch(one, c0);
+                for (;; c0 += 2 * kAll) {
+                    fetch(two, c0 + kAll);
+                    multiply(one, c0);
+                    if (c0 + kAll >= whole) break;
+                    fetch(one, c0 + 2 * kAll);
+                    multiply(two, c0 + kAll);
+                    if (c0 + 2 * kAll >= whole) break;
+                }
+            }
+            if (wave == kLoraWaves - 1 && whole < end) {
+                const int k = whole * kChunkOf<T> + kg * kPiece<T>;
+                const v4u x = load_x<T>(row - kg * kPiece<T>, k, p.K);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) sum[t] = mma<T>(down[((int64_t)(t0 + t) * p.chunks + whole) * 64], x, sum[t]);
             }
             wait_for_products();
 #pragma unroll
-            for (int t = 0; t < RT; ++t) s_sum[wave][t][lane] = sum[t];
+            for (int t = 0; t < NT; ++t) s_sum[wave][t][lane] = sum[t];
             __syncthreads();
-            for (int t = wave; t < RT && t0 + t < tiles; t += kLoraWaves) {
+            for (int t = wave; t < NT; t += kLoraWaves) {
                 v4f y = s_sum[0][t][lane];
 #pragma unroll
                 for (int w = 1; w < kLoraWaves; ++w) y += s_sum[w][t][lane];
                 if (mine == a) *reinterpret_cast<v4f*>(p.sums + ((int64_t)blockIdx.z * p.M + m0 + (lane & 15)) * (16 * p.rank_tiles) + 16 * (t0 + t) + 4 * kg) = y;
             }
             __syncthreads();
-        }
-    }
+        };
+        int t0 = 0;
+        for (; t0 + RT <= tiles; t0 += RT) some(std::integral_constant<int, RT>(), t0);
+        if constexpr (RT > 1)
+            for (; t0 < tiles; ++t0) some(std::integral_constant<int, 1>(), t0);
+    });
 }
 
-// Four elements of `up` as binary32.
+// Sixteen elements side by side, as they are stored.
 template <typename T>
-__device__ inline v4f load_up(const uint8_t* up, int64_t piece) {
-    if constexpr (sizeof(T) == 4) {
-        return reinterpret_cast<const v4f*>(up)[piece];
-    } else {
-        const v2u w = reinterpret_cast<const v2u*>(up)[piece];
-        v4f f;
+struct Sixteen {
+    v4u w[sizeof(T)];
+    __device__ inline void load(const T* at) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = to_f32(__builtin_bit_cast(T, (uint16_t)(w[i / 2] >> (16 * (i % 2)))));
-        return f;
+        for (int h = 0; h < (int)sizeof(T); ++h) w[h] = reinterpret_cast<const v4u*>(at)[h];
     }
-}
+    __device__ inline float operator[](int i) const {
+        constexpr int n = 16 / sizeof(T);
+        const uint32_t v = w[i / n][i % n * (int)sizeof(T) / 4];
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, v);
+        else return to_f32(__builtin_bit_cast(T, (uint16_t)(v >> (16 * (i % 2)))));
+    }
+};
 
-// Y.  A wavefront has 16 rows and 64 columns at a time, a lane 16 columns of one row.
-template <typename T>
+// Y.  A wavefront has 16 rows and 64 columns at a time, a lane 16 columns of one row; RT: the most sixteens of ranks whose sums over K it keeps (an
+// adapter of more reads the others' anew for all columns).  What the next columns need is on its way while these are multiplied, as above.
+// WIDE: rows of base and Y are whole aligned pieces of 16 bytes, and there is one at least.
+template <typename T, int RT, bool WIDE>
 __global__ __launch_bounds__(kLoraWaves * 64) void lora_up_kernel(const LoraParams p) {
+    constexpr int P = kPiece<T>, kPieces = 16 / P;
+    typedef T piece __attribute__((ext_vector_type(P)));
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = lane >> 4;
-    const int m0 = blockIdx.y * kLoraRows, m = m0 + (lane & 15), mine = adapter_of(p, m0);
-    const int block = blockIdx.x * kLoraWaves + wave;
-    if (block >= p.blocks) return;
-    const int n0 = block * kLoraColumns + 16 * kg, columns = min(p.N - n0, 16);
-    const T* const base = static_cast<const T*>(p.base) + (int64_t)min(m, p.M - 1) * p.ldb + n0;
-    T* const y = static_cast<T*>(p.Y) + (int64_t)min(m, p.M - 1) * p.ldy + n0;
-    // what the rows of the group get: base, and `sum` scaled
-    auto store = [&](bool on, const v4f (&sum)[4], float scale) {
-        if (!on || m >= p.M || columns <= 0) return;
-        if (p.wide && columns == 16) {
-            constexpr int n = 16 / sizeof(T);
-            typedef T piece __attribute__((ext_vector_type(n)));
+    const int tile = p.by_rows ? blockIdx.y * kLoraWaves + wave : blockIdx.y, m0 = tile * kLoraRows;
+    const int first = p.by_rows ? blockIdx.x : blockIdx.x * kLoraWaves + wave, stride = p.by_rows ? gridDim.x : gridDim.x * kLoraWaves;
+    if (tile >= p.tiles || first >= p.blocks) return;
+    const int mine = adapter_of(p, m0);
+    for_adapters(mine, blockIdx.z, p.slots, p.base != p.Y, [&](int a) __attribute__((always_inline)) {
+        const uint32_t rows = (uint32_t)__ballot(mine == a) & 0xffffu;
+        const int m = m0 + (mine == a ? lane & 15 : __builtin_ctz(rows));
+        const bool on = mine == a && m < p.M;
+        const T* const base = static_cast<const T*>(p.base) + (int64_t)min(m, p.M - 1) * p.ldb;
+        T* const y = static_cast<T*>(p.Y) + (int64_t)min(m, p.M - 1) * p.ldy;
+        if (a < 0) {   // rows without an adapter: as they are
+            for (int block = first; on && block < p.blocks; block += stride) {
 #pragma unroll
-            for (int h = 0; h < 16 / n; ++h) {
-                piece v = reinterpret_cast<const piece*>(base)[h];
-#pragma unroll
-                for (int i = 0; i < n; ++i) v[i] = from_f32<T>(__builtin_fmaf(scale, sum[(h * n + i) / 4][i % 4], to_f32((T)v[i])));
-                reinterpret_cast<piece*>(y)[h] = v;
+                for (int h = 0; h < kPieces; ++h) {
+                    const int n = block * kLoraColumns + column_of<T>(kg, h * P);
+                    if (WIDE && n + P <= p.N) *reinterpret_cast<v4u*>(y + n) = *reinterpret_cast<const v4u*>(base + n);
+                    else
+                        for (int i = n; i < min(n + P, p.N); ++i) y[i] = base[i];
+                }
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (i < columns) y[i] = from_f32<T>(__builtin_fmaf(scale, sum[i / 4][i % 4], to_f32(base[i])));
+            return;
         }
-    };
-    uint32_t left = 0xffffu;
-    for (int n = 0; left; ++n) {
-        const int a = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
-        left &= ~(uint32_t)__ballot(mine == a);
-        if (n % p.slots != (int)blockIdx.z) continue;
-        v4f sum[4];
+        const Sixteen<T>* const up = reinterpret_cast<const Sixteen<T>*>(p.up) + (int64_t)a * p.blocks * p.rank_tiles * 64 + lane;
+        auto sums_of = [&](int t) __attribute__((always_inline)) {
+            const v4f* const at = reinterpret_cast<const v4f*>(p.sums + (int64_t)m * (16 * p.rank_tiles) + 16 * t + 4 * kg);
+            const int64_t step = (int64_t)p.M * 4 * p.rank_tiles;
+            v4f v = {0, 0, 0, 0};
+            for (int s = 0; s < p.splits; s += 4) {
+                v4f part[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) sum[t] = v4f{0, 0, 0, 0};
-        if (a < 0) {
-            // rows without an adapter: as they are
-            if (p.base != p.Y && mine == a && m < p.M && columns > 0)
-                for (int i = 0; i < columns; ++i) y[i] = base[i];
-            continue;
-        }
+                for (int i = 0; i < 4; ++i) part[i] = at[min(s + i, p.splits - 1) * step];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v += s + i < p.splits ? part[i] : v4f{0, 0, 0, 0};
+            }
+            return v;
+        };
+        const float scale = p.scale[a];
         const int tiles = (rank_of(p, a) + 15) / 16;
-        for (int t0 = 0; t0 < tiles; ++t0) {
-            v4f h = {0, 0, 0, 0};
-            if (mine == a)
-                for (int s = 0; s < p.splits; ++s) h += *reinterpret_cast<const v4f*>(p.sums + ((int64_t)s * p.M + m) * (16 * p.rank_tiles) + 16 * t0 + 4 * kg);
+        auto some = [&](auto nt) __attribute__((always_inline)) {
+            constexpr int NT = decltype(nt)::value;
+            struct Fetched {
+                Sixteen<T> up[NT < 1 ? 1 : NT];
+                v4u base[kPieces];
+            };
+            auto fetch = [&](Fetched& f, int block) __attribute__((always_inline)) {
+                block = min(block, p.blocks - 1);
+                if constexpr (WIDE) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const v4f w = load_up<T>(p.up, ((((int64_t)a * p.blocks + block) * p.rank_tiles + t0) * 4 + t) * 64 + lane);
+                    for (int h = 0; h < kPieces; ++h) f.base[h] = *reinterpret_cast<const v4u*>(base + max(min(block * kLoraColumns + column_of<T>(kg, h * P), p.N - P) & ~(P - 1), 0));
+                }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[i], h[i], sum[t], 0, 0, 0);
+                for (int t = 0; t < NT; ++t) f.up[t].load(reinterpret_cast<const T*>(up + ((int64_t)block * p.rank_tiles + t) * 64));
+            };
+            auto finish = [&](const Fetched& f, int block, const v4f (&h)[NT < 1 ? 1 : NT]) __attribute__((always_inline)) {
+                v4f sum[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) sum[t] = v4f{0, 0, 0, 0};
+                auto multiply = [&](const Sixteen<T>& w, v4f v) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) sum[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[4 * t + i], v[i], sum[t], 0, 0, 0);
+                };
+#pragma unroll
+                for (int t = 0; t < NT; ++t) multiply(f.up[t], h[t]);
+                if constexpr (NT == RT)
+                    for (int t = RT; t < tiles; ++t) {
+                        Sixteen<T> w;
+                        w.load(reinterpret_cast<const T*>(up + ((int64_t)block * p.rank_tiles + t) * 64));
+                        multiply(w, sums_of(t));
+                    }
+                wait_for_products();
+                if (!on) return;
+#pragma unroll
+                for (int h = 0; h < kPieces; ++h) {
+                    const int n = block * kLoraColumns + column_of<T>(kg, h * P);
+                    if (WIDE && n + P <= p.N) {
+                        const piece b = __builtin_bit_cast(piece, f.base[h]);
+                        piece v;
+#pragma unroll
+                        for (int i = 0; i < P; ++i) v[i] = from_f32<T>(__builtin_fmaf(scale, sum[(h * P + i) / 4][i % 4], to_f32((T)b[i])));
+                        *reinterpret_cast<piece*>(y + n) = v;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < P; ++i)
+                            if (n + i < p.N) y[n + i] = from_f32<T>(__builtin_fmaf(scale, sum[(h * P + i) / 4][i % 4], to_f32(base[n + i])));
+                    }
+                }
+            };
+            Fetched one, two;
+            fetch(one, first);
+            v4f h[NT < 1 ? 1 : NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) h[t] = sums_of(t);
+            for (int block = first;; block += 2 * stride) {
+                fetch(two, block + stride);
+                finish(one, block, h);
+                if (block + stride >= p.blocks) break;
+                fetch(one, block + 2 * stride);
+                finish(two, block + stride, h);
+                if (block + 2 * stride >= p.blocks) break;
             }
-        }
-        wait_for_products();
-        store(mine == a, sum, p.scale[a]);
-    }
+        };
+        if (tiles == 0) some(std::integral_constant<int, 0>());
+        else if (RT == 1 || tiles == 1) some(std::integral_constant<int, 1>());
+        else if (RT == 2 || tiles == 2) some(std::integral_constant<int, (RT < 2 ? 1 : 2)>());
+        else if (RT == 3 || tiles == 3) some(std::integral_constant<int, (RT < 3 ? 1 : 3)>());
+        else some(std::integral_constant<int, (RT < 4 ? 1 : 4)>());
+    });
 }
 
 // An adapter into its place: one thread for each element of the layout, zeros where the adapter has none.
@@ -240,11 +353,11 @@ __global__ __launch_bounds__(256) void lora_load_kernel(T* down, T* up, float* s
         const int64_t k = piece % chunks * kChunkOf<T> + (lane >> 4) * n + e;
         down[t] = r < rank && k < K ? A[r * lda + k] : (T)0.0f;
     } else if (t - n_down < n_up) {
-        const int64_t u = t - n_down, piece = u / 256;   // [block][rank tile][tile]
-        const int e = (int)(u & 3), lane = (int)(u / 4) & 63, i = lane & 15, tile = (int)(piece & 3), rt = (int)(piece / 4 % tiles);
-        const int64_t block = piece / 4 / tiles, col = block * kLoraColumns + (i >> 2) * 16 + tile * 4 + (i & 3);
+        const int64_t u = t - n_down, piece = u / 1024;   // [block][rank tile]
+        const int e = (int)(u & 3), tile = (int)(u / 4) & 3, lane = (int)(u / 16) & 63, i = lane & 15, rt = (int)(piece % tiles);
+        const int64_t block = piece / tiles, col = block * kLoraColumns + column_of<T>(i >> 2, tile * 4 + (i & 3));
         const int r = rt * 16 + (lane >> 4) * 4 + e;
-        up[((block * rank_tiles + rt) * 4 + tile) * 256 + lane * 4 + e] = r < rank && col < N ? B[col * ldb + r] : (T)0.0f;
+        up[(block * rank_tiles + rt) * 1024 + lane * 16 + tile * 4 + e] = r < rank && col < N ? B[col * ldb + r] : (T)0.0f;
     }
 }
 
@@ -283,7 +396,19 @@ void launch_gemv(const LoraParams& p, const LoraCut& c, hipStream_t s) {
     if (p.rank_tiles == 1) lora_down_kernel<T, 1><<<down, threads, 0, s>>>(p);
     else if (p.rank_tiles == 2) lora_down_kernel<T, 2><<<down, threads, 0, s>>>(p);
     else lora_down_kernel<T, 4><<<down, threads, 0, s>>>(p);
-    lora_up_kernel<T><<<dim3((unsigned)((p.blocks + kLoraWaves - 1) / kLoraWaves), (unsigned)c.tiles, (unsigned)c.slots), threads, 0, s>>>(p);
+    // enough wavefronts to fill the chip, and no more columns to one than that leaves
+    const int64_t rows = c.by_rows ? (c.tiles + kLoraWaves - 1) / kLoraWaves : c.tiles, most = c.by_rows ? p.blocks : (p.blocks + kLoraWaves - 1) / kLoraWaves;
+    int64_t columns = (kLoraUpGroups + rows * c.slots - 1) / (rows * c.slots);
+    if (columns > most) columns = most;
+    const dim3 up((unsigned)columns, (unsigned)rows, (unsigned)c.slots);
+    auto launch = [&](auto wide) {
+        constexpr bool W = decltype(wide)::value;
+        if (p.rank_tiles == 1) lora_up_kernel<T, 1, W><<<up, threads, 0, s>>>(p);
+        else if (p.rank_tiles == 2) lora_up_kernel<T, 2, W><<<up, threads, 0, s>>>(p);
+        else lora_up_kernel<T, 4, W><<<up, threads, 0, s>>>(p);
+    };
+    if (p.wide) launch(std::true_type());
+    else launch(std::false_type());
 }
 
 }  // namespace
@@ -363,7 +488,9 @@ int abft_lora_gemv(const void* X, int64_t ldx, int M, const abft_lora_t* pool, c
     p.blocks = (int)abft::blocks_of(pool);
     p.splits = c.splits;
     p.slots = c.slots;
-    p.wide = ((at | (uintptr_t)ldb * es | (uintptr_t)ldy * es) & 15) == 0;
+    p.tiles = c.tiles;
+    p.by_rows = c.by_rows;
+    p.wide = ((at | (uintptr_t)ldb * es | (uintptr_t)ldy * es) & 15) == 0 && (uintptr_t)pool->N * es >= 16;
     hipStream_t s = (hipStream_t)stream;
     if (pool->type == ABFT_TYPE_F32) abft::launch_gemv<float>(p, c, s);
     else if (pool->type == ABFT_TYPE_F16) abft::launch_gemv<abft::f16>(p, c, s);

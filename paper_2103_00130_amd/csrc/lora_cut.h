@@ -11,16 +11,20 @@ constexpr int kLoraColumns = 64;       // columns of Y that a wavefront has at a
 constexpr int kLoraStep = 128;         // columns of X that a wavefront has at a time
 constexpr int kLoraWaves = 4;
 constexpr int kLoraMostSplits = 16;
-constexpr int kLoraWanted = 512;       // workgroups
+constexpr int kLoraWanted = 512;       // workgroups of the sums over K
+constexpr int kLoraUpGroups = 1024;    // ... of the products with `up`
+constexpr int kLoraByRows = 32;        // from so many tiles on a workgroup of the latter has four of them
 
 struct LoraCut {
     int tiles, slots, splits;   // tiles of rows; workgroups among which the adapters of a tile are dealt; parts of K
+    bool by_rows;
 };
 inline LoraCut lora_cut(int64_t M, int K) {
     LoraCut c;
     c.tiles = (int)((M + kLoraRows - 1) / kLoraRows);
     const int most = M < kLoraRows ? (int)M : kLoraRows, each = kLoraWanted / (c.tiles < 1 ? 1 : c.tiles);
     c.slots = each < 1 ? 1 : each < most ? each : most;
+    c.by_rows = c.tiles >= kLoraByRows;
     const int64_t groups = (int64_t)c.tiles * c.slots, long_k = ((int64_t)K + kLoraStep * kLoraWaves - 1) / (kLoraStep * kLoraWaves);
     int64_t s = groups ? (kLoraWanted + groups - 1) / groups : 1;
     if (s > long_k) s = long_k;

@@ -89,7 +89,7 @@ def test_a_workspace_of_logprobs_serves_every_smaller_call(cuts):
             r, v = rng.randint(1, rows), rng.randint(1, vocab)
             n = cuts.parts(r, v)
             assert 1 <= n <= 64 and (n == 1 or r * n <= most), (rows, vocab, r, v)
-    assert cuts.parts(1, 131072) > 8 and cuts.parts(5000, 131072) == 1 and cuts.parts(1, 3000) == 1 and cuts.parts(2 ** 31 - 1, 1) == 1
+    assert cuts.parts(1, 131072) == 64 and cuts.parts(5000, 131072) == 1 and cuts.parts(1024, 131072) == 1 and cuts.parts(400, 131072) == 2 and cuts.parts(1, 3000) == 1 and cuts.parts(2 ** 31 - 1, 1) == 1
 
 
 def test_a_workspace_of_adapters_serves_every_smaller_call(cuts):
