@@ -47,8 +47,7 @@ struct LoraParams {
     const int32_t* ids;
     float* sums;     // [split][row][ranks]
     int64_t ldx, ldb, ldy;
-    int M, N, K, adapters, max_rank, rank_tiles, chunks, blocks, splits, tiles, slots;
-    bool by_rows;    // the wavefronts of a workgroup have rows of their own and the same columns
+    int M, N, K, adapters, max_rank, rank_tiles, chunks, blocks, splits, slots;
     bool wide;       // rows of base and Y are whole aligned pieces of 16 bytes
 };
 
@@ -122,9 +121,9 @@ __device__ inline int rank_of(const LoraParams& p, int a) { return __builtin_amd
 // Sums over K.  RT: sixteens of ranks that a wavefront holds; an adapter of more is taken in turns.  The next step's loads are on their way while
 // this one's are multiplied, without a branch about them, so that what is awaited is what is multiplied: rows that are not the adapter's are
 // read from a row that is, and their sums left.
-template <typename T, int RT>
-__global__ __launch_bounds__(kLoraWaves * 64) void lora_down_kernel(const LoraParams p) {
-    __shared__ v4f s_sum[kLoraWaves][RT][64];
+template <typename T, int RT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void lora_down_kernel(const LoraParams p) {
+    __shared__ v4f s_sum[WAVES][RT][64];
     constexpr int kStep = RT > 2 ? 2 : 4;   // chunks of a step
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = lane >> 4;
     const int m0 = blockIdx.y * kLoraRows, mine = adapter_of(p, m0);
@@ -161,7 +160,7 @@ __global__ __launch_bounds__(kLoraWaves * 64) void lora_down_kernel(const LoraPa
                     for (int t = 0; t < NT; ++t) sum[t] = mma<T>(c0 + c < whole ? f.w[c][t] : none, x, sum[t]);
                 }
             };
-            constexpr int kAll = kLoraWaves * kStep;
+            constexpr int kAll = WAVES * kStep;
             int c0 = begin + wave * kStep;
             if (c0 < whole) {
                 Fetched one, two;
@@ -175,7 +174,7 @@ __global__ __launch_bounds__(kLoraWaves * 64) void lora_down_kernel(const LoraPa
                     if (c0 + 2 * kAll >= whole) break;
                 }
             }
-            if (wave == kLoraWaves - 1 && whole < end) {
+            if (wave == WAVES - 1 && whole < end) {
                 const int k = whole * kChunkOf<T> + kg * kPiece<T>;
                 const v4u x = load_x<T>(row - kg * kPiece<T>, k, p.K);
 #pragma unroll
@@ -185,15 +184,16 @@ __global__ __launch_bounds__(kLoraWaves * 64) void lora_down_kernel(const LoraPa
 #pragma unroll
             for (int t = 0; t < NT; ++t) s_sum[wave][t][lane] = sum[t];
             __syncthreads();
-            for (int t = wave; t < NT; t += kLoraWaves) {
+            for (int t = wave; t < NT; t += WAVES) {
                 v4f y = s_sum[0][t][lane];
 #pragma unroll
-                for (int w = 1; w < kLoraWaves; ++w) y += s_sum[w][t][lane];
+                for (int w = 1; w < WAVES; ++w) y += s_sum[w][t][lane];
                 if (mine == a) *reinterpret_cast<v4f*>(p.sums + ((int64_t)blockIdx.z * p.M + m0 + (lane & 15)) * (16 * p.rank_tiles) + 16 * (t0 + t) + 4 * kg) = y;
             }
             __syncthreads();
         };
         int t0 = 0;
+        if constexpr (RT == 1) some(std::integral_constant<int, 1>(), t0++);   // (nothing waits for the rank; of none, what is there is summed and not used)
         for (; t0 + RT <= tiles; t0 += RT) some(std::integral_constant<int, RT>(), t0);
         if constexpr (RT > 1)
             for (; t0 < tiles; ++t0) some(std::integral_constant<int, 1>(), t0);
@@ -216,123 +216,246 @@ struct Sixteen {
     }
 };
 
-// Y.  A wavefront has 16 rows and 64 columns at a time, a lane 16 columns of one row; RT: the most sixteens of ranks whose sums over K it keeps (an
-// adapter of more reads the others' anew for all columns).  What the next columns need is on its way while these are multiplied, as above.
-// WIDE: rows of base and Y are whole aligned pieces of 16 bytes, and there is one at least.
+// The sums over K as the second product takes them: with bfloat16 adapters as three bfloat16 parts that add up to them bit for bit, sixteen ranks
+// in two products of 32 places (first and second part, third part), else as they are.
+template <typename T>
+struct Factor {
+    v4f h;
+    __device__ inline void set(v4f v) { h = v; }
+    // sum[t] += (the four tiles of `up`) . h
+    __device__ inline void multiply(const Sixteen<T>& w, v4f (&sum)[4]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[4 * t + i], h[i], sum[t], 0, 0, 0);
+    }
+};
+template <>
+struct Factor<bf16> {
+    v4u high, low;
+    __device__ inline void set(v4f v) {
+        uint32_t part[3][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x = v[i];
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                part[k][i] = __builtin_bit_cast(uint32_t, x) >> 16;
+                x -= __builtin_bit_cast(float, part[k][i] << 16);
+            }
+        }
+        high = v4u{part[0][0] | part[0][1] << 16, part[0][2] | part[0][3] << 16, part[1][0] | part[1][1] << 16, part[1][2] | part[1][3] << 16};
+        low = v4u{part[2][0] | part[2][1] << 16, part[2][2] | part[2][3] << 16, 0, 0};
+    }
+    __device__ inline void multiply(const Sixteen<bf16>& w, v4f (&sum)[4]) const {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const uint32_t u0 = w.w[t / 2][t % 2 * 2], u1 = w.w[t / 2][t % 2 * 2 + 1];
+            const v4u u = {u0, u1, u0, u1};
+            sum[t] = mma<bf16>(u, low, sum[t]);
+            sum[t] = mma<bf16>(u, high, sum[t]);
+        }
+    }
+};
+
+// Rows S times 16 of one adapter: base plus scale times the product with `up`, for the columns that a wavefront has (64 at a time, a lane 16 of a row).
+// m: the lane's rows, all of which exist; on: which of them are the adapter's, the others being read as they are and left.  NT sixteens of ranks have
+// their sums over K in registers, those of MORE are read anew for all columns.  What the next columns need is on its way while these are
+// multiplied, as above.  WIDE: rows of base and Y are whole aligned pieces of 16 bytes, and there is one at least.
+template <typename T, int NT, bool MORE, bool WIDE, int S>
+__device__ inline void up_pass(const LoraParams& p, int a, int tiles, const int (&m)[S], const bool (&on)[S], int first, int stride) {
+    constexpr int P = kPiece<T>, kPieces = 16 / P, kKept = NT < 1 ? 1 : NT;
+    typedef T piece __attribute__((ext_vector_type(P)));
+    const int lane = threadIdx.x & 63, kg = lane >> 4;
+    const Sixteen<T>* const up = reinterpret_cast<const Sixteen<T>*>(p.up) + (int64_t)a * p.blocks * p.rank_tiles * 64 + lane;
+    const T* base[S];
+    T* y[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        base[s] = static_cast<const T*>(p.base) + (int64_t)m[s] * p.ldb;
+        y[s] = static_cast<T*>(p.Y) + (int64_t)m[s] * p.ldy;
+    }
+    struct Fetched {
+        Sixteen<T> up[kKept];
+        v4u base[S][kPieces];
+    };
+    auto fetch = [&](Fetched& f, int block) __attribute__((always_inline)) {
+        block = min(block, p.blocks - 1);
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int h = 0; h < kPieces; ++h) {
+                const int n = max(min(block * kLoraColumns + column_of<T>(kg, h * P), p.N - P) & ~(P - 1), 0);
+#pragma unroll
+                for (int s = 0; s < S; ++s) f.base[s][h] = *reinterpret_cast<const v4u*>(base[s] + n);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) f.up[t].load(reinterpret_cast<const T*>(up + ((int64_t)block * p.rank_tiles + t) * 64));
+    };
+    auto sums_of = [&](int row, int t) __attribute__((always_inline)) {
+        const v4f* const at = reinterpret_cast<const v4f*>(p.sums + (int64_t)row * (16 * p.rank_tiles) + 16 * t + 4 * kg);
+        const int64_t step = (int64_t)p.M * 4 * p.rank_tiles;
+        v4f v = at[0];
+        for (int i = 1; i < p.splits; i += 4) {
+            v4f part[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) part[j] = at[min(i + j, p.splits - 1) * step];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v += i + j < p.splits ? part[j] : v4f{0, 0, 0, 0};
+        }
+        return v;
+    };
+    Factor<T> h[S][kKept];
+    const float scale = p.scale[a];
+    auto finish = [&](const Fetched& f, int block) __attribute__((always_inline)) {
+        v4f sum[S][4];
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum[s][t] = v4f{0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int s = 0; s < S; ++s) h[s][t].multiply(f.up[t], sum[s]);
+        if constexpr (MORE)
+            for (int t = NT; t < tiles; ++t) {
+                Sixteen<T> w;
+                w.load(reinterpret_cast<const T*>(up + ((int64_t)block * p.rank_tiles + t) * 64));
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    Factor<T> more;
+                    more.set(sums_of(m[s], t));
+                    more.multiply(w, sum[s]);
+                }
+            }
+        wait_for_products();
+        if (tiles == 0)
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) sum[s][t] = v4f{0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            if (!on[s]) continue;
+#pragma unroll
+            for (int h = 0; h < kPieces; ++h) {
+                const int n = block * kLoraColumns + column_of<T>(kg, h * P);
+                if (WIDE && n + P <= p.N) {
+                    const piece b = __builtin_bit_cast(piece, f.base[s][h]);
+                    piece v;
+#pragma unroll
+                    for (int i = 0; i < P; ++i) v[i] = from_f32<T>(__builtin_fmaf(scale, sum[s][(h * P + i) / 4][i % 4], to_f32((T)b[i])));
+                    *reinterpret_cast<piece*>(y[s] + n) = v;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < P; ++i)
+                        if (n + i < p.N) y[s][n + i] = from_f32<T>(__builtin_fmaf(scale, sum[s][(h * P + i) / 4][i % 4], to_f32(base[s][n + i])));
+                }
+            }
+        }
+    };
+    Fetched one, two;
+    fetch(one, first);
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) h[s][t].set(sums_of(m[s], t));
+    for (int block = first;; block += 2 * stride) {
+        fetch(two, block + stride);
+        finish(one, block);
+        if (block + stride >= p.blocks) break;
+        fetch(one, block + 2 * stride);
+        finish(two, block + stride);
+        if (block + 2 * stride >= p.blocks) break;
+    }
+}
+template <typename T, int RT, bool WIDE, int S>
+__device__ inline void up_passes(const LoraParams& p, int a, const int (&m)[S], const bool (&on)[S], int first, int stride) {
+    const int tiles = (rank_of(p, a) + 15) / 16;
+    // (with one sixteen in the pool nothing waits for the rank: what is there is multiplied, and left if the adapter has none)
+    if (RT == 1) up_pass<T, 1, false, WIDE, S>(p, a, tiles, m, on, first, stride);
+    else if (tiles == 0) up_pass<T, 0, false, WIDE, S>(p, a, tiles, m, on, first, stride);
+    else if (tiles == 1) up_pass<T, 1, false, WIDE, S>(p, a, tiles, m, on, first, stride);
+    else if (tiles == 2) up_pass<T, (RT > 1 ? 2 : 1), false, WIDE, S>(p, a, tiles, m, on, first, stride);
+    else if (tiles == 3) up_pass<T, (RT > 2 ? 3 : 1), false, WIDE, S>(p, a, tiles, m, on, first, stride);
+    else if (RT > 2) up_pass<T, (RT > 2 ? 4 : 1), true, WIDE, S>(p, a, tiles, m, on, first, stride);
+}
+// Rows without an adapter: as they are.
+template <typename T, bool WIDE>
+__device__ inline void copy_row(const LoraParams& p, int m, bool on, int first, int stride) {
+    constexpr int P = kPiece<T>;
+    if (!on || m >= p.M) return;
+    const T* const base = static_cast<const T*>(p.base) + (int64_t)m * p.ldb;
+    T* const y = static_cast<T*>(p.Y) + (int64_t)m * p.ldy;
+    for (int block = first; block < p.blocks; block += stride) {
+#pragma unroll
+        for (int h = 0; h < 16 / P; ++h) {
+            const int n = block * kLoraColumns + column_of<T>((threadIdx.x & 63) >> 4, h * P);
+            if (WIDE && n + P <= p.N) *reinterpret_cast<v4u*>(y + n) = *reinterpret_cast<const v4u*>(base + n);
+            else
+                for (int i = n; i < min(n + P, p.N); ++i) y[i] = base[i];
+        }
+    }
+}
+
+// Y, 16 rows to a wavefront.  RT: the most sixteens of ranks whose sums it keeps.
 template <typename T, int RT, bool WIDE>
 __global__ __launch_bounds__(kLoraWaves * 64) void lora_up_kernel(const LoraParams p) {
-    constexpr int P = kPiece<T>, kPieces = 16 / P;
-    typedef T piece __attribute__((ext_vector_type(P)));
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = lane >> 4;
-    const int tile = p.by_rows ? blockIdx.y * kLoraWaves + wave : blockIdx.y, m0 = tile * kLoraRows;
-    const int first = p.by_rows ? blockIdx.x : blockIdx.x * kLoraWaves + wave, stride = p.by_rows ? gridDim.x : gridDim.x * kLoraWaves;
-    if (tile >= p.tiles || first >= p.blocks) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m0 = blockIdx.y * kLoraRows, first = blockIdx.x * kLoraWaves + wave, stride = gridDim.x * kLoraWaves;
+    if (first >= p.blocks) return;
     const int mine = adapter_of(p, m0);
     for_adapters(mine, blockIdx.z, p.slots, p.base != p.Y, [&](int a) __attribute__((always_inline)) {
-        const uint32_t rows = (uint32_t)__ballot(mine == a) & 0xffffu;
-        const int m = m0 + (mine == a ? lane & 15 : __builtin_ctz(rows));
-        const bool on = mine == a && m < p.M;
-        const T* const base = static_cast<const T*>(p.base) + (int64_t)min(m, p.M - 1) * p.ldb;
-        T* const y = static_cast<T*>(p.Y) + (int64_t)min(m, p.M - 1) * p.ldy;
-        if (a < 0) {   // rows without an adapter: as they are
-            for (int block = first; on && block < p.blocks; block += stride) {
-#pragma unroll
-                for (int h = 0; h < kPieces; ++h) {
-                    const int n = block * kLoraColumns + column_of<T>(kg, h * P);
-                    if (WIDE && n + P <= p.N) *reinterpret_cast<v4u*>(y + n) = *reinterpret_cast<const v4u*>(base + n);
-                    else
-                        for (int i = n; i < min(n + P, p.N); ++i) y[i] = base[i];
-                }
-            }
+        if (a < 0) {
+            copy_row<T, WIDE>(p, m0 + (lane & 15), mine < 0, first, stride);
             return;
         }
-        const Sixteen<T>* const up = reinterpret_cast<const Sixteen<T>*>(p.up) + (int64_t)a * p.blocks * p.rank_tiles * 64 + lane;
-        auto sums_of = [&](int t) __attribute__((always_inline)) {
-            const v4f* const at = reinterpret_cast<const v4f*>(p.sums + (int64_t)m * (16 * p.rank_tiles) + 16 * t + 4 * kg);
-            const int64_t step = (int64_t)p.M * 4 * p.rank_tiles;
-            v4f v = {0, 0, 0, 0};
-            for (int s = 0; s < p.splits; s += 4) {
-                v4f part[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) part[i] = at[min(s + i, p.splits - 1) * step];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v += s + i < p.splits ? part[i] : v4f{0, 0, 0, 0};
-            }
-            return v;
-        };
-        const float scale = p.scale[a];
-        const int tiles = (rank_of(p, a) + 15) / 16;
-        auto some = [&](auto nt) __attribute__((always_inline)) {
-            constexpr int NT = decltype(nt)::value;
-            struct Fetched {
-                Sixteen<T> up[NT < 1 ? 1 : NT];
-                v4u base[kPieces];
-            };
-            auto fetch = [&](Fetched& f, int block) __attribute__((always_inline)) {
-                block = min(block, p.blocks - 1);
-                if constexpr (WIDE) {
-#pragma unroll
-                    for (int h = 0; h < kPieces; ++h) f.base[h] = *reinterpret_cast<const v4u*>(base + max(min(block * kLoraColumns + column_of<T>(kg, h * P), p.N - P) & ~(P - 1), 0));
-                }
-#pragma unroll
-                for (int t = 0; t < NT; ++t) f.up[t].load(reinterpret_cast<const T*>(up + ((int64_t)block * p.rank_tiles + t) * 64));
-            };
-            auto finish = [&](const Fetched& f, int block, const v4f (&h)[NT < 1 ? 1 : NT]) __attribute__((always_inline)) {
-                v4f sum[4];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) sum[t] = v4f{0, 0, 0, 0};
-                auto multiply = [&](const Sixteen<T>& w, v4f v) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int t = 0; t < 4; ++t) sum[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[4 * t + i], v[i], sum[t], 0, 0, 0);
-                };
-#pragma unroll
-                for (int t = 0; t < NT; ++t) multiply(f.up[t], h[t]);
-                if constexpr (NT == RT)
-                    for (int t = RT; t < tiles; ++t) {
-                        Sixteen<T> w;
-                        w.load(reinterpret_cast<const T*>(up + ((int64_t)block * p.rank_tiles + t) * 64));
-                        multiply(w, sums_of(t));
-                    }
-                wait_for_products();
-                if (!on) return;
-#pragma unroll
-                for (int h = 0; h < kPieces; ++h) {
-                    const int n = block * kLoraColumns + column_of<T>(kg, h * P);
-                    if (WIDE && n + P <= p.N) {
-                        const piece b = __builtin_bit_cast(piece, f.base[h]);
-                        piece v;
-#pragma unroll
-                        for (int i = 0; i < P; ++i) v[i] = from_f32<T>(__builtin_fmaf(scale, sum[(h * P + i) / 4][i % 4], to_f32((T)b[i])));
-                        *reinterpret_cast<piece*>(y + n) = v;
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < P; ++i)
-                            if (n + i < p.N) y[n + i] = from_f32<T>(__builtin_fmaf(scale, sum[(h * P + i) / 4][i % 4], to_f32(base[n + i])));
-                    }
-                }
-            };
-            Fetched one, two;
-            fetch(one, first);
-            v4f h[NT < 1 ? 1 : NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) h[t] = sums_of(t);
-            for (int block = first;; block += 2 * stride) {
-                fetch(two, block + stride);
-                finish(one, block, h);
-                if (block + stride >= p.blocks) break;
-                fetch(one, block + 2 * stride);
-                finish(two, block + stride, h);
-                if (block + 2 * stride >= p.blocks) break;
-            }
-        };
-        if (tiles == 0) some(std::integral_constant<int, 0>());
-        else if (RT == 1 || tiles == 1) some(std::integral_constant<int, 1>());
-        else if (RT == 2 || tiles == 2) some(std::integral_constant<int, (RT < 2 ? 1 : 2)>());
-        else if (RT == 3 || tiles == 3) some(std::integral_constant<int, (RT < 3 ? 1 : 3)>());
-        else some(std::integral_constant<int, (RT < 4 ? 1 : 4)>());
+        const bool on[1] = {mine == a};
+        const int m[1] = {m0 + (mine == a ? lane & 15 : __builtin_ctz((uint32_t)__ballot(mine == a) & 0xffffu))};
+        up_passes<T, RT, WIDE, 1>(p, a, m, on, first, stride);
     });
+}
+// Y, 64 rows to a wavefront, which share what it reads of `up`: S times 16 of them at once where all of these sixteens have rows of the adapter.
+template <typename T, int RT, int S>
+__global__ __launch_bounds__(kLoraWaves * 64) void lora_up_rows_kernel(const LoraParams p) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m0 = blockIdx.y * 64, first = blockIdx.x * kLoraWaves + wave, stride = gridDim.x * kLoraWaves;
+    if (first >= p.blocks) return;
+    int mine = m0 + lane < p.M ? p.ids[m0 + lane] : -1;
+    if (mine >= p.adapters) mine = -1;
+    unsigned long long left = __ballot(mine >= 0);
+    if (p.base != p.Y && left != ~0ull)
+        for (int s = 0; s < 4; ++s) copy_row<T, true>(p, m0 + 16 * s + (lane & 15), __shfl(mine, 16 * s + (lane & 15)) < 0, first, stride);
+    while (left) {
+        const int a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
+        const unsigned long long rows = __ballot(mine == a);
+        left &= ~rows;
+        auto place = [&](int s, int* m, bool* on) __attribute__((always_inline)) {
+            const uint32_t these = (uint32_t)(rows >> (16 * s)) & 0xffffu;
+            *on = these >> (lane & 15) & 1;
+            *m = m0 + 16 * s + (*on ? lane & 15 : __builtin_ctz(these));
+        };
+        for (int s0 = 0; s0 < 4; s0 += S) {
+            bool all = true;
+#pragma unroll
+            for (int s = 0; s < S; ++s) all = all && (rows >> (16 * (s0 + s)) & 0xffffu);
+            if (all) {
+                int m[S];
+                bool on[S];
+#pragma unroll
+                for (int s = 0; s < S; ++s) place(s0 + s, &m[s], &on[s]);
+                up_passes<T, RT, true, S>(p, a, m, on, first, stride);
+                continue;
+            }
+            for (int s = s0; s < s0 + S; ++s) {
+                if (!(rows >> (16 * s) & 0xffffu)) continue;
+                int m[1];
+                bool on[1];
+                place(s, &m[0], &on[0]);
+                up_passes<T, RT, true, 1>(p, a, m, on, first, stride);
+            }
+        }
+    }
 }
 
 // An adapter into its place: one thread for each element of the layout, zeros where the adapter has none.
@@ -393,22 +516,30 @@ void launch_load(const abft_lora_t* L, int slot, const void* A, int64_t lda, con
 template <typename T>
 void launch_gemv(const LoraParams& p, const LoraCut& c, hipStream_t s) {
     const dim3 threads(kLoraWaves * 64), down((unsigned)c.slots, (unsigned)c.tiles, (unsigned)c.splits);
-    if (p.rank_tiles == 1) lora_down_kernel<T, 1><<<down, threads, 0, s>>>(p);
-    else if (p.rank_tiles == 2) lora_down_kernel<T, 2><<<down, threads, 0, s>>>(p);
-    else lora_down_kernel<T, 4><<<down, threads, 0, s>>>(p);
-    // enough wavefronts to fill the chip, and no more columns to one than that leaves
-    const int64_t rows = c.by_rows ? (c.tiles + kLoraWaves - 1) / kLoraWaves : c.tiles, most = c.by_rows ? p.blocks : (p.blocks + kLoraWaves - 1) / kLoraWaves;
-    int64_t columns = (kLoraUpGroups + rows * c.slots - 1) / (rows * c.slots);
-    if (columns > most) columns = most;
-    const dim3 up((unsigned)columns, (unsigned)rows, (unsigned)c.slots);
-    auto launch = [&](auto wide) {
-        constexpr bool W = decltype(wide)::value;
-        if (p.rank_tiles == 1) lora_up_kernel<T, 1, W><<<up, threads, 0, s>>>(p);
-        else if (p.rank_tiles == 2) lora_up_kernel<T, 2, W><<<up, threads, 0, s>>>(p);
-        else lora_up_kernel<T, 4, W><<<up, threads, 0, s>>>(p);
+    auto launch_down = [&](auto rt) {
+        constexpr int RT = decltype(rt)::value;
+        if (c.waves == 2 * kLoraWaves) lora_down_kernel<T, RT, 2 * kLoraWaves><<<down, dim3(2 * kLoraWaves * 64), 0, s>>>(p);
+        else lora_down_kernel<T, RT, kLoraWaves><<<down, threads, 0, s>>>(p);
     };
-    if (p.wide) launch(std::true_type());
-    else launch(std::false_type());
+    const bool by_rows = c.by_rows && p.wide;
+    // enough wavefronts to fill the chip, and no more columns to one than that leaves
+    const int64_t rows = by_rows ? (p.M + 63) / 64 : (int64_t)c.tiles * c.slots, most = (p.blocks + kLoraWaves - 1) / kLoraWaves;
+    int64_t columns = (c.up_groups + rows - 1) / rows;
+    if (columns > most) columns = most;
+    const dim3 up = by_rows ? dim3((unsigned)columns, (unsigned)rows) : dim3((unsigned)columns, (unsigned)c.tiles, (unsigned)c.slots);
+    auto launch_up = [&](auto rt) {
+        constexpr int RT = decltype(rt)::value;
+        if (by_rows) lora_up_rows_kernel<T, RT, (RT > 2 ? 1 : 2)><<<up, threads, 0, s>>>(p);
+        else if (p.wide) lora_up_kernel<T, RT, true><<<up, threads, 0, s>>>(p);
+        else lora_up_kernel<T, RT, false><<<up, threads, 0, s>>>(p);
+    };
+    auto launch = [&](auto rt) {
+        launch_down(rt);
+        launch_up(rt);
+    };
+    if (p.rank_tiles == 1) launch(std::integral_constant<int, 1>());
+    else if (p.rank_tiles == 2) launch(std::integral_constant<int, 2>());
+    else launch(std::integral_constant<int, 4>());
 }
 
 }  // namespace
@@ -488,8 +619,6 @@ int abft_lora_gemv(const void* X, int64_t ldx, int M, const abft_lora_t* pool, c
     p.blocks = (int)abft::blocks_of(pool);
     p.splits = c.splits;
     p.slots = c.slots;
-    p.tiles = c.tiles;
-    p.by_rows = c.by_rows;
     p.wide = ((at | (uintptr_t)ldb * es | (uintptr_t)ldy * es) & 15) == 0 && (uintptr_t)pool->N * es >= 16;
     hipStream_t s = (hipStream_t)stream;
     if (pool->type == ABFT_TYPE_F32) abft::launch_gemv<float>(p, c, s);
