@@ -29,7 +29,7 @@ struct CacheParams {
 };
 
 constexpr int kNT = 256;
-constexpr int kMaxWindow = 16, kMaxBlock = 128, kMaxAhead = kMaxWindow + kMaxBlock + 1;
+constexpr int kMaxWindow = 64, kMaxBlock = 128, kMaxAhead = kMaxWindow + kMaxBlock + 1;
 
 // Eight columns of a token, as they are stored.
 template <typename T>
@@ -174,14 +174,20 @@ __device__ inline void store_unit(const CacheParams& p, const Eight<T> (&v)[U], 
     }
 }
 
-// The tokens of a run, as they are.
+// The tokens of a run, as they are.  kSets: how many times 8 columns a lane has of a token where runs are long; column(c, set): where those of its
+// c-th place begin.
 template <typename T, bool WIDE>
 struct Rows {
     typedef T Kept;
     static constexpr bool kWide = WIDE;
+    static constexpr int kSets = 1;
     const T* x;
     int64_t stride;
     __device__ inline void load(Eight<T>& e, int token, int d, int dim) const { load_eight<T, WIDE>(e, x + (int64_t)token * stride, d, dim); }
+    __device__ inline int column(int c, int) const { return 8 * c; }
+    typedef Eight<T> Raw;   // what is loaded of a token, and what becomes of it
+    __device__ inline void fetch(Raw& raw, int token, int c, int dim) const { load(raw, token, 8 * c, dim); }
+    __device__ inline void make(const Raw& raw, Eight<T>* const (&e)[1], int) const { *e[0] = raw; }
 };
 
 // A run of n tokens, whose slots begin at token `first` of a block, by one wavefront.  codes: of the block and head.
@@ -194,13 +200,26 @@ __device__ inline void append_run(const CacheParams& p, const Source& src, int8_
     const float old = first > 0 ? *scale_at : 0.0f;
     const bool few = !WIDE || items <= 64;
     // Few tokens (and rows that are read by elements): a lane has 8 columns of a token, as often as it takes.  Else it has units of U
-    // tokens of a group and 8 columns, mostly one.
-    const int units = p.block / U * pieces;
-    Eight<T> e, v[U];
+    // tokens of a group and 8 columns (or kSets times 8), mostly one.
+    constexpr int kSets = Source::kSets;
+    const int places = (pieces + kSets - 1) / kSets, units = p.block / U * places;
+    Eight<T> e, v[kSets][U];
     // (every token of a unit is loaded, from rows that exist, so that the loads go out together)
-    auto load = [&](int o, int d) __attribute__((always_inline)) {
+    auto load = [&](int o, int c) __attribute__((always_inline)) {
+        constexpr int kTogether = kSets == 1 || U < 4 ? U : 4;
 #pragma unroll
-        for (int j = 0; j < U; ++j) src.load(v[j], min(max(o + j - first, 0), n - 1), d, p.dim);
+        for (int j0 = 0; j0 < U; j0 += kTogether) {
+            typename Source::Raw raw[kTogether];
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j) src.fetch(raw[j], min(max(o + j0 + j - first, 0), n - 1), c, p.dim);
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j) {
+                Eight<T>* to[kSets];
+#pragma unroll
+                for (int s = 0; s < kSets; ++s) to[s] = &v[s][j0 + j];
+                src.make(raw[j], to, c);
+            }
+        }
     };
     uint32_t most = 0;
     if (few) {
@@ -212,11 +231,13 @@ __device__ inline void append_run(const CacheParams& p, const Source& src, int8_
     } else if constexpr (WIDE) {
 #pragma unroll 1
         for (int u = lane; u < units; u += 64) {
-            const int o = u / pieces * U, d = u % pieces * 8;
+            const int o = u / places * U;
             if (o + U <= first || o >= first + n) continue;
-            load(o, d);
+            load(o, u % places);
 #pragma unroll
-            for (int j = 0; j < U; ++j) most = max_bits(most, v[j]);
+            for (int s = 0; s < kSets; ++s)
+#pragma unroll
+                for (int j = 0; j < U; ++j) most = max_bits(most, v[s][j]);
         }
     }
     // (as bits: those of an infinity or a NaN are above all others, where a maximum of floats would pass a NaN by)
@@ -270,11 +291,16 @@ __device__ inline void append_run(const CacheParams& p, const Source& src, int8_
     } else if constexpr (WIDE) {
 #pragma unroll 1
         for (int u = lane; u < units; u += 64) {
-            const int o = u / pieces * U, d = u % pieces * 8;
+            const int o = u / places * U;
             if (o + U <= first || o >= first + n) continue;
-            if (units > 64) load(o, d);   // (with one unit to a lane it is there)
-            if (finite) store_unit<T, VALUES, true, U>(p, v, codes, o, d, first, n, r);
-            else store_unit<T, VALUES, false, U>(p, v, codes, o, d, first, n, r);
+            if (units > 64) load(o, u % places);   // (with one unit to a lane it is there)
+#pragma unroll
+            for (int s = 0; s < kSets; ++s) {
+                const int d = src.column(u % places, s);
+                if (kSets > 1 && d >= p.dim) continue;
+                if (finite) store_unit<T, VALUES, true, U>(p, v[s], codes, o, d, first, n, r);
+                else store_unit<T, VALUES, false, U>(p, v[s], codes, o, d, first, n, r);
+            }
         }
     }
 }
@@ -354,10 +380,10 @@ inline int fill(CacheParams& p, const char* fn, const abft_kv_cache_t* c, const 
 // workgroups; of more tokens most lie inside runs, and the workgroups that find none would hold up the others (us, 1 / 2 / 4 / 8 /
 // 16 tokens: 6000 of one request 94 / 86 / 30 / 16 / 11, 64 single tokens 4.2 / 4.8 / 7.3 / 11.8 / 21, 1169 of 40 requests 8.8 / 8.2 / 8.7 /
 // 10.6 / 12.6).
-inline int append_window(const CacheParams& p) {
+inline int append_window(const CacheParams& p, int64_t groups = 2048, int most = 16) {
     const int64_t all = p.n_tokens * ((p.heads + kAppendHeads - 1) / kAppendHeads);
     int window = 1;
-    while (window < kMaxWindow && all > 2048ll * window) window *= 2;
+    while (window < most && all > groups * window) window *= 2;
     return window;
 }
 // So few tokens to a lane's units that a block has one for every lane, if it can (us with the read behind, 16 tokens / the rule: 6000 tokens of

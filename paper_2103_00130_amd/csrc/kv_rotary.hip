@@ -42,12 +42,12 @@ __device__ inline void load_angles(float (&cs)[8], float (&sn)[8], const float* 
     }
 }
 
-// The keys of a run, turned.  WIDE: rows of keys are whole aligned pieces of 8 columns, and so are the columns that turn (either half of them,
-// unless neighbours turn).
+// The keys of a run, turned.  WIDE: rows of keys are whole aligned pieces of 8 columns, and the columns that turn are eights of pairs.
 template <typename T, bool WIDE, bool NEIGHBOURS>
 struct Turned {
     typedef float Kept;
     static constexpr bool kWide = WIDE;
+    static constexpr int kSets = 2;   // of long runs a lane has both sides of 8 pairs
     const T* x;
     int64_t stride;
     const float* table;
@@ -102,6 +102,40 @@ struct Turned {
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) e.w[k] = __builtin_bit_cast(uint32_t, y[k]);
+    }
+    // Both sides of the c-th 8 pairs; of columns that do not turn the next sixteen (the last may be eight).  (halves: rot is a multiple of 16)
+    __device__ inline int column(int c, int set) const {
+        return NEIGHBOURS || 16 * c >= rot ? 16 * c + 8 * set : 8 * c + (set ? rot / 2 : 0);
+    }
+    struct Raw {
+        Eight<T> a, b;
+        float cs[8], sn[8];
+    };
+    __device__ inline void fetch(Raw& raw, int token, int c, int dim) const {
+        const T* const row = x + (int64_t)token * stride;
+        load_eight<T, true>(raw.a, row, column(c, 0), dim);
+        load_eight<T, true>(raw.b, row, min(column(c, 1), dim - 8), dim);
+        load_angles(raw.cs, raw.sn, table + (int64_t)positions[token] * rot, rot / 2, min(8 * c, rot / 2 - 8));
+    }
+    __device__ inline void make(const Raw& raw, Eight<float>* const (&e)[2], int c) const {
+        const Eight<T>&a = raw.a, &b = raw.b;
+        const float(&cs)[8] = raw.cs, (&sn)[8] = raw.sn;
+        // (columns that do not turn are left by what is chosen, not by a cosine of one: an infinity times a sine of zero is no number)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if constexpr (NEIGHBOURS) {
+                // (k-th pair: columns 2k and 2k + 1 of the sixteen; rot may end inside them)
+                const float u0 = k < 4 ? value_of(a, 2 * (k % 4)) : value_of(b, 2 * (k % 4)), u1 = k < 4 ? value_of(a, 2 * (k % 4) + 1) : value_of(b, 2 * (k % 4) + 1);
+                const bool turns = 16 * c + 2 * k < rot;
+                (k < 4 ? e[0] : e[1])->w[2 * (k % 4)] = __builtin_bit_cast(uint32_t, turns ? u0 * cs[k] - u1 * sn[k] : u0);
+                (k < 4 ? e[0] : e[1])->w[2 * (k % 4) + 1] = __builtin_bit_cast(uint32_t, turns ? u1 * cs[k] + u0 * sn[k] : u1);
+            } else {
+                const float u0 = value_of(a, k), u1 = value_of(b, k);
+                const bool turns = 16 * c < rot;
+                e[0]->w[k] = __builtin_bit_cast(uint32_t, turns ? u0 * cs[k] - u1 * sn[k] : u0);
+                e[1]->w[k] = __builtin_bit_cast(uint32_t, turns ? u1 * cs[k] + u0 * sn[k] : u1);
+            }
+        }
     }
 };
 
@@ -170,9 +204,18 @@ __device__ inline void turn_queries(const RotaryParams& p, int group) {
             }
         } else {
             const int d = p.rot + (piece - pairs) * unit;
-            for (int h = head0; h < min(head0 + (WIDE ? kQueryHeads : 1), p.q_heads); ++h) {
-                if constexpr (WIDE) *reinterpret_cast<Eight<T>*>(r + (int64_t)h * p.r_head + d) = *reinterpret_cast<const Eight<T>*>(q + (int64_t)h * p.q_head + d);
-                else r[h * p.r_head + d] = q[h * p.q_head + d];
+            if constexpr (WIDE) {
+                Eight<T> e[kQueryHeads];
+#pragma unroll
+                for (int h = 0; h < kQueryHeads; ++h) load_eight<T, true>(e[h], q + (int64_t)min(head0 + h, p.q_heads - 1) * p.q_head, d, p.cache.dim);
+#pragma unroll
+                for (int h = 0; h < kQueryHeads; ++h)
+                    if (head0 + h < p.q_heads)
+#pragma unroll
+                        for (int k = 0; k < Eight<T>::kWords / 4; ++k)
+                            reinterpret_cast<v4u*>(r + (int64_t)(head0 + h) * p.r_head + d)[k] = v4u{e[h].w[4 * k], e[h].w[4 * k + 1], e[h].w[4 * k + 2], e[h].w[4 * k + 3]};
+            } else {
+                r[head0 * p.r_head + d] = q[head0 * p.q_head + d];
             }
         }
     }
@@ -199,7 +242,7 @@ __global__ __launch_bounds__(kAppendWaves * 64) void kv_append_rotary_kernel(con
             const T* const x = static_cast<const T*>(s.x) + t * s.token_stride + head * s.head_stride;
             int8_t* const codes = s.codes + (block * c.heads + head) * c.block * c.cols;
             float* const scale_at = s.scale + block * c.heads + head;
-            if (side == 0) append_run<Turned<T, WIDE, NEIGHBOURS>, false, (U < 8 ? U : 8)>(c, Turned<T, WIDE, NEIGHBOURS>{x, s.token_stride, p.table, s_position + at, p.rot}, codes, scale_at, first, n);
+            if (side == 0) append_run<Turned<T, WIDE, NEIGHBOURS>, false, U / 2>(c, Turned<T, WIDE, NEIGHBOURS>{x, s.token_stride, p.table, s_position + at, p.rot}, codes, scale_at, first, n);
             else append_run<Rows<T, WIDE>, true, U>(c, Rows<T, WIDE>{x, s.token_stride}, codes, scale_at, first, n);
         });
 }
@@ -253,12 +296,12 @@ extern "C" int abft_kv_append_rotary(const abft_kv_cache_t* cache, const void* Q
     p.n_positions = n_positions;
     p.rot = rot_dim;
     p.in_place = Q == QR;
-    c.window = abft::append_window(c);
+    c.window = abft::append_window(c, 512, 64);
     const bool neighbours = pairs == ABFT_ROTARY_NEIGHBOURS;
-    const bool angles = (reinterpret_cast<uintptr_t>(table) & 15) == 0 && rot_dim % 8 == 0;   // pieces of four of a row's cosines and sines, aligned
-    const bool wide = c.side[0].wide && c.side[1].wide && angles && (neighbours || rot_dim % 16 == 0);
+    const bool angles = (reinterpret_cast<uintptr_t>(table) & 15) == 0 && rot_dim % 16 == 0;   // eight pairs at a time, their cosines and sines aligned
+    const bool wide = c.side[0].wide && c.side[1].wide && angles;
     const bool wide_q = q_heads > 0 && abft::pieces_aligned(Q, q_token_stride, q_head_stride, c.dim, type) &&
-                        abft::pieces_aligned(QR, qr_token_stride, qr_head_stride, c.dim, type) && angles && rot_dim % 16 == 0;
+                        abft::pieces_aligned(QR, qr_token_stride, qr_head_stride, c.dim, type) && angles;
     p.key_groups = (c.heads + abft::kAppendHeads - 1) / abft::kAppendHeads;
     // so many workgroups for the queries of a window that a thread has one item, or a few
     const int64_t unit = wide_q ? 8 : 1, items = (int64_t)c.window * (wide_q ? (q_heads + abft::kQueryHeads - 1) / abft::kQueryHeads : q_heads) * (rot_dim / 2 / unit + (p.in_place ? 0 : (c.dim - rot_dim) / unit));
