@@ -48,7 +48,6 @@ struct LoraParams {
     float* sums;     // [split][row][ranks]
     int64_t ldx, ldb, ldy;
     int M, N, K, adapters, max_rank, rank_tiles, chunks, blocks, splits, slots;
-    bool wide;       // rows of base and Y are whole aligned pieces of 16 bytes
 };
 
 template <typename T>
@@ -260,12 +259,13 @@ struct Factor<bf16> {
 
 // Rows S times 16 of one adapter: base plus scale times the product with `up`, for the columns that a wavefront has (64 at a time, a lane 16 of a row).
 // m: the lane's rows, all of which exist; on: which of them are the adapter's, the others being read as they are and left.  NT sixteens of ranks have
-// their sums over K in registers, those of MORE are read anew for all columns.  What the next columns need is on its way while these are
-// multiplied, as above.  WIDE: rows of base and Y are whole aligned pieces of 16 bytes, and there is one at least.
-template <typename T, int NT, bool MORE, bool WIDE, int S>
-__device__ inline void up_pass(const LoraParams& p, int a, int tiles, const int (&m)[S], const bool (&on)[S], int first, int stride) {
+// their sums over K in registers, those of MORE in `more`.  What the next columns need is on its way while these are multiplied, as above.
+// PIECES: a row has 16 bytes at least, so that whatever it has can be read 16 bytes at a time.
+template <typename T, int NT, bool MORE, bool PIECES, int S>
+__device__ inline void up_pass(const LoraParams& p, int a, int tiles, const int (&m)[S], const bool (&on)[S], int first, int stride, v4f* more) {
     constexpr int P = kPiece<T>, kPieces = 16 / P, kKept = NT < 1 ? 1 : NT;
     typedef T piece __attribute__((ext_vector_type(P)));
+    typedef piece piece_any __attribute__((aligned(2)));
     const int lane = threadIdx.x & 63, kg = lane >> 4;
     const Sixteen<T>* const up = reinterpret_cast<const Sixteen<T>*>(p.up) + (int64_t)a * p.blocks * p.rank_tiles * 64 + lane;
     const T* base[S];
@@ -281,13 +281,11 @@ __device__ inline void up_pass(const LoraParams& p, int a, int tiles, const int 
     };
     auto fetch = [&](Fetched& f, int block) __attribute__((always_inline)) {
         block = min(block, p.blocks - 1);
-        if constexpr (WIDE) {
+        if constexpr (PIECES) {
 #pragma unroll
-            for (int h = 0; h < kPieces; ++h) {
-                const int n = max(min(block * kLoraColumns + column_of<T>(kg, h * P), p.N - P) & ~(P - 1), 0);
+            for (int h = 0; h < kPieces; ++h)
 #pragma unroll
-                for (int s = 0; s < S; ++s) f.base[s][h] = *reinterpret_cast<const v4u*>(base[s] + n);
-            }
+                for (int s = 0; s < S; ++s) f.base[s][h] = *reinterpret_cast<const v4u_any*>(base[s] + min(block * kLoraColumns + column_of<T>(kg, h * P), p.N - P));
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) f.up[t].load(reinterpret_cast<const T*>(up + ((int64_t)block * p.rank_tiles + t) * 64));
@@ -323,9 +321,9 @@ __device__ inline void up_pass(const LoraParams& p, int a, int tiles, const int 
                 w.load(reinterpret_cast<const T*>(up + ((int64_t)block * p.rank_tiles + t) * 64));
 #pragma unroll
                 for (int s = 0; s < S; ++s) {
-                    Factor<T> more;
-                    more.set(sums_of(m[s], t));
-                    more.multiply(w, sum[s]);
+                    Factor<T> other;
+                    other.set(more[((t - NT) * S + s) * 64 + lane]);
+                    other.multiply(w, sum[s]);
                 }
             }
         wait_for_products();
@@ -340,12 +338,12 @@ __device__ inline void up_pass(const LoraParams& p, int a, int tiles, const int 
 #pragma unroll
             for (int h = 0; h < kPieces; ++h) {
                 const int n = block * kLoraColumns + column_of<T>(kg, h * P);
-                if (WIDE && n + P <= p.N) {
+                if (PIECES && n + P <= p.N) {
                     const piece b = __builtin_bit_cast(piece, f.base[s][h]);
                     piece v;
 #pragma unroll
                     for (int i = 0; i < P; ++i) v[i] = from_f32<T>(__builtin_fmaf(scale, sum[s][(h * P + i) / 4][i % 4], to_f32((T)b[i])));
-                    *reinterpret_cast<piece*>(y[s] + n) = v;
+                    *reinterpret_cast<piece_any*>(y[s] + n) = v;
                 } else {
 #pragma unroll
                     for (int i = 0; i < P; ++i)
@@ -360,6 +358,10 @@ __device__ inline void up_pass(const LoraParams& p, int a, int tiles, const int 
     for (int s = 0; s < S; ++s)
 #pragma unroll
         for (int t = 0; t < NT; ++t) h[s][t].set(sums_of(m[s], t));
+    if constexpr (MORE)
+        for (int t = NT; t < tiles; ++t)
+#pragma unroll
+            for (int s = 0; s < S; ++s) more[((t - NT) * S + s) * 64 + lane] = sums_of(m[s], t);   // (read back by the lane that writes it)
     for (int block = first;; block += 2 * stride) {
         fetch(two, block + stride);
         finish(one, block);
@@ -369,19 +371,19 @@ __device__ inline void up_pass(const LoraParams& p, int a, int tiles, const int 
         if (block + 2 * stride >= p.blocks) break;
     }
 }
-template <typename T, int RT, bool WIDE, int S>
-__device__ inline void up_passes(const LoraParams& p, int a, const int (&m)[S], const bool (&on)[S], int first, int stride) {
+template <typename T, int RT, bool PIECES, int S>
+__device__ inline void up_passes(const LoraParams& p, int a, const int (&m)[S], const bool (&on)[S], int first, int stride, v4f* more) {
     const int tiles = (rank_of(p, a) + 15) / 16;
     // (with one sixteen in the pool nothing waits for the rank: what is there is multiplied, and left if the adapter has none)
-    if (RT == 1) up_pass<T, 1, false, WIDE, S>(p, a, tiles, m, on, first, stride);
-    else if (tiles == 0) up_pass<T, 0, false, WIDE, S>(p, a, tiles, m, on, first, stride);
-    else if (tiles == 1) up_pass<T, 1, false, WIDE, S>(p, a, tiles, m, on, first, stride);
-    else if (tiles == 2) up_pass<T, (RT > 1 ? 2 : 1), false, WIDE, S>(p, a, tiles, m, on, first, stride);
-    else if (tiles == 3) up_pass<T, (RT > 2 ? 3 : 1), false, WIDE, S>(p, a, tiles, m, on, first, stride);
-    else if (RT > 2) up_pass<T, (RT > 2 ? 4 : 1), true, WIDE, S>(p, a, tiles, m, on, first, stride);
+    if (RT == 1) up_pass<T, 1, false, PIECES, S>(p, a, tiles, m, on, first, stride, more);
+    else if (tiles == 0) up_pass<T, 0, false, PIECES, S>(p, a, tiles, m, on, first, stride, more);
+    else if (tiles == 1) up_pass<T, 1, false, PIECES, S>(p, a, tiles, m, on, first, stride, more);
+    else if (tiles == 2) up_pass<T, (RT > 1 ? 2 : 1), false, PIECES, S>(p, a, tiles, m, on, first, stride, more);
+    else if (tiles == 3) up_pass<T, (RT > 2 ? 3 : 1), false, PIECES, S>(p, a, tiles, m, on, first, stride, more);
+    else if (RT > 2) up_pass<T, (RT > 2 ? 4 : 1), true, PIECES, S>(p, a, tiles, m, on, first, stride, more);
 }
 // Rows without an adapter: as they are.
-template <typename T, bool WIDE>
+template <typename T, bool PIECES>
 __device__ inline void copy_row(const LoraParams& p, int m, bool on, int first, int stride) {
     constexpr int P = kPiece<T>;
     if (!on || m >= p.M) return;
@@ -391,68 +393,56 @@ __device__ inline void copy_row(const LoraParams& p, int m, bool on, int first, 
 #pragma unroll
         for (int h = 0; h < 16 / P; ++h) {
             const int n = block * kLoraColumns + column_of<T>((threadIdx.x & 63) >> 4, h * P);
-            if (WIDE && n + P <= p.N) *reinterpret_cast<v4u*>(y + n) = *reinterpret_cast<const v4u*>(base + n);
+            if (PIECES && n + P <= p.N) *reinterpret_cast<v4u_any*>(y + n) = *reinterpret_cast<const v4u_any*>(base + n);
             else
                 for (int i = n; i < min(n + P, p.N); ++i) y[i] = base[i];
         }
     }
 }
 
-// Y, 16 rows to a wavefront.  RT: the most sixteens of ranks whose sums it keeps.
-template <typename T, int RT, bool WIDE>
+// Y, ROWS (16 or 32) rows to a wavefront.  RT: the most sixteens of ranks whose sums it keeps in registers.  Both sixteens of 32 rows are taken at
+// once, and share what is read of `up`, where both have rows of the adapter.
+template <typename T, int RT, bool PIECES, int ROWS>
 __global__ __launch_bounds__(kLoraWaves * 64) void lora_up_kernel(const LoraParams p) {
+    constexpr int S = ROWS / 16, kMore = RT == 4 ? kLoraMostRank / 16 - RT : 0;
+    __shared__ v4f s_more[kLoraWaves][kMore ? kMore * S * 64 : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int m0 = blockIdx.y * kLoraRows, first = blockIdx.x * kLoraWaves + wave, stride = gridDim.x * kLoraWaves;
+    const int m0 = blockIdx.y * ROWS, first = blockIdx.x * kLoraWaves + wave, stride = gridDim.x * kLoraWaves;
     if (first >= p.blocks) return;
-    const int mine = adapter_of(p, m0);
-    for_adapters(mine, blockIdx.z, p.slots, p.base != p.Y, [&](int a) __attribute__((always_inline)) {
-        if (a < 0) {
-            copy_row<T, WIDE>(p, m0 + (lane & 15), mine < 0, first, stride);
-            return;
-        }
-        const bool on[1] = {mine == a};
-        const int m[1] = {m0 + (mine == a ? lane & 15 : __builtin_ctz((uint32_t)__ballot(mine == a) & 0xffffu))};
-        up_passes<T, RT, WIDE, 1>(p, a, m, on, first, stride);
-    });
-}
-// Y, 64 rows to a wavefront, which share what it reads of `up`: S times 16 of them at once where all of these sixteens have rows of the adapter.
-template <typename T, int RT, int S>
-__global__ __launch_bounds__(kLoraWaves * 64) void lora_up_rows_kernel(const LoraParams p) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int m0 = blockIdx.y * 64, first = blockIdx.x * kLoraWaves + wave, stride = gridDim.x * kLoraWaves;
-    if (first >= p.blocks) return;
-    int mine = m0 + lane < p.M ? p.ids[m0 + lane] : -1;
-    if (mine >= p.adapters) mine = -1;
-    unsigned long long left = __ballot(mine >= 0);
-    if (p.base != p.Y && left != ~0ull)
-        for (int s = 0; s < 4; ++s) copy_row<T, true>(p, m0 + 16 * s + (lane & 15), __shfl(mine, 16 * s + (lane & 15)) < 0, first, stride);
-    while (left) {
-        const int a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
-        const unsigned long long rows = __ballot(mine == a);
-        left &= ~rows;
-        auto place = [&](int s, int* m, bool* on) __attribute__((always_inline)) {
-            const uint32_t these = (uint32_t)(rows >> (16 * s)) & 0xffffu;
-            *on = these >> (lane & 15) & 1;
-            *m = m0 + 16 * s + (*on ? lane & 15 : __builtin_ctz(these));
-        };
-        for (int s0 = 0; s0 < 4; s0 += S) {
-            bool all = true;
-#pragma unroll
-            for (int s = 0; s < S; ++s) all = all && (rows >> (16 * (s0 + s)) & 0xffffu);
-            if (all) {
-                int m[S];
-                bool on[S];
-#pragma unroll
-                for (int s = 0; s < S; ++s) place(s0 + s, &m[s], &on[s]);
-                up_passes<T, RT, true, S>(p, a, m, on, first, stride);
-                continue;
+    v4f* const more = s_more[wave];
+    const bool copies = p.base != p.Y;
+    if constexpr (S == 1) {
+        const int mine = adapter_of(p, m0);
+        for_adapters(mine, blockIdx.z, p.slots, copies, [&](int a) __attribute__((always_inline)) {
+            if (a < 0) {
+                copy_row<T, PIECES>(p, m0 + (lane & 15), mine < 0, first, stride);
+                return;
             }
-            for (int s = s0; s < s0 + S; ++s) {
-                if (!(rows >> (16 * s) & 0xffffu)) continue;
-                int m[1];
-                bool on[1];
-                place(s, &m[0], &on[0]);
-                up_passes<T, RT, true, 1>(p, a, m, on, first, stride);
+            const bool on[1] = {mine == a};
+            const int m[1] = {m0 + (mine == a ? lane & 15 : __builtin_ctz((uint32_t)__ballot(mine == a) & 0xffffu))};
+            up_passes<T, RT, PIECES, 1>(p, a, m, on, first, stride, more);
+        });
+    } else {
+        const int one = adapter_of(p, m0), two = adapter_of(p, m0 + 16);
+        const int mine = lane & 16 ? two : one;   // of row m0 + lane % 32
+        uint32_t left = (uint32_t)__ballot(mine >= 0);
+        if (copies && left != 0xffffffffu) {
+            copy_row<T, PIECES>(p, m0 + (lane & 15), one < 0, first, stride);
+            copy_row<T, PIECES>(p, m0 + 16 + (lane & 15), two < 0, first, stride);
+        }
+        while (left) {
+            const int a = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
+            const uint32_t rows = (uint32_t)__ballot(mine == a);
+            left &= ~rows;
+            const bool on[2] = {one == a, two == a};
+            const uint32_t low = rows & 0xffffu, high = rows >> 16;
+            const int m[2] = {m0 + (on[0] ? lane & 15 : low ? __builtin_ctz(low) : 0), m0 + 16 + (on[1] ? lane & 15 : high ? __builtin_ctz(high) : 0)};
+            if (low && high) {
+                up_passes<T, RT, PIECES, 2>(p, a, m, on, first, stride, more);
+            } else {
+                const int m1[1] = {low ? m[0] : m[1]};
+                const bool on1[1] = {low ? on[0] : on[1]};
+                up_passes<T, RT, PIECES, 1>(p, a, m1, on1, first, stride, more);
             }
         }
     }
@@ -521,17 +511,16 @@ void launch_gemv(const LoraParams& p, const LoraCut& c, hipStream_t s) {
         if (c.waves == 2 * kLoraWaves) lora_down_kernel<T, RT, 2 * kLoraWaves><<<down, dim3(2 * kLoraWaves * 64), 0, s>>>(p);
         else lora_down_kernel<T, RT, kLoraWaves><<<down, threads, 0, s>>>(p);
     };
-    const bool by_rows = c.by_rows && p.wide;
     // enough wavefronts to fill the chip, and no more columns to one than that leaves
-    const int64_t rows = by_rows ? (p.M + 63) / 64 : (int64_t)c.tiles * c.slots, most = (p.blocks + kLoraWaves - 1) / kLoraWaves;
+    const int64_t rows = c.by_rows ? (p.M + 31) / 32 : (int64_t)c.tiles * c.slots, most = (p.blocks + kLoraWaves - 1) / kLoraWaves;
     int64_t columns = (c.up_groups + rows - 1) / rows;
     if (columns > most) columns = most;
-    const dim3 up = by_rows ? dim3((unsigned)columns, (unsigned)rows) : dim3((unsigned)columns, (unsigned)c.tiles, (unsigned)c.slots);
+    const dim3 up = c.by_rows ? dim3((unsigned)columns, (unsigned)rows) : dim3((unsigned)columns, (unsigned)c.tiles, (unsigned)c.slots);
     auto launch_up = [&](auto rt) {
         constexpr int RT = decltype(rt)::value;
-        if (by_rows) lora_up_rows_kernel<T, RT, (RT > 2 ? 1 : 2)><<<up, threads, 0, s>>>(p);
-        else if (p.wide) lora_up_kernel<T, RT, true><<<up, threads, 0, s>>>(p);
-        else lora_up_kernel<T, RT, false><<<up, threads, 0, s>>>(p);
+        if (p.N < kPiece<T>) lora_up_kernel<T, RT, false, 16><<<dim3(1, (unsigned)c.tiles, (unsigned)c.slots), threads, 0, s>>>(p);
+        else if (c.by_rows) lora_up_kernel<T, RT, true, 32><<<up, threads, 0, s>>>(p);
+        else lora_up_kernel<T, RT, true, 16><<<up, threads, 0, s>>>(p);
     };
     auto launch = [&](auto rt) {
         launch_down(rt);
@@ -619,7 +608,6 @@ int abft_lora_gemv(const void* X, int64_t ldx, int M, const abft_lora_t* pool, c
     p.blocks = (int)abft::blocks_of(pool);
     p.splits = c.splits;
     p.slots = c.slots;
-    p.wide = ((at | (uintptr_t)ldb * es | (uintptr_t)ldy * es) & 15) == 0 && (uintptr_t)pool->N * es >= 16;
     hipStream_t s = (hipStream_t)stream;
     if (pool->type == ABFT_TYPE_F32) abft::launch_gemv<float>(p, c, s);
     else if (pool->type == ABFT_TYPE_F16) abft::launch_gemv<abft::f16>(p, c, s);

@@ -28,7 +28,7 @@ inline LoraCut lora_cut(int64_t M, int K) {
     if (c.slots < 1) c.slots = 1;
     c.by_rows = M >= kLoraManyRows;
     c.waves = M >= kLoraManyRows ? 2 * kLoraWaves : kLoraWaves;
-    c.up_groups = c.by_rows ? 256 : 1024;
+    c.up_groups = c.by_rows ? 512 : 1024;
     const int64_t groups = (int64_t)c.tiles * c.slots, long_k = ((int64_t)K + kLoraStep * c.waves - 1) / (kLoraStep * c.waves);
     int64_t s = groups ? (kLoraWanted + groups - 1) / groups : 1;
     if (s > long_k) s = long_k;
