@@ -418,8 +418,10 @@ __global__ __launch_bounds__(kLoraWaves * 64) void lora_up_kernel(const LoraPara
                 copy_row<T, PIECES>(p, m0 + (lane & 15), mine < 0, first, stride);
                 return;
             }
+            // (the vote is taken by all lanes: inside the choice only those would vote that take that side of it, none for the adapter)
+            const uint32_t rows = (uint32_t)__ballot(mine == a) & 0xffffu;
             const bool on[1] = {mine == a};
-            const int m[1] = {m0 + (mine == a ? lane & 15 : __builtin_ctz((uint32_t)__ballot(mine == a) & 0xffffu))};
+            const int m[1] = {m0 + (mine == a ? lane & 15 : __builtin_ctz(rows))};
             up_passes<T, RT, PIECES, 1>(p, a, m, on, first, stride, more);
         });
     } else {

@@ -76,6 +76,19 @@ def test_the_search_finds_what_it_looks_for():
         "_Zk:\n\tv_mfma_f32_16x16x32_f16 v[0:3], v[4:7], v[8:11], 0\n\ts_nop 7\n\tv_mov_b32_e32 v2, 0\n")
 
 
+def test_no_vote_inside_a_choice():
+    """A ballot on one side of `c ? a : b` is taken by the lanes that come to that side alone.  Such a vote, for the rows that the lanes on the
+    other side had, found none, and the row that was read instead lay ahead of the first."""
+    def votes(text):
+        text = re.sub(r"//[^\n]*|/\*.*?\*/", "", text, flags=re.S)
+        return [s.strip() for s in re.split(r"[;{}]", text) if "?" in s and re.search(r"__ballot|__any|__all|__shfl|readlane", s.split("?", 1)[1])]
+    assert votes("{ const int m = on ? lane : __builtin_ctz(__ballot(on)); }") and votes("x = on ? __shfl(a, 1) : 0;")
+    assert not votes("const auto r = __ballot(on); // ? __ballot\n const int m = on ? lane : __builtin_ctz(r); a = __ballot(b ? c : d) ")
+    for name in ("kv_append.h", *SOURCES):
+        found = votes(open(os.path.join(b.CSRC, name)).read())
+        assert not found, (name, found)
+
+
 @pytest.fixture(scope="module")
 def assembly(tmp_path_factory):
     out = tmp_path_factory.mktemp("asm")
