@@ -100,7 +100,7 @@ __device__ inline int adapter_of(const LoraParams& p, int m0) {
 // The adapters among a tile's rows (and -1, where `none` says so), dealt to `slots` workgroups: to one for each row that has its adapter first, where there
 // are as many, else in turns.
 template <typename F>
-__device__ inline void for_adapters(int mine, int slot, int slots, bool none, const F& f) {
+__device__ __attribute__((always_inline)) inline void for_adapters(int mine, int slot, int slots, bool none, const F& f) {
     uint32_t left = (uint32_t)__ballot(none || mine >= 0) & 0xffffu;
     if (slots == kLoraRows) {
         const int a = __builtin_amdgcn_readlane(mine, slot);
@@ -257,41 +257,34 @@ struct Factor<bf16> {
     }
 };
 
-// Rows S times 16 of one adapter: base plus scale times the product with `up`, for the columns that a wavefront has (64 at a time, a lane 16 of a row).
-// m: the lane's rows, all of which exist; on: which of them are the adapter's, the others being read as they are and left.  NT sixteens of ranks have
-// their sums over K in registers, those of MORE in `more`.  What the next columns need is on its way while these are multiplied, as above.
+// Rows of one adapter: base plus scale times the product with `up`, for the columns that a wavefront has (64 at a time, a lane 16 of a row).
+// m: the lane's row, which exists; on: whether it is the adapter's, others being read as they are and left.  NT sixteens of ranks have their sums over K
+// in registers, those of MORE in `more`.  What the next columns need is on its way while these are multiplied, as above.
 // PIECES: a row has 16 bytes at least, so that whatever it has can be read 16 bytes at a time.
-template <typename T, int NT, bool MORE, bool PIECES, int S>
-__device__ inline void up_pass(const LoraParams& p, int a, int tiles, const int (&m)[S], const bool (&on)[S], int first, int stride, v4f* more) {
+template <typename T, int NT, bool MORE, bool PIECES>
+__device__ __attribute__((always_inline)) inline void up_pass(const LoraParams& p, int a, int tiles, int m, bool on, int first, int last, v4f* more) {
     constexpr int P = kPiece<T>, kPieces = 16 / P, kKept = NT < 1 ? 1 : NT;
     typedef T piece __attribute__((ext_vector_type(P)));
     typedef piece piece_any __attribute__((aligned(2)));
     const int lane = threadIdx.x & 63, kg = lane >> 4;
     const Sixteen<T>* const up = reinterpret_cast<const Sixteen<T>*>(p.up) + (int64_t)a * p.blocks * p.rank_tiles * 64 + lane;
-    const T* base[S];
-    T* y[S];
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-        base[s] = static_cast<const T*>(p.base) + (int64_t)m[s] * p.ldb;
-        y[s] = static_cast<T*>(p.Y) + (int64_t)m[s] * p.ldy;
-    }
+    const T* const base = static_cast<const T*>(p.base) + (int64_t)m * p.ldb;
+    T* const y = static_cast<T*>(p.Y) + (int64_t)m * p.ldy;
     struct Fetched {
         Sixteen<T> up[kKept];
-        v4u base[S][kPieces];
+        v4u base[kPieces];
     };
     auto fetch = [&](Fetched& f, int block) __attribute__((always_inline)) {
-        block = min(block, p.blocks - 1);
+        block = min(block, last - 1);
         if constexpr (PIECES) {
 #pragma unroll
-            for (int h = 0; h < kPieces; ++h)
-#pragma unroll
-                for (int s = 0; s < S; ++s) f.base[s][h] = *reinterpret_cast<const v4u_any*>(base[s] + min(block * kLoraColumns + column_of<T>(kg, h * P), p.N - P));
+            for (int h = 0; h < kPieces; ++h) f.base[h] = *reinterpret_cast<const v4u_any*>(base + min(block * kLoraColumns + column_of<T>(kg, h * P), p.N - P));
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) f.up[t].load(reinterpret_cast<const T*>(up + ((int64_t)block * p.rank_tiles + t) * 64));
     };
-    auto sums_of = [&](int row, int t) __attribute__((always_inline)) {
-        const v4f* const at = reinterpret_cast<const v4f*>(p.sums + (int64_t)row * (16 * p.rank_tiles) + 16 * t + 4 * kg);
+    auto sums_of = [&](int t) __attribute__((always_inline)) {
+        const v4f* const at = reinterpret_cast<const v4f*>(p.sums + (int64_t)m * (16 * p.rank_tiles) + 16 * t + 4 * kg);
         const int64_t step = (int64_t)p.M * 4 * p.rank_tiles;
         v4f v = at[0];
         for (int i = 1; i < p.splits; i += 4) {
@@ -303,93 +296,66 @@ __device__ inline void up_pass(const LoraParams& p, int a, int tiles, const int 
         }
         return v;
     };
-    Factor<T> h[S][kKept];
+    Factor<T> h[kKept];
     const float scale = p.scale[a];
     auto finish = [&](const Fetched& f, int block) __attribute__((always_inline)) {
-        v4f sum[S][4];
+        v4f sum[4];
 #pragma unroll
-        for (int s = 0; s < S; ++s)
+        for (int t = 0; t < 4; ++t) sum[t] = v4f{0, 0, 0, 0};
 #pragma unroll
-            for (int t = 0; t < 4; ++t) sum[s][t] = v4f{0, 0, 0, 0};
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int s = 0; s < S; ++s) h[s][t].multiply(f.up[t], sum[s]);
+        for (int t = 0; t < NT; ++t) h[t].multiply(f.up[t], sum);
         if constexpr (MORE)
             for (int t = NT; t < tiles; ++t) {
                 Sixteen<T> w;
                 w.load(reinterpret_cast<const T*>(up + ((int64_t)block * p.rank_tiles + t) * 64));
-#pragma unroll
-                for (int s = 0; s < S; ++s) {
-                    Factor<T> other;
-                    other.set(more[((t - NT) * S + s) * 64 + lane]);
-                    other.multiply(w, sum[s]);
-                }
+                Factor<T> other;
+                other.set(more[(t - NT) * 64 + lane]);
+                other.multiply(w, sum);
             }
         wait_for_products();
         if (tiles == 0)
 #pragma unroll
-            for (int s = 0; s < S; ++s)
+            for (int t = 0; t < 4; ++t) sum[t] = v4f{0, 0, 0, 0};
+        if (!on) return;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) sum[s][t] = v4f{0, 0, 0, 0};
+        for (int h = 0; h < kPieces; ++h) {
+            const int n = block * kLoraColumns + column_of<T>(kg, h * P);
+            if (PIECES && n + P <= p.N) {
+                const piece b = __builtin_bit_cast(piece, f.base[h]);
+                piece v;
 #pragma unroll
-        for (int s = 0; s < S; ++s) {
-            if (!on[s]) continue;
+                for (int i = 0; i < P; ++i) v[i] = from_f32<T>(__builtin_fmaf(scale, sum[(h * P + i) / 4][i % 4], to_f32((T)b[i])));
+                *reinterpret_cast<piece_any*>(y + n) = v;
+            } else {
 #pragma unroll
-            for (int h = 0; h < kPieces; ++h) {
-                const int n = block * kLoraColumns + column_of<T>(kg, h * P);
-                if (PIECES && n + P <= p.N) {
-                    const piece b = __builtin_bit_cast(piece, f.base[s][h]);
-                    piece v;
-#pragma unroll
-                    for (int i = 0; i < P; ++i) v[i] = from_f32<T>(__builtin_fmaf(scale, sum[s][(h * P + i) / 4][i % 4], to_f32((T)b[i])));
-                    *reinterpret_cast<piece_any*>(y[s] + n) = v;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < P; ++i)
-                        if (n + i < p.N) y[s][n + i] = from_f32<T>(__builtin_fmaf(scale, sum[s][(h * P + i) / 4][i % 4], to_f32(base[s][n + i])));
-                }
+                for (int i = 0; i < P; ++i)
+                    if (n + i < p.N) y[n + i] = from_f32<T>(__builtin_fmaf(scale, sum[(h * P + i) / 4][i % 4], to_f32(base[n + i])));
             }
         }
     };
     Fetched one, two;
     fetch(one, first);
 #pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) h[s][t].set(sums_of(m[s], t));
+    for (int t = 0; t < NT; ++t) h[t].set(sums_of(t));
     if constexpr (MORE)
-        for (int t = NT; t < tiles; ++t)
-#pragma unroll
-            for (int s = 0; s < S; ++s) more[((t - NT) * S + s) * 64 + lane] = sums_of(m[s], t);   // (read back by the lane that writes it)
-    for (int block = first;; block += 2 * stride) {
-        fetch(two, block + stride);
+        for (int t = NT; t < tiles; ++t) more[(t - NT) * 64 + lane] = sums_of(t);   // (read back by the lane that writes it)
+    for (int block = first;; block += 2) {
+        fetch(two, block + 1);
         finish(one, block);
-        if (block + stride >= p.blocks) break;
-        fetch(one, block + 2 * stride);
-        finish(two, block + stride);
-        if (block + 2 * stride >= p.blocks) break;
+        if (block + 1 >= last) break;
+        fetch(one, block + 2);
+        finish(two, block + 1);
+        if (block + 2 >= last) break;
     }
-}
-template <typename T, int RT, bool PIECES, int S>
-__device__ inline void up_passes(const LoraParams& p, int a, const int (&m)[S], const bool (&on)[S], int first, int stride, v4f* more) {
-    const int tiles = (rank_of(p, a) + 15) / 16;
-    // (with one sixteen in the pool nothing waits for the rank: what is there is multiplied, and left if the adapter has none)
-    if (RT == 1) up_pass<T, 1, false, PIECES, S>(p, a, tiles, m, on, first, stride, more);
-    else if (tiles == 0) up_pass<T, 0, false, PIECES, S>(p, a, tiles, m, on, first, stride, more);
-    else if (tiles == 1) up_pass<T, 1, false, PIECES, S>(p, a, tiles, m, on, first, stride, more);
-    else if (tiles == 2) up_pass<T, (RT > 1 ? 2 : 1), false, PIECES, S>(p, a, tiles, m, on, first, stride, more);
-    else if (tiles == 3) up_pass<T, (RT > 2 ? 3 : 1), false, PIECES, S>(p, a, tiles, m, on, first, stride, more);
-    else if (RT > 2) up_pass<T, (RT > 2 ? 4 : 1), true, PIECES, S>(p, a, tiles, m, on, first, stride, more);
 }
 // Rows without an adapter: as they are.
 template <typename T, bool PIECES>
-__device__ inline void copy_row(const LoraParams& p, int m, bool on, int first, int stride) {
+__device__ __attribute__((always_inline)) inline void copy_row(const LoraParams& p, int m, bool on, int first, int last) {
     constexpr int P = kPiece<T>;
     if (!on || m >= p.M) return;
     const T* const base = static_cast<const T*>(p.base) + (int64_t)m * p.ldb;
     T* const y = static_cast<T*>(p.Y) + (int64_t)m * p.ldy;
-    for (int block = first; block < p.blocks; block += stride) {
+    for (int block = first; block < last; ++block) {
 #pragma unroll
         for (int h = 0; h < 16 / P; ++h) {
             const int n = block * kLoraColumns + column_of<T>((threadIdx.x & 63) >> 4, h * P);
@@ -400,54 +366,34 @@ __device__ inline void copy_row(const LoraParams& p, int m, bool on, int first, 
     }
 }
 
-// Y, ROWS (16 or 32) rows to a wavefront.  RT: the most sixteens of ranks whose sums it keeps in registers.  Both sixteens of 32 rows are taken at
-// once, and share what is read of `up`, where both have rows of the adapter.
-template <typename T, int RT, bool PIECES, int ROWS>
+// Y, 16 rows to a wavefront, and columns next to each other.  RT: the most sixteens of ranks whose sums it keeps in registers.
+template <typename T, int RT, bool PIECES>
 __global__ __launch_bounds__(kLoraWaves * 64) void lora_up_kernel(const LoraParams p) {
-    constexpr int S = ROWS / 16, kMore = RT == 4 ? kLoraMostRank / 16 - RT : 0;
-    __shared__ v4f s_more[kLoraWaves][kMore ? kMore * S * 64 : 1];
+    constexpr int kMore = RT == 4 ? kLoraMostRank / 16 - RT : 0;
+    __shared__ v4f s_more[kLoraWaves][kMore ? kMore * 64 : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int m0 = blockIdx.y * ROWS, first = blockIdx.x * kLoraWaves + wave, stride = gridDim.x * kLoraWaves;
-    if (first >= p.blocks) return;
+    const int waves = gridDim.x * kLoraWaves, each = (p.blocks + waves - 1) / waves;
+    const int m0 = blockIdx.y * kLoraRows, first = (blockIdx.x * kLoraWaves + wave) * each, last = min(first + each, p.blocks);
+    if (first >= last) return;
     v4f* const more = s_more[wave];
-    const bool copies = p.base != p.Y;
-    if constexpr (S == 1) {
-        const int mine = adapter_of(p, m0);
-        for_adapters(mine, blockIdx.z, p.slots, copies, [&](int a) __attribute__((always_inline)) {
-            if (a < 0) {
-                copy_row<T, PIECES>(p, m0 + (lane & 15), mine < 0, first, stride);
-                return;
-            }
-            // (the vote is taken by all lanes: inside the choice only those would vote that take that side of it, none for the adapter)
-            const uint32_t rows = (uint32_t)__ballot(mine == a) & 0xffffu;
-            const bool on[1] = {mine == a};
-            const int m[1] = {m0 + (mine == a ? lane & 15 : __builtin_ctz(rows))};
-            up_passes<T, RT, PIECES, 1>(p, a, m, on, first, stride, more);
-        });
-    } else {
-        const int one = adapter_of(p, m0), two = adapter_of(p, m0 + 16);
-        const int mine = lane & 16 ? two : one;   // of row m0 + lane % 32
-        uint32_t left = (uint32_t)__ballot(mine >= 0);
-        if (copies && left != 0xffffffffu) {
-            copy_row<T, PIECES>(p, m0 + (lane & 15), one < 0, first, stride);
-            copy_row<T, PIECES>(p, m0 + 16 + (lane & 15), two < 0, first, stride);
+    const int mine = adapter_of(p, m0);
+    for_adapters(mine, blockIdx.z, p.slots, p.base != p.Y, [&](int a) __attribute__((always_inline)) {
+        if (a < 0) {
+            copy_row<T, PIECES>(p, m0 + (lane & 15), mine < 0, first, last);
+            return;
         }
-        while (left) {
-            const int a = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
-            const uint32_t rows = (uint32_t)__ballot(mine == a);
-            left &= ~rows;
-            const bool on[2] = {one == a, two == a};
-            const uint32_t low = rows & 0xffffu, high = rows >> 16;
-            const int m[2] = {m0 + (on[0] ? lane & 15 : low ? __builtin_ctz(low) : 0), m0 + 16 + (on[1] ? lane & 15 : high ? __builtin_ctz(high) : 0)};
-            if (low && high) {
-                up_passes<T, RT, PIECES, 2>(p, a, m, on, first, stride, more);
-            } else {
-                const int m1[1] = {low ? m[0] : m[1]};
-                const bool on1[1] = {low ? on[0] : on[1]};
-                up_passes<T, RT, PIECES, 1>(p, a, m1, on1, first, stride, more);
-            }
-        }
-    }
+        // (the vote is taken by all lanes: inside the choice only those would vote that take that side of it, none for the adapter)
+        const uint32_t rows = (uint32_t)__ballot(mine == a) & 0xffffu;
+        const bool on = mine == a;
+        const int m = m0 + (on ? lane & 15 : __builtin_ctz(rows));
+        const int tiles = (rank_of(p, a) + 15) / 16;
+        // (with one sixteen in the pool nothing waits for the rank: what is there is multiplied, and left if the adapter has none)
+        if (RT == 1 || tiles == 1) up_pass<T, 1, false, PIECES>(p, a, tiles, m, on, first, last, more);
+        else if (tiles == 0) up_pass<T, 0, false, PIECES>(p, a, tiles, m, on, first, last, more);
+        else if (tiles == 2) up_pass<T, (RT > 1 ? 2 : 1), false, PIECES>(p, a, tiles, m, on, first, last, more);
+        else if (tiles == 3) up_pass<T, (RT > 2 ? 3 : 1), false, PIECES>(p, a, tiles, m, on, first, last, more);
+        else up_pass<T, (RT > 2 ? 4 : 1), (RT > 2), PIECES>(p, a, tiles, m, on, first, last, more);
+    });
 }
 
 // An adapter into its place: one thread for each element of the layout, zeros where the adapter has none.
@@ -513,16 +459,14 @@ void launch_gemv(const LoraParams& p, const LoraCut& c, hipStream_t s) {
         if (c.waves == 2 * kLoraWaves) lora_down_kernel<T, RT, 2 * kLoraWaves><<<down, dim3(2 * kLoraWaves * 64), 0, s>>>(p);
         else lora_down_kernel<T, RT, kLoraWaves><<<down, threads, 0, s>>>(p);
     };
-    // enough wavefronts to fill the chip, and no more columns to one than that leaves
-    const int64_t rows = c.by_rows ? (p.M + 31) / 32 : (int64_t)c.tiles * c.slots, most = (p.blocks + kLoraWaves - 1) / kLoraWaves;
-    int64_t columns = (c.up_groups + rows - 1) / rows;
+    const int64_t rows = (int64_t)c.tiles * c.slots, most = (p.blocks + kLoraWaves - 1) / kLoraWaves;
+    int64_t columns = (kLoraUpGroups + rows - 1) / rows;
     if (columns > most) columns = most;
-    const dim3 up = c.by_rows ? dim3((unsigned)columns, (unsigned)rows) : dim3((unsigned)columns, (unsigned)c.tiles, (unsigned)c.slots);
+    const dim3 up((unsigned)columns, (unsigned)c.tiles, (unsigned)c.slots);
     auto launch_up = [&](auto rt) {
         constexpr int RT = decltype(rt)::value;
-        if (p.N < kPiece<T>) lora_up_kernel<T, RT, false, 16><<<dim3(1, (unsigned)c.tiles, (unsigned)c.slots), threads, 0, s>>>(p);
-        else if (c.by_rows) lora_up_kernel<T, RT, true, 32><<<up, threads, 0, s>>>(p);
-        else lora_up_kernel<T, RT, true, 16><<<up, threads, 0, s>>>(p);
+        if (p.N < kPiece<T>) lora_up_kernel<T, RT, false><<<up, threads, 0, s>>>(p);
+        else lora_up_kernel<T, RT, true><<<up, threads, 0, s>>>(p);
     };
     auto launch = [&](auto rt) {
         launch_down(rt);

@@ -12,23 +12,20 @@ constexpr int kLoraStep = 128;         // columns of X that a wavefront has at a
 constexpr int kLoraWaves = 4;
 constexpr int kLoraMostSplits = 16;
 constexpr int kLoraWanted = 512;       // workgroups of the sums over K
+constexpr int kLoraUpGroups = 1024;    // workgroups of the products with `up`
 constexpr int kLoraFewRows = 128;      // rows up to which any may have an adapter of its own: a workgroup for each
 constexpr int kLoraManyRows = 512;     // rows from which on most tiles are one adapter's
 
 struct LoraCut {
     int tiles, slots, splits;   // tiles of rows; workgroups among which the adapters of a tile are dealt; parts of K
     int waves;                  // of a workgroup of the sums over K
-    bool by_rows;               // 64 rows to a wavefront of the products with `up`
-    int up_groups;              // workgroups of those
 };
 inline LoraCut lora_cut(int64_t M, int K) {
     LoraCut c;
     c.tiles = (int)((M + kLoraRows - 1) / kLoraRows);
     c.slots = M < kLoraRows ? (int)M : M <= kLoraFewRows ? kLoraRows : M < kLoraManyRows ? 8 : 1;
     if (c.slots < 1) c.slots = 1;
-    c.by_rows = M >= kLoraManyRows;
     c.waves = M >= kLoraManyRows ? 2 * kLoraWaves : kLoraWaves;
-    c.up_groups = c.by_rows ? 512 : 1024;
     const int64_t groups = (int64_t)c.tiles * c.slots, long_k = ((int64_t)K + kLoraStep * c.waves - 1) / (kLoraStep * c.waves);
     int64_t s = groups ? (kLoraWanted + groups - 1) / groups : 1;
     if (s > long_k) s = long_k;

@@ -101,6 +101,8 @@ def assembly(tmp_path_factory):
 def test_kernels(assembly, source):
     spills = re.findall(r"\.vgpr_spill_count:\s*(\d+)", assembly[source])
     assert spills and set(spills) == {"0"}
+    # (nor private memory: a function that is not inlined has the kernel's parameters copied there)
+    assert set(re.findall(r"\.private_segment_fixed_size:\s*(\d+)", assembly[source])) == {"0"}
     assert not early_vector_work(assembly[source])
     assert not early_touches(assembly[source])
     assert source != "lora.hip" or "v_mfma" in assembly[source]
