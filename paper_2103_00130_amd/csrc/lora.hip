@@ -120,9 +120,9 @@ __device__ inline int rank_of(const LoraParams& p, int a) { return __builtin_amd
 // Sums over K.  RT: sixteens of ranks that a wavefront holds; an adapter of more is taken in turns.  The next step's loads are on their way while
 // this one's are multiplied, without a branch about them, so that what is awaited is what is multiplied: rows that are not the adapter's are
 // read from a row that is, and their sums left.
-template <typename T, int RT, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void lora_down_kernel(const LoraParams p) {
-    __shared__ v4f s_sum[WAVES][RT][64];
+template <typename T, int RT>
+__global__ __launch_bounds__(kLoraWaves * 64) void lora_down_kernel(const LoraParams p) {
+    __shared__ v4f s_sum[kLoraWaves][RT][64];
     constexpr int kStep = RT > 2 ? 2 : 4;   // chunks of a step
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = lane >> 4;
     const int m0 = blockIdx.y * kLoraRows, mine = adapter_of(p, m0);
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(WAVES * 64) void lora_down_kernel(const LoraParams 
                     for (int t = 0; t < NT; ++t) sum[t] = mma<T>(c0 + c < whole ? f.w[c][t] : none, x, sum[t]);
                 }
             };
-            constexpr int kAll = WAVES * kStep;
+            constexpr int kAll = kLoraWaves * kStep;
             int c0 = begin + wave * kStep;
             if (c0 < whole) {
                 Fetched one, two;
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(WAVES * 64) void lora_down_kernel(const LoraParams 
                     if (c0 + 2 * kAll >= whole) break;
                 }
             }
-            if (wave == WAVES - 1 && whole < end) {
+            if (wave == kLoraWaves - 1 && whole < end) {
                 const int k = whole * kChunkOf<T> + kg * kPiece<T>;
                 const v4u x = load_x<T>(row - kg * kPiece<T>, k, p.K);
 #pragma unroll
@@ -183,10 +183,10 @@ __global__ __launch_bounds__(WAVES * 64) void lora_down_kernel(const LoraParams 
 #pragma unroll
             for (int t = 0; t < NT; ++t) s_sum[wave][t][lane] = sum[t];
             __syncthreads();
-            for (int t = wave; t < NT; t += WAVES) {
+            for (int t = wave; t < NT; t += kLoraWaves) {
                 v4f y = s_sum[0][t][lane];
 #pragma unroll
-                for (int w = 1; w < WAVES; ++w) y += s_sum[w][t][lane];
+                for (int w = 1; w < kLoraWaves; ++w) y += s_sum[w][t][lane];
                 if (mine == a) *reinterpret_cast<v4f*>(p.sums + ((int64_t)blockIdx.z * p.M + m0 + (lane & 15)) * (16 * p.rank_tiles) + 16 * (t0 + t) + 4 * kg) = y;
             }
             __syncthreads();
@@ -454,23 +454,15 @@ void launch_load(const abft_lora_t* L, int slot, const void* A, int64_t lda, con
 template <typename T>
 void launch_gemv(const LoraParams& p, const LoraCut& c, hipStream_t s) {
     const dim3 threads(kLoraWaves * 64), down((unsigned)c.slots, (unsigned)c.tiles, (unsigned)c.splits);
-    auto launch_down = [&](auto rt) {
-        constexpr int RT = decltype(rt)::value;
-        if (c.waves == 2 * kLoraWaves) lora_down_kernel<T, RT, 2 * kLoraWaves><<<down, dim3(2 * kLoraWaves * 64), 0, s>>>(p);
-        else lora_down_kernel<T, RT, kLoraWaves><<<down, threads, 0, s>>>(p);
-    };
     const int64_t rows = (int64_t)c.tiles * c.slots, most = (p.blocks + kLoraWaves - 1) / kLoraWaves;
     int64_t columns = (kLoraUpGroups + rows - 1) / rows;
     if (columns > most) columns = most;
     const dim3 up((unsigned)columns, (unsigned)c.tiles, (unsigned)c.slots);
-    auto launch_up = [&](auto rt) {
+    auto launch = [&](auto rt) {
         constexpr int RT = decltype(rt)::value;
+        lora_down_kernel<T, RT><<<down, threads, 0, s>>>(p);
         if (p.N < kPiece<T>) lora_up_kernel<T, RT, false><<<up, threads, 0, s>>>(p);
         else lora_up_kernel<T, RT, true><<<up, threads, 0, s>>>(p);
-    };
-    auto launch = [&](auto rt) {
-        launch_down(rt);
-        launch_up(rt);
     };
     if (p.rank_tiles == 1) launch(std::integral_constant<int, 1>());
     else if (p.rank_tiles == 2) launch(std::integral_constant<int, 2>());
