@@ -7,6 +7,8 @@
 // their own: a thread has 8 pairs (or 8 columns that do not turn) of up to four heads of a token, whose cosines and sines it loads once.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "kv_append.h"
 
 namespace abft {
@@ -42,11 +44,96 @@ __device__ inline void load_angles(float (&cs)[8], float (&sn)[8], const float* 
     }
 }
 
-// The keys of a run, turned.  WIDE: rows of keys are whole aligned pieces of 8 columns, and the columns that turn are eights of pairs.
-template <typename T, bool WIDE, bool NEIGHBOURS>
-struct Turned {
+// How rows are read: by elements; by aligned pieces of 8 columns; and that way where the columns that turn are eights of pairs, whose cosines and
+// sines are aligned as well.
+enum { kElements, kPieces, kPairs };
+
+// The column that turns with column c, and its pair; where c does not turn c itself, and any pair.
+template <bool NEIGHBOURS>
+__device__ inline void partner_of(int c, int rot, int* other, int* pair, bool* front) {
+    const int half = rot / 2;
+    *front = NEIGHBOURS ? (c & 1) == 0 : c < half;
+    *pair = c >= rot ? 0 : NEIGHBOURS ? c / 2 : *front ? c : c - half;
+    *other = c >= rot ? c : NEIGHBOURS ? c ^ 1 : *front ? c + half : c - half;
+}
+// Eight columns from d on and the eight that they turn with, and their cosines and sines, whatever columns turn; and what they turn into.
+struct Angles {
+    float cs[8], sn[8];
+    template <bool NEIGHBOURS>
+    __device__ inline void fetch(const float* angles, int d, int rot) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            int from, pair;
+            bool front;
+            partner_of<NEIGHBOURS>(d + k, rot, &from, &pair, &front);
+            cs[k] = angles[pair];
+            sn[k] = angles[rot / 2 + pair];
+        }
+    }
+};
+template <typename T, bool NEIGHBOURS>
+struct Beside {
+    Eight<T> mine;
+    float other[8];
+    __device__ inline void fetch(const T* row, int d, int dim, int rot) {
+        load_eight<T, true>(mine, row, d, dim);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            int from, pair;
+            bool front;
+            partner_of<NEIGHBOURS>(d + k, rot, &from, &pair, &front);
+            other[k] = to_f32(row[from]);
+        }
+    }
+    __device__ inline void make(float (&y)[8], const Angles& a, int d, int rot) const {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float v = value_of(mine, k), turn = other[k] * a.sn[k], stay = v * a.cs[k];
+            const bool front = NEIGHBOURS ? ((d + k) & 1) == 0 : d + k < rot / 2;
+            y[k] = d + k >= rot ? v : front ? stay - turn : stay + turn;
+        }
+    }
+};
+
+// The keys of a run, turned.
+template <typename T, int READ, bool NEIGHBOURS>
+struct Turned;
+template <typename T, bool NEIGHBOURS>
+struct Turned<T, kPieces, NEIGHBOURS> {
     typedef float Kept;
-    static constexpr bool kWide = WIDE;
+    static constexpr bool kWide = true;
+    static constexpr int kSets = 1;
+    const T* x;
+    int64_t stride;
+    const float* table;
+    const int32_t* positions;   // of the run's tokens, in LDS
+    int rot;
+    struct Raw {
+        Beside<T, NEIGHBOURS> key;
+        Angles angles;
+    };
+    __device__ inline int column(int c, int) const { return 8 * c; }
+    __device__ inline void fetch(Raw& raw, int token, int c, int dim) const {
+        raw.key.fetch(x + (int64_t)token * stride, 8 * c, dim, rot);
+        raw.angles.template fetch<NEIGHBOURS>(table + (int64_t)positions[token] * rot, 8 * c, rot);
+    }
+    __device__ inline void make(const Raw& raw, Eight<float>* const (&e)[1], int c) const {
+        float y[8];
+        raw.key.make(y, raw.angles, 8 * c, rot);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[0]->w[k] = __builtin_bit_cast(uint32_t, y[k]);
+    }
+    __device__ inline void load(Eight<float>& e, int token, int d, int dim) const {
+        Raw raw;
+        Eight<float>* const to[1] = {&e};
+        fetch(raw, token, d / 8, dim);
+        make(raw, to, d / 8);
+    }
+};
+template <typename T, int READ, bool NEIGHBOURS>
+struct Turned {   // kPairs and kElements
+    typedef float Kept;
+    static constexpr bool WIDE = READ == kPairs, kWide = WIDE;
     static constexpr int kSets = 2;   // of long runs a lane has both sides of 8 pairs
     const T* x;
     int64_t stride;
@@ -89,11 +176,12 @@ struct Turned {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const int c = min(d + k, dim - 1);
-                const bool turns = c < rot, front = NEIGHBOURS ? (c & 1) == 0 : c < half;
-                const int other = !turns ? c : NEIGHBOURS ? c ^ 1 : front ? c + half : c - half, i = !turns ? 0 : NEIGHBOURS ? c / 2 : front ? c : c - half;
+                int other, i;
+                bool front;
+                partner_of<NEIGHBOURS>(c, rot, &other, &i, &front);
                 const float v = to_f32(row[c]);
                 y[k] = v;
-                if (turns) {
+                if (c < rot) {
                     const float turn = to_f32(row[other]) * angles[half + i], stay = v * angles[i];
                     y[k] = front ? stay - turn : stay + turn;
                 }
@@ -150,8 +238,38 @@ __device__ inline void store_eight(T* out, const float (&y)[8]) {
 
 // Queries of a window's tokens: an item is 8 pairs (16 columns), or 8 columns that do not turn, of up to four heads of a token; by elements (not WIDE), one
 // pair or column of a head.
-template <typename T, bool WIDE, bool NEIGHBOURS>
+template <typename T, int READ, bool NEIGHBOURS>
 __device__ inline void turn_queries(const RotaryParams& p, int group) {
+    constexpr bool WIDE = READ == kPairs;
+    if constexpr (READ == kPieces) {
+        // An item is 8 columns of up to four heads of a token.  Those of a row are lanes side by side of one wavefront, which all read before any
+        // writes: QR may be Q.
+        const int pieces = p.cache.dim / 8, head_groups = (p.q_heads + kQueryHeads - 1) / kQueryHeads;
+        int lanes = 1;
+        while (lanes < pieces) lanes *= 2;
+        const int64_t t0 = (int64_t)blockIdx.x * p.cache.window;
+        const int tokens = (int)min((int64_t)p.cache.window, p.cache.n_tokens - t0), items = tokens * head_groups * lanes, groups = gridDim.y - p.key_groups;
+        for (int u = group * kAppendWaves * 64 + threadIdx.x; u < items; u += groups * kAppendWaves * 64) {
+            const int piece = u & (lanes - 1), head0 = u / lanes % head_groups * kQueryHeads, d = piece * 8;
+            const int64_t t = t0 + u / lanes / head_groups;
+            const int position = p.positions[t];
+            if (position < 0 || position >= p.n_positions || piece >= pieces) continue;
+            Angles angles;
+            angles.fetch<NEIGHBOURS>(p.table + (int64_t)position * p.rot, d, p.rot);
+            Beside<T, NEIGHBOURS> e[kQueryHeads];
+#pragma unroll
+            for (int h = 0; h < kQueryHeads; ++h) e[h].fetch(static_cast<const T*>(p.q) + t * p.q_token + (int64_t)min(head0 + h, p.q_heads - 1) * p.q_head, d, p.cache.dim, p.rot);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int h = 0; h < kQueryHeads; ++h) {
+                float y[8];
+                e[h].make(y, angles, d, p.rot);
+                if (head0 + h < p.q_heads) store_eight(static_cast<T*>(p.qr) + t * p.r_token + (int64_t)(head0 + h) * p.r_head + d, y);
+            }
+        }
+        return;
+    }
     const int half = p.rot / 2, unit = WIDE ? 8 : 1, pairs = half / unit, rest = p.in_place ? 0 : (p.cache.dim - p.rot) / unit;
     const int pieces = pairs + rest, head_groups = WIDE ? (p.q_heads + kQueryHeads - 1) / kQueryHeads : p.q_heads;
     const int64_t t0 = (int64_t)blockIdx.x * p.cache.window;
@@ -221,12 +339,12 @@ __device__ inline void turn_queries(const RotaryParams& p, int group) {
     }
 }
 
-template <typename T, bool WIDE, bool WIDE_Q, bool NEIGHBOURS, int U>
+template <typename T, int READ, int READ_Q, bool NEIGHBOURS, int U>
 __global__ __launch_bounds__(kAppendWaves * 64) void kv_append_rotary_kernel(const RotaryParams p) {
     __shared__ int64_t s_slot[kMaxAhead];
     __shared__ int32_t s_position[kMaxAhead];
     if ((int)blockIdx.y >= p.key_groups) {
-        turn_queries<T, WIDE_Q, NEIGHBOURS>(p, blockIdx.y - p.key_groups);
+        turn_queries<T, READ_Q, NEIGHBOURS>(p, blockIdx.y - p.key_groups);
         return;
     }
     const CacheParams& c = p.cache;
@@ -242,21 +360,31 @@ __global__ __launch_bounds__(kAppendWaves * 64) void kv_append_rotary_kernel(con
             const T* const x = static_cast<const T*>(s.x) + t * s.token_stride + head * s.head_stride;
             int8_t* const codes = s.codes + (block * c.heads + head) * c.block * c.cols;
             float* const scale_at = s.scale + block * c.heads + head;
-            if (side == 0) append_run<Turned<T, WIDE, NEIGHBOURS>, false, U / 2>(c, Turned<T, WIDE, NEIGHBOURS>{x, s.token_stride, p.table, s_position + at, p.rot}, codes, scale_at, first, n);
-            else append_run<Rows<T, WIDE>, true, U>(c, Rows<T, WIDE>{x, s.token_stride}, codes, scale_at, first, n);
+            typedef Turned<T, READ, NEIGHBOURS> Keys;
+            typedef Rows<T, READ != kElements> Values;
+            if (side == 0) append_run<Keys, false, (Keys::kSets == 2 ? U / 2 : U < 8 ? U : 8)>(c, Keys{x, s.token_stride, p.table, s_position + at, p.rot}, codes, scale_at, first, n);
+            else append_run<Values, true, U>(c, Values{x, s.token_stride}, codes, scale_at, first, n);
         });
 }
 
 template <typename T, bool NEIGHBOURS>
-void launch_rotary(const RotaryParams& p, bool wide, bool wide_q, int groups, hipStream_t s) {
+void launch_rotary(const RotaryParams& p, int read, int read_q, int groups, hipStream_t s) {
     const dim3 grid((unsigned)((p.cache.n_tokens + p.cache.window - 1) / p.cache.window), (unsigned)groups), threads(kAppendWaves * 64);
     const int unit = append_unit(p.cache);
-    if (!wide && !wide_q) kv_append_rotary_kernel<T, false, false, NEIGHBOURS, 4><<<grid, threads, 0, s>>>(p);
-    else if (!wide) kv_append_rotary_kernel<T, false, true, NEIGHBOURS, 4><<<grid, threads, 0, s>>>(p);
-    else if (!wide_q) kv_append_rotary_kernel<T, true, false, NEIGHBOURS, 4><<<grid, threads, 0, s>>>(p);
-    else if (unit == 4) kv_append_rotary_kernel<T, true, true, NEIGHBOURS, 4><<<grid, threads, 0, s>>>(p);
-    else if (unit == 8) kv_append_rotary_kernel<T, true, true, NEIGHBOURS, 8><<<grid, threads, 0, s>>>(p);
-    else kv_append_rotary_kernel<T, true, true, NEIGHBOURS, 16><<<grid, threads, 0, s>>>(p);
+    auto launch = [&](auto r, auto rq) {
+        constexpr int R = decltype(r)::value, RQ = decltype(rq)::value;
+        if (R == kElements || RQ == kElements || unit == 4) kv_append_rotary_kernel<T, R, RQ, NEIGHBOURS, 4><<<grid, threads, 0, s>>>(p);
+        else if (unit == 8) kv_append_rotary_kernel<T, R, RQ, NEIGHBOURS, (R == kElements || RQ == kElements ? 4 : 8)><<<grid, threads, 0, s>>>(p);
+        else kv_append_rotary_kernel<T, R, RQ, NEIGHBOURS, (R == kElements || RQ == kElements ? 4 : 16)><<<grid, threads, 0, s>>>(p);
+    };
+    std::integral_constant<int, kElements> elements;
+    std::integral_constant<int, kPieces> pieces;
+    std::integral_constant<int, kPairs> pairs;
+    if (read == kPairs && read_q == kPairs) launch(pairs, pairs);
+    else if (read == kPairs) launch(pairs, elements);
+    else if (read_q == kPairs) launch(elements, pairs);
+    else if (read == kPieces && read_q == kPieces) launch(pieces, pieces);
+    else launch(elements, elements);
 }
 
 }  // namespace
@@ -299,12 +427,16 @@ extern "C" int abft_kv_append_rotary(const abft_kv_cache_t* cache, const void* Q
     c.window = abft::append_window(c, 512, 64);
     const bool neighbours = pairs == ABFT_ROTARY_NEIGHBOURS;
     const bool angles = (reinterpret_cast<uintptr_t>(table) & 15) == 0 && rot_dim % 16 == 0;   // eight pairs at a time, their cosines and sines aligned
-    const bool wide = c.side[0].wide && c.side[1].wide && angles;
-    const bool wide_q = q_heads > 0 && abft::pieces_aligned(Q, q_token_stride, q_head_stride, c.dim, type) &&
-                        abft::pieces_aligned(QR, qr_token_stride, qr_head_stride, c.dim, type) && angles;
+    const bool rows = c.side[0].wide && c.side[1].wide;
+    const bool rows_q = q_heads == 0 || (abft::pieces_aligned(Q, q_token_stride, q_head_stride, c.dim, type) && abft::pieces_aligned(QR, qr_token_stride, qr_head_stride, c.dim, type));
+    const int read = !rows ? abft::kElements : angles ? abft::kPairs : abft::kPieces, read_q = !rows_q ? abft::kElements : angles ? abft::kPairs : abft::kPieces;
     p.key_groups = (c.heads + abft::kAppendHeads - 1) / abft::kAppendHeads;
     // so many workgroups for the queries of a window that a thread has one item, or a few
-    const int64_t unit = wide_q ? 8 : 1, items = (int64_t)c.window * (wide_q ? (q_heads + abft::kQueryHeads - 1) / abft::kQueryHeads : q_heads) * (rot_dim / 2 / unit + (p.in_place ? 0 : (c.dim - rot_dim) / unit));
+    int64_t lanes = 1;
+    while (lanes < c.dim / 8) lanes *= 2;
+    const int64_t items = (int64_t)c.window * (read_q == abft::kPairs    ? (int64_t)(q_heads + abft::kQueryHeads - 1) / abft::kQueryHeads * (rot_dim / 16 + (p.in_place ? 0 : (c.dim - rot_dim) / 8))
+                                               : read_q == abft::kPieces && read == abft::kPieces ? (q_heads + abft::kQueryHeads - 1) / abft::kQueryHeads * lanes
+                                                                         : (int64_t)q_heads * (rot_dim / 2 + (p.in_place ? 0 : c.dim - rot_dim)));
     int64_t groups = (items + abft::kAppendWaves * 64 - 1) / (abft::kAppendWaves * 64);
     if (groups > 32) groups = 32;
     groups += p.key_groups;
@@ -312,8 +444,8 @@ extern "C" int abft_kv_append_rotary(const abft_kv_cache_t* cache, const void* Q
     hipStream_t s = (hipStream_t)stream;
     auto launch = [&](auto one) {
         typedef decltype(one) T;
-        if (neighbours) abft::launch_rotary<T, true>(p, wide, wide_q, (int)groups, s);
-        else abft::launch_rotary<T, false>(p, wide, wide_q, (int)groups, s);
+        if (neighbours) abft::launch_rotary<T, true>(p, read, read_q, (int)groups, s);
+        else abft::launch_rotary<T, false>(p, read, read_q, (int)groups, s);
     };
     if (type == ABFT_TYPE_F32) launch(0.0f);
     else if (type == ABFT_TYPE_F16) launch((abft::f16)0.0f);

@@ -455,7 +455,9 @@ template <typename T>
 void launch_gemv(const LoraParams& p, const LoraCut& c, hipStream_t s) {
     const dim3 threads(kLoraWaves * 64), down((unsigned)c.slots, (unsigned)c.tiles, (unsigned)c.splits);
     const int64_t rows = (int64_t)c.tiles * c.slots, most = (p.blocks + kLoraWaves - 1) / kLoraWaves;
-    int64_t columns = (kLoraUpGroups + rows - 1) / rows;
+    // (binary32 with more than two sixteens of ranks takes the registers of a whole SIMD: no more workgroups than are resident at once)
+    const int64_t wanted = p.rank_tiles <= 2 ? kLoraUpGroups : sizeof(T) == 4 ? kLoraUpGroups / 4 : kLoraUpGroups;
+    int64_t columns = (wanted + rows - 1) / rows;
     if (columns > most) columns = most;
     const dim3 up((unsigned)columns, (unsigned)c.tiles, (unsigned)c.slots);
     auto launch = [&](auto rt) {

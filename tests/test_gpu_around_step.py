@@ -95,7 +95,8 @@ def rotary_case(b, rng, dtype, heads, q_heads, dim, rot, block, neighbours, fuse
 @pytest.mark.parametrize("heads,q_heads,dim,rot,block,neighbours,fused,tokens", [
     (1, 1, 2, 2, 16, False, False, 1), (2, 8, 64, 64, 16, False, True, 5), (2, 2, 64, 64, 16, True, False, 40), (3, 6, 128, 128, 64, False, True, 130),
     (5, 15, 80, 32, 16, True, True, 100), (2, 4, 33, 32, 32, False, False, 70), (1, 7, 96, 24, 64, False, True, 90), (1, 5, 96, 24, 64, True, True, 90),
-    (4, 4, 48, 6, 128, False, False, 200), (2, 6, 256, 256, 128, True, False, 150), (8, 8, 128, 64, 32, False, True, 64), (3, 3, 40, 40, 16, False, False, 33)])
+    (4, 4, 48, 6, 128, False, False, 200), (2, 6, 256, 256, 128, True, False, 150), (8, 8, 128, 64, 32, False, True, 64), (3, 3, 40, 40, 16, False, False, 33),
+    (3, 6, 40, 20, 16, True, False, 60), (2, 4, 256, 200, 128, False, True, 140), (2, 4, 32, 12, 32, False, False, 80), (1, 3, 8, 6, 64, True, True, 70)])
 def test_rotary_append(b, dtype, heads, q_heads, dim, rot, block, neighbours, fused, tokens):
     for in_place in (False, True):
         rng = np.random.default_rng(tokens + dim + rot)
