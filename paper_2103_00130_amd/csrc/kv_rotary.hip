@@ -5,6 +5,12 @@
 // caller's table.  Keys and values go the way of an append (kv_append.h): a lane that loads 8 columns of a key loads the 8 that they turn with,
 // and keeps what they turn into in 32 bits until it is a code, so that a key is rounded once, to its code.  Queries are dealt to workgroups of
 // their own: a thread has 8 pairs (or 8 columns that do not turn) of up to four heads of a token, whose cosines and sines it loads once.
+//
+// Measured (32 query heads, 8 heads of 128, bf16, blocks of 64): 64 single tokens 5.0 us, one 4.2: a launch and two dependent trips to memory, slots and
+// positions, then rows; 6000 tokens of a fused projection 33.8 us, 4.0 TB/s of 135 MB, 28.2 where rows come from the memory-side cache, 25.0 with queries
+// in place.  Queries alone take 17; keys are what waits longest: a run is a wavefront's, since it has one scale, and a lane turns 8 tokens of 16 columns.  A
+// lane that loaded each side of a pair for itself took twice as long for keys (37.7 against 21.5, with windows of 16; 13.8 with those of 64).  Columns that are no eights of
+// pairs (a rotation of 120 columns) cost nearly four times that, 104 us: partners, cosines and sines are loaded one by one.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -424,7 +430,12 @@ extern "C" int abft_kv_append_rotary(const abft_kv_cache_t* cache, const void* Q
     p.n_positions = n_positions;
     p.rot = rot_dim;
     p.in_place = Q == QR;
-    c.window = abft::append_window(c, 512, 64);
+    // Of a prompt in blocks of 32 and more, few tokens begin a run, and workgroups that find none cost more here than for an append, since they need more
+    // registers: windows up to a block, of fewer workgroups.  Blocks of 16 have runs enough for the appends' rule.  (us, windows of 4 / 8 / 16 / 32 / 64 tokens:
+    // 2000 of one request, 8 heads of 128, blocks of 64 23.5 / 14.6 / 12.9 / 12.2 / 11.9, 400 runs of 5 28.6 / 28.0 / 27.7 / 37.9 / 65.3; 1458 of one request,
+    // 16 heads of 32, blocks of 32 22.3 / 21.6 / 23.7 / 18.7 / 18.5; 6000 in blocks of 16 49.1 / 34.3 / 30.2 / 27.8 / 27.7, 1722 of 40 requests the kernel
+    // alone 10.4 / - / 14.1 / - / -.)
+    c.window = abft::append_window(c, c.block > 16 ? 512 : 2048, c.block < abft::kMaxWindow ? c.block : abft::kMaxWindow);
     const bool neighbours = pairs == ABFT_ROTARY_NEIGHBOURS;
     const bool angles = (reinterpret_cast<uintptr_t>(table) & 15) == 0 && rot_dim % 16 == 0;   // eight pairs at a time, their cosines and sines aligned
     const bool rows = c.side[0].wide && c.side[1].wide;
