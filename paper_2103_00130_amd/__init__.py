@@ -6,8 +6,8 @@ verified against A (B e) inside the same int8-MFMA pass, before requantization.
 All arithmetic runs in the HIP kernels behind the C ABI declared in
 include/abft_gemm.h and include/abft_eb.h; `binding` only marshals arguments.
 Beside it: the checked EmbeddingBag, and the operators of a decoding step (4-bit
-weights, an 8-bit key/value cache and attention over it), which `decode_step` runs
-as a layer.
+weights, an 8-bit key/value cache and attention over it, rotation by position,
+low-rank adapters, log probabilities), which `decode_step` runs as a layer.
 """
 from . import workloads  # noqa: F401
 
