@@ -192,7 +192,7 @@ int abft_kv_append(const abft_kv_cache_t* cache, const void* K, int64_t k_token_
  *     a becomes a * cos - b * sin,   b becomes b * cos + a * sin,
  * in binary32, the products and their sum or difference rounded one by one; the other columns stay.
  *   Q, QR      n_tokens x q_heads x head_dim of `type`: queries, and where they go, rounded once to `type`.  QR may be Q (the
- *              same pointer and strides), or does not overlap it.  q_heads 0: no queries, and both may be NULL
+ *              same pointer and strides), or does not overlap it; its rows do not overlap each other.  q_heads 0: no queries, and both may be NULL
  *   K, V, slots   as above; what a key turns into goes to its code without being rounded to `type`
  *   positions  int32 [n_tokens]
  *   table      float32 [n_positions][rot_dim]: for each position the cosines of the pairs, then their sines, any scaling of

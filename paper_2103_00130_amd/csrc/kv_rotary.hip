@@ -418,6 +418,8 @@ extern "C" int abft_kv_append_rotary(const abft_kv_cache_t* cache, const void* Q
     if (q_heads > 0 && (reinterpret_cast<uintptr_t>(Q) % es || reinterpret_cast<uintptr_t>(QR) % es)) return abft::set_error(ABFT_EINVAL, "%s: Q or QR is not aligned to its type", fn);
     if (q_heads > 0 && Q == QR && (q_token_stride != qr_token_stride || q_head_stride != qr_head_stride))
         return abft::set_error(ABFT_EINVAL, "%s: QR is Q, with other strides", fn);
+    if (q_heads > 0 && ((n_tokens > 1 && qr_token_stride == 0) || (q_heads > 1 && qr_head_stride == 0)))
+        return abft::set_error(ABFT_EINVAL, "%s: rows of QR overlap each other", fn);
     p.q = Q;
     p.qr = QR;
     p.q_token = q_token_stride;

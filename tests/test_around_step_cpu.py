@@ -133,6 +133,15 @@ def test_rotary_refusals(b):
     assert call(n=0, Q=None, QR=None, K=None, V=None, slots=None, positions=None, table=None) == b.ABFT_OK
 
 
+# rows of QR that lie on each other (expanded tensors) would be turned as often as they are named
+@pytest.mark.parametrize("place", [0x1000, 0x2000])
+@pytest.mark.parametrize("strides", [(0, 64), (256, 0), (0, 0)])
+def test_rotary_refuses_rows_on_each_other(b, place, strides):
+    d = ctypes.c_void_p(0x1000)
+    rc = b.lib.abft_kv_append_rotary(cache(b), d, *strides, 4, ctypes.c_void_p(place), *strides, d, 128, 64, d, 128, 64, 2, d, d, 3, d, 100, 64, 0, None)
+    assert rc == b.ABFT_EINVAL and b"overlap" in b.lib.abft_last_error()
+
+
 def pool(b, **kw):
     f = dict(down=0x1000, up=0x1000, scale=0x1000, rank=0x1000, adapters=3, max_rank=20, K=100, N=70, type=2)
     f.update(kw)
