@@ -198,8 +198,10 @@ int abft_kv_append(const abft_kv_cache_t* cache, const void* K, int64_t k_token_
  *   table      float32 [n_positions][rot_dim]: for each position the cosines of the pairs, then their sines, any scaling of
  *              frequencies and of the result being the caller's
  *   rot_dim    even, 2..head_dim
- * A token whose position is outside the table is left out: the cache and QR stay as they are there.  One whose slot is outside the cache has
- * its queries turned and is not appended. */
+ * A token whose position is outside the table is left out: QR stays as it is there, and nothing of it goes into the cache.  Inside a run of
+ * slots it cuts the run: the tokens behind it are a run of their own, appended behind the one before it, also to the same block.  (Its own place is past the
+ * one and before the other: no token's, so that the codes there may be rescaled.)  One whose slot is outside the cache has its queries turned and is
+ * not appended. */
 #define ABFT_ROTARY_HALVES 0
 #define ABFT_ROTARY_NEIGHBOURS 1
 int abft_kv_append_rotary(const abft_kv_cache_t* cache, const void* Q, int64_t q_token_stride, int64_t q_head_stride, int q_heads, void* QR,

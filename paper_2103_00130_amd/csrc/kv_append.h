@@ -308,9 +308,11 @@ __device__ inline void append_run(const CacheParams& p, const Source& src, int8_
 constexpr int kAppendHeads = 2, kAppendWaves = 2 * kAppendHeads;
 
 // The runs that begin among the tokens of a window, by a workgroup: two heads of each (those of `group`), keys and values, dealt to its
-// wavefronts.  s_slot: kMaxAhead slots; slot_of(t, i) is token t's (or -1: left out), i its place there; append(side, head, token, its place, block, first, n).
-template <typename Slot, typename Append>
-__device__ inline void append_runs(const CacheParams& p, int64_t* s_slot, int group, const Slot& slot_of, const Append& append) {
+// wavefronts.  s_slot: kMaxAhead slots; slot_of(t, i) is token t's, i its place there; append(side, head, token, its place, block, first, n).
+// LEAVES: tokens of a run for whose place left_out holds stay out of it, and those behind them are appended as a run of their own, behind the one
+// before them: by the same wavefront, since a block's runs share its scale and the codes that it rescales.
+template <bool LEAVES, typename Slot, typename LeftOut, typename Append>
+__device__ inline void append_runs(const CacheParams& p, int64_t* s_slot, int group, const Slot& slot_of, const LeftOut& left_out, const Append& append) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t t0 = (int64_t)blockIdx.x * p.window;
     // of the token before the window, the window, and what a run can reach
@@ -330,20 +332,35 @@ __device__ inline void append_runs(const CacheParams& p, int64_t* s_slot, int gr
     unsigned long long left = __ballot(begins);
     const int side = wave & 1, head = group * kAppendHeads + (wave >> 1);
     if (head >= p.heads) return;
+    // the first number for which it does not hold (at most kMaxBlock)
+    auto count = [&](const auto& holds) __attribute__((always_inline)) {
+        int n = 0;
+#pragma unroll
+        for (int h = 0; h < kMaxBlock / 64; ++h) {
+            const unsigned long long b = __ballot(holds(h * 64 + lane));
+            if (n == h * 64) n += b == ~0ull ? 64 : __builtin_ctzll(~b);
+        }
+        return n;
+    };
     for (; left; left &= left - 1) {
         const int w = __builtin_ctzll(left);
         const int64_t slot = s_slot[w + 1], block = slot >> p.shift;
         const int first = (int)slot & (p.block - 1);
         // the run's length: how many slots count up from here without leaving the block
-        int n = 0;
-#pragma unroll
-        for (int h = 0; h < kMaxBlock / 64; ++h) {
-            const int j = h * 64 + lane;
-            const bool on = j < p.block - first && s_slot[w + 1 + j] == slot + j;
-            const unsigned long long b = __ballot(on);
-            if (n == h * 64) n += b == ~0ull ? 64 : __builtin_ctzll(~b);
+        const int n = count([&](int j) { return j < p.block - first && s_slot[w + 1 + j] == slot + j; });
+        if constexpr (!LEAVES) {
+            append(side, head, t0 + w, w + 1, block, first, n);
+        } else {
+            for (int at = 0; at < n;) {
+                const int kept = count([&](int j) { return at + j < n && !left_out(w + 1 + at + j); });
+                if (kept > 0) append(side, head, t0 + w + at, w + 1 + at, block, first + at, kept);
+                at += kept + 1;
+                if (kept > 0 && at < n) {   // (what is behind reads the scale and the codes that were stored)
+                    __builtin_amdgcn_s_waitcnt(0);
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+                }
+            }
         }
-        append(side, head, t0 + w, w + 1, block, first, n);
     }
 }
 

@@ -10,7 +10,7 @@
 // positions, then rows; 6000 tokens of a fused projection 33.8 us, 4.0 TB/s of 135 MB, 28.2 where rows come from the memory-side cache, 25.0 with queries
 // in place.  Queries alone take 17; keys are what waits longest: a run is a wavefront's, since it has one scale, and a lane turns 8 tokens of 16 columns.  A
 // lane that loaded each side of a pair for itself took twice as long for keys (37.7 against 21.5, with windows of 16; 13.8 with those of 64).  Columns that are no eights of
-// pairs (a rotation of 120 columns) cost nearly four times that, 104 us: partners, cosines and sines are loaded one by one.
+// pairs (a rotation of 120 columns) cost nearly four times that, 100 us: partners, cosines and sines are loaded one by one.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -354,13 +354,15 @@ __global__ __launch_bounds__(kAppendWaves * 64) void kv_append_rotary_kernel(con
         return;
     }
     const CacheParams& c = p.cache;
-    append_runs(
+    // (runs go by the slots alone: two of one block have to be the same wavefront's, which a token without a row of the table does not change)
+    append_runs<true>(
         c, s_slot, blockIdx.y,
         [&](int64_t t, int i) {
             const int position = p.positions[t];
-            s_position[i] = position;
-            return position >= 0 && position < p.n_positions ? c.slots[t] : (int64_t)-1;
+            s_position[i] = position < p.n_positions ? position : -1;
+            return c.slots[t];
         },
+        [&](int i) { return s_position[i] < 0; },
         [&](int side, int head, int64_t t, int at, int64_t block, int first, int n) {
             const Side& s = c.side[side];
             const T* const x = static_cast<const T*>(s.x) + t * s.token_stride + head * s.head_stride;
