@@ -144,7 +144,12 @@ __device__ inline void fetch_scales(Scales<WIDE, BIAS>& s, const uint8_t* p) {
 // (16 + code) * scale + shift is the weight
 template <bool WIDE, bool BIAS>
 __device__ inline void scales_of(const Scales<WIDE, BIAS>& s, bool half, float* scale, float* shift) {
-    auto value = [&](uint32_t h) __attribute__((always_inline)) { return half ? (float)__builtin_bit_cast(f16, (uint16_t)h) : __builtin_bit_cast(float, h << 16); };
+    // (both readings are worked out and one is taken: with a branch for each scale the conversion on one side of it wrote a register that a matrix
+    // instruction ahead of the branch was still to write, six instructions later where eight are needed)
+    auto value = [&](uint32_t h) __attribute__((always_inline)) {
+        const float a = (float)__builtin_bit_cast(f16, (uint16_t)h), b = __builtin_bit_cast(float, h << 16);
+        return half ? a : b;
+    };
     *scale = WIDE ? __builtin_bit_cast(float, s.w[0]) : value(s.w[0] & 0xffffu);
     if constexpr (BIAS) *shift = __builtin_fmaf(-16.0f, *scale, WIDE ? __builtin_bit_cast(float, s.w[WIDE ? 1 : 0]) : value(s.w[0] >> 16));
     else *shift = -24.0f * *scale;
