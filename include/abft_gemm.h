@@ -454,7 +454,7 @@ int abft_lora_gemv(const void* X, int64_t ldx, int M, const abft_lora_t* pool, c
  *            fewer parts.  Calls that may run at the same time need workspaces of their own
  * A row of -inf alone has logprob and lse -inf and entropy 0.  A row that holds a NaN or +inf gives NaN (logprob 0 where it has no
  * target) and -1 in rank and top_index.  Sums are binary32; order and ranks are those of the logits themselves.
- * n_rows == 0 is a valid call that does nothing.  No host synchronisation; the same bits every time. */
+ * n_rows == 0 is a valid call that does nothing, more than 2^24 - 1 are refused.  No host synchronisation; the same bits every time. */
 size_t abft_logprobs_workspace_bytes(int64_t n_rows, int vocab, int top);
 int abft_logprobs(const void* logits, int64_t ldl, int type, int64_t n_rows, int vocab, float scale, const int64_t* targets, float* logprob,
                   int32_t* rank, float* entropy, float* lse, int top, float* top_logprob, int64_t* top_index, void* workspace,

@@ -7,7 +7,7 @@ namespace abft {
 
 constexpr int kMostTop = 64;                     // entries of a list of a wavefront, one a lane
 constexpr int kMostParts = 64;                   // one a lane where they are joined
-constexpr int64_t kMostLogprobRows = 0x7fffffff;
+constexpr int64_t kMostLogprobRows = 0xffffff;   // a workgroup of 256 threads each, and a launch has fewer than 2^32 of them
 constexpr int kMostVocab = 0x7fffff00;
 // us by parts of a row, with alternatives: 1 x 131072 bf16 1: 54.9, 8: 18.2, 32: 10.9, 64: 10.7; 1 x 32000 f32 1: 17.0, 4: 11.3, 8: 9.4, 32: 9.4; 1 x 8000 1: 8.0, 3:
 // 9.3; 16 x 32000 f32 1: 23.3, 8: 12.4, 32: 11.7; 64 x 50001 f16 1: 23.7, 8: 12.2, 16: 12.9, 32: 18.6; 256 x 32000 1: 21.4, 4: 18.9, 8: 19.7; 256 x 131072 bf16 1: 62.5,
