@@ -440,7 +440,7 @@ int abft_lora_gemv(const void* X, int64_t ldx, int M, const abft_lora_t* pool, c
 
 /* ------------------------------------------------------------------------- */
 /* What rows of logits say about tokens.  With p = softmax(scale * logits[row]):
- *   logits   n_rows x vocab of `type`, ldl >= vocab; scale > 0 (one over the temperature), scale * log2(e) finite
+ *   logits   n_rows x vocab of `type`, ldl >= vocab; scale > 0 (one over the temperature): 2^-120 at least, and scale * log2(e) finite
  *   targets  int64 [n_rows] or NULL: a token of each row; outside 0..vocab-1: none
  *   logprob  float32 [n_rows] or NULL: ln p[target]; 0 where there is no target
  *   rank     int32 [n_rows] or NULL: tokens ahead of the target, those with a larger logit, or an equal one and a

@@ -45,6 +45,7 @@ struct LogprobsParams {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr float kLowest = -3.402823466e38f, kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 constexpr float kNothing = -200.0f;   // 2^t is 0 from here on; t itself may be -inf, which 0 times is no number
+constexpr float kLeastScale = 0x1p-120f;   // t of a difference of logits that binary32 does not hold is below kNothing: taken as -inf it counts as much
 
 // Eight logits, as they are stored.
 template <typename T>
@@ -187,7 +188,8 @@ __device__ inline Target target_of(const LogprobsParams& p, int64_t row, const T
 __device__ inline void finish(const LogprobsParams& p, int64_t row, Target target, Sums r, int ahead, uint64_t list, int lane) {
     const bool bad = !(r.s == r.s), none = r.s == 0.0f;   // (a NaN or a +inf among the logits; nothing but -inf)
     const float nan = __builtin_nanf(""), ln = none ? 0.0f : logf(r.s);
-    auto log_p = [&](float x) { return bad ? nan : none ? -INFINITY : (x - r.m) * p.scale - ln; };
+    // (halves: the difference of two logits may be twice what a number holds, and its product with the scale a number again)
+    auto log_p = [&](float x) { return bad ? nan : none ? -INFINITY : 2.0f * ((0.5f * x - 0.5f * r.m) * p.scale) - ln; };
     if (lane == 0) {
         if (p.logprob) p.logprob[row] = target.at >= 0 ? log_p(target.x) : 0.0f;
         if (p.rank) p.rank[row] = target.at >= 0 && !bad ? ahead : -1;
@@ -488,7 +490,7 @@ int abft_logprobs(const void* logits, int64_t ldl, int type, int64_t n_rows, int
     const char* fn = "abft_logprobs";
     if (!abft::known_type(type)) return abft::set_error(ABFT_EINVAL, "%s: unknown type %d", fn, type);
     if (n_rows < 0 || vocab < 1) return abft::set_error(ABFT_EINVAL, "%s: n_rows=%lld vocab=%d", fn, (long long)n_rows, vocab);
-    if (!(scale > 0.0f) || !std::isfinite(scale * abft::kLog2e)) return abft::set_error(ABFT_EINVAL, "%s: scale must be above 0, and scale * log2(e) finite", fn);
+    if (!(scale >= abft::kLeastScale) || !std::isfinite(scale * abft::kLog2e)) return abft::set_error(ABFT_EINVAL, "%s: scale must be above 0 (2^-120 at least), and scale * log2(e) finite", fn);
     if (top < 0) return abft::set_error(ABFT_EINVAL, "%s: top=%d must be >= 0", fn, top);
     if (top > abft::kMostTop) return abft::set_error(ABFT_EUNSUPPORTED, "%s: top=%d (at most %d)", fn, top, abft::kMostTop);
     if (n_rows > abft::kMostLogprobRows || vocab > abft::kMostVocab)

@@ -21,3 +21,9 @@ def test_rows_of_logits_beyond_a_launch(b):
         assert logprobs(b, rows=rows) == b.ABFT_EUNSUPPORTED and b"too large" in b.lib.abft_last_error(), rows
         assert b.lib.abft_logprobs_workspace_bytes(rows, 100000, 5) == 0
     assert b.lib.abft_logprobs_workspace_bytes(2 ** 24 - 1, 100000, 5) > 0
+
+
+def test_scales_under_which_differences_that_32_bits_do_not_hold_would_count(b):
+    for scale in (2.0 ** -121, 1e-38, 2.0 ** -140):
+        assert logprobs(b, scale=scale) == b.ABFT_EINVAL and b"scale" in b.lib.abft_last_error(), scale
+    assert logprobs(b, rows=0, scale=2.0 ** -120) == b.ABFT_OK

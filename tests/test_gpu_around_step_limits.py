@@ -1,8 +1,9 @@
 """The largest calls of the operators around a decoding step, and numbers at the ends of their types."""
+import numpy as np
 import pytest
 import torch
 
-from test_gpu_around_step import b  # noqa: F401 (the fixture)
+from test_gpu_around_step import TYPES, b, check_logprobs  # noqa: F401 (b: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -24,3 +25,21 @@ def test_as_many_rows_of_logits_as_a_launch_takes(b):  # noqa: F811
     assert torch.equal(rank, ((x > mine) | ((x == mine) & lower)).sum(1).int())
     # (of equal ones the first)
     assert torch.equal(index, torch.where(x == x.max(1, keepdim=True).values, torch.arange(3, device="cuda"), 3).amin(1, keepdim=True))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [40, 20000])
+def test_logits_at_both_ends_of_their_type(b, dtype, V):  # noqa: F811
+    """Differences of logits that binary32 does not hold, whose product with the scale it does."""
+    most = torch.finfo(TYPES[dtype]).max
+    rng = np.random.default_rng(V)
+    x = torch.from_numpy(rng.standard_normal((6, V)).astype(np.float32)).to(TYPES[dtype])
+    x[0], x[0, 5] = -most, most
+    x[1, 3], x[1, 7] = most, -most
+    x[2] = most * torch.from_numpy(rng.uniform(-1, 1, V).astype(np.float32)).to(x.dtype)
+    x[3, ::2], x[3, 1::2] = most, -most
+    x[4], x[4, 7] = -most, -0.5 * most
+    x[5], x[5, 7] = -float("inf"), -most
+    for scale in (0.5, 0.01, 1e-30, 2.0 ** -120):
+        for target in (3, 5, 7, V - 1):
+            check_logprobs(b, x.cuda(), np.full(6, target, np.int64), scale, 8, f"scale {scale}, target {target}")
