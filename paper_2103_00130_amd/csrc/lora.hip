@@ -404,29 +404,31 @@ __global__ __launch_bounds__(kLoraWaves * 64) void lora_up_kernel(const LoraPara
     });
 }
 
-// An adapter into its place: one thread for each element of the layout, zeros where the adapter has none.
+// An adapter into its place: an element of the layout to a thread, or several where there are more than a launch has threads; zeros where the adapter has none.
 template <typename T>
 __global__ __launch_bounds__(256) void lora_load_kernel(T* down, T* up, float* scale_at, int32_t* rank_at, const T* A, int64_t lda, const T* B, int64_t ldb,
                                                         int rank, float scale, int K, int N, int chunks, int blocks, int rank_tiles) {
     const int tiles = (rank + 15) / 16;
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, n_down = (int64_t)tiles * chunks * (1024 / sizeof(T)), n_up = (int64_t)blocks * tiles * 1024;
-    if (t == 0) {
+    const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, n_down = (int64_t)tiles * chunks * (1024 / sizeof(T)), n_up = (int64_t)blocks * tiles * 1024;
+    if (first == 0) {
         *scale_at = scale;
         *rank_at = rank;
     }
-    if (t < n_down) {
-        constexpr int n = 16 / sizeof(T);   // elements of a lane
-        const int e = (int)(t % n), lane = (int)(t / n) & 63;
-        const int64_t piece = t / (64 * n);
-        const int r = (int)(piece / chunks) * 16 + (lane & 15);
-        const int64_t k = piece % chunks * kChunkOf<T> + (lane >> 4) * n + e;
-        down[t] = r < rank && k < K ? A[r * lda + k] : (T)0.0f;
-    } else if (t - n_down < n_up) {
-        const int64_t u = t - n_down, piece = u / 1024;   // [block][rank tile]
-        const int e = (int)(u & 3), tile = (int)(u / 4) & 3, lane = (int)(u / 16) & 63, i = lane & 15, rt = (int)(piece % tiles);
-        const int64_t block = piece / tiles, col = block * kLoraColumns + column_of<T>(i >> 2, tile * 4 + (i & 3));
-        const int r = rt * 16 + (lane >> 4) * 4 + e;
-        up[(block * rank_tiles + rt) * 1024 + lane * 16 + tile * 4 + e] = r < rank && col < N ? B[col * ldb + r] : (T)0.0f;
+    for (int64_t t = first; t < n_down + n_up; t += (int64_t)gridDim.x * 256) {
+        if (t < n_down) {
+            constexpr int n = 16 / sizeof(T);   // elements of a lane
+            const int e = (int)(t % n), lane = (int)(t / n) & 63;
+            const int64_t piece = t / (64 * n);
+            const int r = (int)(piece / chunks) * 16 + (lane & 15);
+            const int64_t k = piece % chunks * kChunkOf<T> + (lane >> 4) * n + e;
+            down[t] = r < rank && k < K ? A[r * lda + k] : (T)0.0f;
+        } else {
+            const int64_t u = t - n_down, piece = u / 1024;   // [block][rank tile]
+            const int e = (int)(u & 3), tile = (int)(u / 4) & 3, lane = (int)(u / 16) & 63, i = lane & 15, rt = (int)(piece % tiles);
+            const int64_t block = piece / tiles, col = block * kLoraColumns + column_of<T>(i >> 2, tile * 4 + (i & 3));
+            const int r = rt * 16 + (lane >> 4) * 4 + e;
+            up[(block * rank_tiles + rt) * 1024 + lane * 16 + tile * 4 + e] = r < rank && col < N ? B[col * ldb + r] : (T)0.0f;
+        }
     }
 }
 
@@ -455,7 +457,7 @@ void launch_load(const abft_lora_t* L, int slot, const void* A, int64_t lda, con
     const int64_t count = tiles * chunks * (int64_t)(1024 / sizeof(T)) + blocks * tiles * 1024;
     T* const down = static_cast<T*>(L->down) + (int64_t)slot * rank_tiles_of(L) * chunks * (int64_t)(1024 / sizeof(T));
     T* const up = static_cast<T*>(L->up) + (int64_t)slot * blocks * rank_tiles_of(L) * 1024;
-    lora_load_kernel<T><<<dim3((unsigned)(count ? (count + 255) / 256 : 1)), dim3(256), 0, s>>>(down, up, L->scale + slot, L->rank + slot, static_cast<const T*>(A), lda,
+    lora_load_kernel<T><<<dim3((unsigned)lora_load_groups(count)), dim3(256), 0, s>>>(down, up, L->scale + slot, L->rank + slot, static_cast<const T*>(A), lda,
                                                                                           static_cast<const T*>(B), ldb, rank, scale, L->K, L->N, (int)chunks, (int)blocks, rank_tiles_of(L));
 }
 

@@ -32,6 +32,11 @@ inline LoraCut lora_cut(int64_t M, int K) {
     c.splits = s < 1 ? 1 : (int)s;
     return c;
 }
+// Workgroups of 256 threads for the elements of an adapter's layout: no more than a launch may have, of fewer than 2^32 threads.
+inline int64_t lora_load_groups(int64_t elements) {
+    const int64_t groups = (elements + 255) / 256;
+    return groups < 1 ? 1 : groups > 0xffffff ? 0xffffff : groups;
+}
 // floats of a call's sums over K
 inline int64_t lora_sums(int64_t M, int K, int max_rank) { return (int64_t)lora_cut(M, K).splits * M * ((max_rank + 15) / 16 * 16); }
 // ... that every call on up to M rows needs at most

@@ -1,7 +1,11 @@
 """The largest and smallest calls of the operators around a decoding step, as the host sees them: what no launch can hold is refused as such."""
 import ctypes
+import os
+import subprocess
 
 import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2103_00130_amd", "csrc")
 
 
 @pytest.fixture(scope="module")
@@ -27,3 +31,14 @@ def test_scales_under_which_differences_that_32_bits_do_not_hold_would_count(b):
     for scale in (2.0 ** -121, 1e-38, 2.0 ** -140):
         assert logprobs(b, scale=scale) == b.ABFT_EINVAL and b"scale" in b.lib.abft_last_error(), scale
     assert logprobs(b, rows=0, scale=2.0 ** -120) == b.ABFT_OK
+
+
+def test_an_adapter_of_any_size_is_loaded_by_one_launch(tmp_path):
+    src = '#include "lora_cut.h"\nextern "C" long long groups(long long elements) { return abft::lora_load_groups(elements); }\n'
+    lib = str(tmp_path / "cut.so")
+    subprocess.run([os.environ.get("CXX", "g++"), "-std=c++17", "-Wall", "-Werror", "-shared", "-fPIC", f"-I{CSRC}", "-x", "c++", "-", "-o", lib], input=src, text=True, check=True)
+    f = ctypes.CDLL(lib).groups
+    f.restype, f.argtypes = ctypes.c_longlong, [ctypes.c_longlong]
+    assert [f(n) for n in (0, 1, 256, 257)] == [1, 1, 1, 2]
+    for n in (2 ** 32 - 256, 2 ** 32 - 255, 2 ** 32, 2 ** 33, 128 * 2 * (2 ** 31 - 256)):
+        assert 0 < f(n) * 256 < 2 ** 32, n

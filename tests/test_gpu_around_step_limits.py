@@ -43,3 +43,26 @@ def test_logits_at_both_ends_of_their_type(b, dtype, V):  # noqa: F811
     for scale in (0.5, 0.01, 1e-30, 2.0 ** -120):
         for target in (3, 5, 7, V - 1):
             check_logprobs(b, x.cuda(), np.full(6, target, np.int64), scale, 8, f"scale {scale}, target {target}")
+
+
+@pytest.mark.parametrize("K,N", [(64, 2 ** 25), (2 ** 25, 64)])
+def test_an_adapter_of_more_elements_than_a_launch_has_threads(b, K, N):  # noqa: F811
+    """Rank 128 of K + N = 2^25 + 64 columns: 2^32 + 2^13 elements.  Small whole numbers, whose sums are exact in every type."""
+    rank, g = 128, torch.Generator("cuda").manual_seed(2)
+    whole = lambda *s: torch.randint(-2, 3, s, dtype=torch.int8, device="cuda", generator=g).to(torch.bfloat16)
+    A, B = whole(rank, K), whole(N, rank)
+    pool = b.LoraPool(1, K, N, rank)
+    pool.load(0, A, B)
+    # rows that meet a few columns at both ends and in the middle
+    x = torch.zeros((2, K), dtype=torch.bfloat16, device="cuda")
+    x[0, [0, K // 2, K - 1]] = 1.0
+    x[1, [1, K - 2]] = 2.0
+    mid = (A[:, [0, K // 2, K - 1]].float().sum(1), 2.0 * A[:, [1, K - 2]].float().sum(1))
+    base = whole(2, N)
+    y = torch.empty_like(base)
+    b.abft_lora_gemv(x, pool, torch.zeros(2, dtype=torch.int32, device="cuda"), y, base=base, workspace=b.LoraWorkspace(pool, 2).tensor)
+    for i in range(2):
+        want = base[i].float()
+        for n in range(0, N, 2 ** 22):      # (whole numbers below 2^24)
+            want[n:n + 2 ** 22] += B[n:n + 2 ** 22].float() @ mid[i]
+        assert torch.equal(y[i], want.to(torch.bfloat16))
