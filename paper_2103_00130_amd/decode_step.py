@@ -48,8 +48,14 @@ class DecodeLayer:
     def __init__(self, wqkv: b.W4Weight, wo: b.W4Weight, q_heads: int, heads: int, head_dim: int, requests: int, longest: int, most_rows: int,
                  block_tokens: int = 64, dtype=torch.bfloat16, rotary: torch.Tensor | None = None, neighbours: bool = False,
                  adapters: tuple[b.LoraPool, b.LoraPool] | None = None):
-        if rotary is not None and rotary.shape[0] < longest:
-            raise ValueError(f"a table of {rotary.shape[0]} positions for requests of up to {longest} tokens")
+        if rotary is not None:
+            if rotary.dim() != 2 or rotary.shape[0] < longest or not 2 <= rotary.shape[1] <= head_dim or rotary.shape[1] % 2 or not rotary.is_contiguous():
+                raise ValueError(f"a table of {tuple(rotary.shape)} for requests of up to {longest} tokens and heads of {head_dim} columns: it has a row for each "
+                                 "position, for an even number of columns, side by side")
+            if not rotary.is_cuda or rotary.dtype != torch.float32:
+                raise TypeError("a table of angles is float32 on the device")
+        if adapters is not None and len(adapters) != 2:
+            raise ValueError(f"{len(adapters)} pools of adapters: a layer has one beside either weight")
         for pool, weight in zip(adapters or (), (wqkv, wo)):
             if (pool.K, pool.N, pool.dtype, pool.adapters) != (weight.K, weight.N, dtype, adapters[0].adapters):
                 raise ValueError(f"a pool of {pool.adapters} adapters of {pool.K} to {pool.N} columns in {pool.dtype} beside a weight of {weight.N} x {weight.K}")
@@ -132,11 +138,17 @@ class DecodeLayer:
     def step(self, x, new):
         """x: a row for each new token, those of request 0 first; new: how many each request has (a list).  Returns the rows' output."""
         self._check_rows(x, sum(new))
+        held, used = list(self.lengths), self.used
         first = self._take(new)
-        y = torch.empty((x.shape[0], self.wo.N), dtype=x.dtype, device=x.device)
-        if x.shape[0]:
-            self._launch(x, torch.tensor(new, dtype=torch.int32).to(x.device), self.pool[first:self.used], y, max(new), max(self.lengths),
-                         *self._positions(new))
+        try:
+            y = torch.empty((x.shape[0], self.wo.N), dtype=x.dtype, device=x.device)
+            if x.shape[0]:
+                self._launch(x, torch.tensor(new, dtype=torch.int32).to(x.device), self.pool[first:self.used], y, max(new), max(self.lengths),
+                             *self._positions(new))
+        except Exception:
+            # (the device's lengths are the last that a step writes: what it appended before is past every request, and appended anew by the next)
+            self.lengths, self.used = held, used
+            raise
         return y
 
     def record(self):
