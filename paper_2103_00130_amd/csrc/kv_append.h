@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include "kv_append_cut.h"
 #include "kv_cache.h"
 #include "values.h"
 
@@ -29,7 +30,7 @@ struct CacheParams {
 };
 
 constexpr int kNT = 256;
-constexpr int kMaxWindow = 64, kMaxBlock = 128, kMaxAhead = kMaxWindow + kMaxBlock + 1;
+constexpr int kMaxBlock = 128, kMaxAhead = kMaxWindow + kMaxBlock + 1;
 
 // Eight columns of a token, as they are stored.
 template <typename T>
@@ -305,7 +306,7 @@ __device__ inline void append_run(const CacheParams& p, const Source& src, int8_
     }
 }
 
-constexpr int kAppendHeads = 2, kAppendWaves = 2 * kAppendHeads;
+constexpr int kAppendWaves = 2 * kAppendHeads;
 
 // The runs that begin among the tokens of a window, by a workgroup: two heads of each (those of `group`), keys and values, dealt to its
 // wavefronts.  s_slot: kMaxAhead slots; slot_of(t, i) is token t's, i its place there; append(side, head, token, its place, block, first, n).
@@ -393,16 +394,6 @@ inline int fill(CacheParams& p, const char* fn, const abft_kv_cache_t* c, const 
     return ABFT_OK;
 }
 
-// A workgroup looks for runs among so many tokens: few, so that single tokens do not wait for each other, while that makes up to 2048
-// workgroups; of more tokens most lie inside runs, and the workgroups that find none would hold up the others (us, 1 / 2 / 4 / 8 /
-// 16 tokens: 6000 of one request 94 / 86 / 30 / 16 / 11, 64 single tokens 4.2 / 4.8 / 7.3 / 11.8 / 21, 1169 of 40 requests 8.8 / 8.2 / 8.7 /
-// 10.6 / 12.6).
-inline int append_window(const CacheParams& p, int64_t groups = 2048, int most = 16) {
-    const int64_t all = p.n_tokens * ((p.heads + kAppendHeads - 1) / kAppendHeads);
-    int window = 1;
-    while (window < most && all > groups * window) window *= 2;
-    return window;
-}
 // So few tokens to a lane's units that a block has one for every lane, if it can (us with the read behind, 16 tokens / the rule: 6000 tokens of
 // one request, 8 heads of 128, blocks of 16 24.3 / 20.8, of 32 22.2 / 20.2; 40 requests of up to 300, 5 heads of 80, blocks of 16 15.7 / 12.8;
 // 30 of up to 200, 8 heads of 64, binary32, blocks of 16 18.1 / 13.0).

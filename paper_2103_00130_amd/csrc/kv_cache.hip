@@ -182,7 +182,7 @@ int abft_kv_append(const abft_kv_cache_t* cache, const void* K, int64_t k_token_
     if (rc != ABFT_OK) return rc;
     if (n_tokens == 0) return ABFT_OK;
     if (!K || !V) return abft::set_error(ABFT_EINVAL, "%s: null pointer", fn);
-    p.window = abft::append_window(p);
+    p.window = abft::append_window(n_tokens, p.heads);
     hipStream_t s = (hipStream_t)stream;
     if (type == ABFT_TYPE_F32) abft::launch_append<float>(p, s);
     else if (type == ABFT_TYPE_F16) abft::launch_append<abft::f16>(p, s);

@@ -434,12 +434,7 @@ extern "C" int abft_kv_append_rotary(const abft_kv_cache_t* cache, const void* Q
     p.n_positions = n_positions;
     p.rot = rot_dim;
     p.in_place = Q == QR;
-    // Of a prompt in blocks of 32 and more, few tokens begin a run, and workgroups that find none cost more here than for an append, since they need more
-    // registers: windows up to a block, of fewer workgroups.  Blocks of 16 have runs enough for the appends' rule.  (us, windows of 4 / 8 / 16 / 32 / 64 tokens:
-    // 2000 of one request, 8 heads of 128, blocks of 64 23.5 / 14.6 / 12.9 / 12.2 / 11.9, 400 runs of 5 28.6 / 28.0 / 27.7 / 37.9 / 65.3; 1458 of one request,
-    // 16 heads of 32, blocks of 32 22.3 / 21.6 / 23.7 / 18.7 / 18.5; 6000 in blocks of 16 49.1 / 34.3 / 30.2 / 27.8 / 27.7, 1722 of 40 requests the kernel
-    // alone 10.4 / - / 14.1 / - / -.)
-    c.window = abft::append_window(c, c.block > 16 ? 512 : 2048, c.block < abft::kMaxWindow ? c.block : abft::kMaxWindow);
+    c.window = abft::rotary_window(n_tokens, c.heads, c.block);
     const bool neighbours = pairs == ABFT_ROTARY_NEIGHBOURS;
     const bool angles = (reinterpret_cast<uintptr_t>(table) & 15) == 0 && rot_dim % 16 == 0;   // eight pairs at a time, their cosines and sines aligned
     const bool rows = c.side[0].wide && c.side[1].wide;

@@ -116,3 +116,59 @@ def test_no_position_is_known(b):  # noqa: F811
     table = b.rotary_table(50, 32)
     for t in (table, table[:0]):
         check(b, rng, "bf16", 1, 2, 32, 16, 8, slots, pos, x, t, False, True)
+
+
+# (how rows are read, heads, query heads, block, tokens, tokens among which a workgroup looks for runs)
+WINDOWS = [("pairs", 8, 8, 64, 201, 2), ("pairs_part", 7, 14, 64, 501, 4), ("neighbours", 8, 16, 32, 1003, 8), ("pairs", 8, 8, 64, 1501, 16), ("pieces", 16, 16, 32, 1801, 32),
+           ("pairs", 16, 16, 64, 2501, 64), ("elements", 16, 16, 128, 2333, 64), ("pieces_neighbours", 15, 15, 64, 2501, 64), ("wide", 16, 80, 128, 2200, 64),
+           ("neighbours", 16, 16, 128, 2501, 64), ("pairs", 16, 32, 16, 4200, 16), ("elements", 8, 8, 16, 1100, 4), ("pieces", 3, 3, 16, 5000, 8)]
+
+
+def mixed_tokens(rng, tokens, block):
+    """(slots, positions, blocks): single tokens, short runs and prompts over several blocks, from anywhere in a block; some left out by their slot or position."""
+    slots, pos, blk = [], [], 0
+    order = rng.permutation(2 * tokens)
+    while len(slots) < tokens:
+        kind = rng.integers(0, 4)
+        first = int(rng.integers(0, block)) if rng.integers(0, 2) else 0
+        n = min(tokens - len(slots), 1 if kind < 2 else int(rng.integers(2, 9)) if kind == 2 else int(rng.integers(block, 5 * block)))
+        slots += [int(order[blk + (first + i) // block]) * block + (first + i) % block for i in range(n)]
+        pos += list(range(first, first + n))
+        blk += (first + n + block - 1) // block
+    slots, pos = np.array(slots, np.int64), np.array(pos, np.int32)
+    pos[rng.random(tokens) < 0.01] = -1
+    # (a slot that is outside the cache would cut a run in two: the last tokens of their blocks, and single ones)
+    last = np.flatnonzero(np.append(slots[1:] != slots[:-1] + 1, True) | (slots % block == block - 1))
+    slots[last[rng.random(len(last)) < 0.05]] = rng.choice([-1, 2 * tokens * block, 2 ** 62])
+    return slots, pos, 2 * tokens
+
+
+@pytest.mark.parametrize("dtype,in_place,fused", [("bf16", True, True), ("f32", False, True), ("f16", False, False)])
+@pytest.mark.parametrize("read,heads,q_heads,block,tokens,window", WINDOWS)
+def test_runs_found_among_many_tokens(b, dtype, in_place, fused, read, heads, q_heads, block, tokens, window):  # noqa: F811
+    dim, rot, neighbours = READS[read]
+    rng = np.random.default_rng(tokens + block + dim)
+    slots, pos, n_blocks = mixed_tokens(rng, tokens, block)
+    x = values(rng, (tokens, (q_heads + 2 * heads) * dim), dtype)
+    check(b, rng, dtype, heads, q_heads, dim, block, n_blocks, slots, pos, x, b.rotary_table(6 * block, rot, 1000.0), neighbours, in_place, fused)
+
+
+def test_a_prompt_gives_the_same_bits_every_time(b):  # noqa: F811
+    """6000 tokens of one request, whose windows hold few beginnings of runs and many tokens of others'."""
+    rng = np.random.default_rng(5)
+    heads, q_heads, dim, block, T = 8, 32, 128, 64, 6000
+    n_blocks = -(-T // block) + 3
+    order = rng.permutation(n_blocks)
+    t = np.arange(T)
+    slots, pos = order[t // block].astype(np.int64) * block + t % block, t.astype(np.int32)
+    x, table = values(rng, (T, (q_heads + 2 * heads) * dim), "bf16"), b.rotary_table(T, dim)
+    c, qr = check(b, rng, "bf16", heads, q_heads, dim, block, n_blocks, slots, pos, x, table, False, False)
+    q, kx, vx = (p.unflatten(1, (n, dim)) for p, n in zip(x.split((q_heads * dim, heads * dim, heads * dim), 1), (q_heads, heads, heads)))
+    for _ in range(5):
+        again, turned = b.KvCache(n_blocks, heads, dim, block), torch.empty_like(qr)
+        b.abft_kv_append_rotary(again, q, kx, vx, dev(slots), dev(pos), table, QR=turned)
+        used = torch.unique(dev(slots) // block)
+        assert torch.equal(turned, qr) and torch.equal(again.k_scale[used], c.k_scale[used]) and torch.equal(again.v_scale[used], c.v_scale[used])
+        for one, two in zip(again.codes(), c.codes()):
+            one, two = (a[dev(slots) // block, :, dev(slots) % block] for a in (one, two))
+            assert torch.equal(one, two)
