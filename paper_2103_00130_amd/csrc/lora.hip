@@ -464,12 +464,7 @@ void launch_load(const abft_lora_t* L, int slot, const void* A, int64_t lda, con
 template <typename T>
 void launch_gemv(const LoraParams& p, const LoraCut& c, hipStream_t s) {
     const dim3 threads(kLoraWaves * 64), down((unsigned)c.slots, (unsigned)c.tiles, (unsigned)c.splits);
-    const int64_t rows = (int64_t)c.tiles * c.slots, most = (p.blocks + kLoraWaves - 1) / kLoraWaves;
-    // (binary32 with more than two sixteens of ranks takes the registers of a whole SIMD: no more workgroups than are resident at once)
-    const int64_t wanted = p.rank_tiles <= 2 ? kLoraUpGroups : sizeof(T) == 4 ? kLoraUpGroups / 4 : kLoraUpGroups;
-    int64_t columns = (wanted + rows - 1) / rows;
-    if (columns > most) columns = most;
-    const dim3 up((unsigned)columns, (unsigned)c.tiles, (unsigned)c.slots);
+    const dim3 up((unsigned)lora_up_groups(c, p.blocks, p.rank_tiles, sizeof(T) == 4), (unsigned)c.tiles, (unsigned)c.slots);
     auto launch = [&](auto rt) {
         constexpr int RT = decltype(rt)::value;
         lora_down_kernel<T, RT><<<down, threads, 0, s>>>(p);

@@ -32,6 +32,14 @@ inline LoraCut lora_cut(int64_t M, int K) {
     c.splits = s < 1 ? 1 : (int)s;
     return c;
 }
+// Workgroups among which the columns of a tile's rows are dealt, `blocks` times 64 of them.  (binary32 with more than two sixteens of ranks takes the
+// registers of a whole SIMD: no more workgroups than are resident at once)
+inline int lora_up_groups(const LoraCut& c, int blocks, int rank_tiles, bool f32) {
+    const int64_t rows = (int64_t)c.tiles * c.slots, most = (blocks + kLoraWaves - 1) / kLoraWaves;
+    const int64_t wanted = rank_tiles <= 2 ? kLoraUpGroups : f32 ? kLoraUpGroups / 4 : kLoraUpGroups;
+    const int64_t groups = (wanted + rows - 1) / rows;
+    return (int)(groups < most ? groups : most);
+}
 // Workgroups of 256 threads for the elements of an adapter's layout: no more than a launch may have, of fewer than 2^32 threads.
 inline int64_t lora_load_groups(int64_t elements) {
     const int64_t groups = (elements + 255) / 256;
