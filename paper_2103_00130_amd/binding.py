@@ -558,6 +558,13 @@ def _entries(t, dtype, n, name):
     return _ptr(t, dtype, name)
 
 
+def _int32(n, name) -> int:
+    """n as the library takes it, which a number of more bits would reach as another one."""
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{name}={n} is too large")
+    return int(n)
+
+
 class W4Weight:
     """Owner of an abft_w4 handle."""
 
@@ -632,7 +639,8 @@ class LoraPool:
     def __init__(self, adapters: int, K: int, N: int, max_rank: int, dtype=torch.bfloat16, device="cuda"):
         if dtype not in _TYPES:
             raise TypeError(f"adapters are float32, float16 or bfloat16, not {dtype}")
-        self.adapters, self.K, self.N, self.max_rank, self.dtype = int(adapters), int(K), int(N), int(max_rank), dtype
+        self.adapters, self.K, self.N, self.max_rank = (_int32(n, name) for n, name in ((adapters, "adapters"), (K, "K"), (N, "N"), (max_rank, "max_rank")))
+        self.dtype = dtype
         sizes = (self.adapters, self.max_rank, self.K, self.N, _TYPES[dtype])
         down, up = ctypes.c_size_t(), ctypes.c_size_t()
         if lib.abft_lora_bytes(ctypes.byref(abft_lora_t(None, None, None, None, *sizes)), ctypes.byref(down), ctypes.byref(up)) != ABFT_OK:
@@ -655,18 +663,19 @@ class LoraPool:
 def abft_lora_load(pool: LoraPool, slot: int, A: torch.Tensor | None, B: torch.Tensor | None, scale: float = 1.0, stream=None):
     if (A is None) != (B is None):
         raise ValueError("an adapter has both A and B, or neither")
+    slot = _int32(slot, "slot")
     if A is None:
-        _check(lib.abft_lora_load(pool.ref, int(slot), None, 0, None, 0, 0, float(scale), _stream(stream)))
+        _check(lib.abft_lora_load(pool.ref, slot, None, 0, None, 0, 0, float(scale), _stream(stream)))
         return
     lda, ldb = _ld(A, "A"), _ld(B, "B")
-    rank = A.shape[0]
+    rank = _int32(A.shape[0], "rank")
     if tuple(A.shape) != (rank, pool.K) or tuple(B.shape) != (pool.N, rank):
         raise ValueError(f"A is {tuple(A.shape)} and B {tuple(B.shape)}, the pool takes rank x {pool.K} and {pool.N} x rank")
-    _check(lib.abft_lora_load(pool.ref, int(slot), _ptr(A, pool.dtype, "A"), lda, _ptr(B, pool.dtype, "B"), ldb, rank, float(scale), _stream(stream)))
+    _check(lib.abft_lora_load(pool.ref, slot, _ptr(A, pool.dtype, "A"), lda, _ptr(B, pool.dtype, "B"), ldb, rank, float(scale), _stream(stream)))
 
 
 def abft_lora_workspace_bytes(pool: LoraPool, M: int) -> int:
-    return int(lib.abft_lora_workspace_bytes(pool.ref, int(M)))
+    return int(lib.abft_lora_workspace_bytes(pool.ref, _int32(M, "M")))
 
 
 class LoraWorkspace:
@@ -689,12 +698,12 @@ def abft_lora_gemv(X: torch.Tensor, pool: LoraPool, ids: torch.Tensor, Y: torch.
     M = X.shape[0]
     if X.shape[1] != pool.K or tuple(Y.shape) != (M, pool.N) or tuple(base.shape) != (M, pool.N):
         raise ValueError(f"X is {tuple(X.shape)}, base {tuple(base.shape)} and Y {tuple(Y.shape)}, the pool has K={pool.K}, N={pool.N}")
-    _check(lib.abft_lora_gemv(_ptr(X, pool.dtype, "X"), ldx, M, pool.ref, _entries(ids, torch.int32, M, "ids"), _ptr(base, pool.dtype, "base"), ldb,
+    _check(lib.abft_lora_gemv(_ptr(X, pool.dtype, "X"), ldx, _int32(M, "M"), pool.ref, _entries(ids, torch.int32, M, "ids"), _ptr(base, pool.dtype, "base"), ldb,
                               _ptr(Y, pool.dtype, "Y"), ldy, *_lent(workspace, "workspace"), _stream(stream)))
 
 
 def abft_logprobs_workspace_bytes(n_rows: int, vocab: int, top: int) -> int:
-    return int(lib.abft_logprobs_workspace_bytes(int(n_rows), int(vocab), int(top)))
+    return int(lib.abft_logprobs_workspace_bytes(int(n_rows), _int32(vocab, "vocab"), _int32(top, "top")))
 
 
 class LogprobsWorkspace:
@@ -723,7 +732,8 @@ def abft_logprobs(logits: torch.Tensor, targets=None, logprob=None, rank=None, e
     if top_index is not None:
         if top_index.dim() != 2 or top_index.shape[0] != n_rows or tuple(top_logprob.shape) != tuple(top_index.shape):
             raise ValueError(f"top_logprob and top_index must be {n_rows} x alternatives")
-        top = top_index.shape[1]
+        top = _int32(top_index.shape[1], "top")
+    _int32(vocab, "vocab")
     each = lambda t, dtype, n, name: None if t is None else _entries(t, dtype, n, name)
     _check(lib.abft_logprobs(at, ldl, kind, n_rows, vocab, float(scale), each(targets, torch.int64, n_rows, "targets"), each(logprob, torch.float32, n_rows, "logprob"),
                              each(rank, torch.int32, n_rows, "rank"), each(entropy, torch.float32, n_rows, "entropy"), each(lse, torch.float32, n_rows, "lse"), top,
@@ -835,7 +845,7 @@ def abft_kv_append_rotary(cache: KvCache, Q, K, V, slots, positions, table, QR=N
     if Q is not None:
         if Q.dim() != 3:
             raise ValueError("Q must be tokens x query heads x head_dim")
-        q_heads = Q.shape[1]
+        q_heads = _int32(Q.shape[1], "q_heads")
         if _typed(Q, "Q")[1] != k_type or _typed(QR, "QR")[1] != k_type:
             raise TypeError("Q, QR, K and V must have the same type")
     elif QR is not None:
@@ -844,6 +854,7 @@ def abft_kv_append_rotary(cache: KvCache, Q, K, V, slots, positions, table, QR=N
         raise TypeError("K and V must have the same type")
     if table.dim() != 2:
         raise ValueError("table must be positions x columns that turn")
+    _int32(table.shape[1], "rot_dim")
     q, r = ((none if t is None else _kv_rows(t, cache, T, name, q_heads)) for t, name in ((Q, "Q"), (QR, "QR")))
     _check(lib.abft_kv_append_rotary(cache.ref, *q, q_heads, *r, *_kv_rows(K, cache, T, "K"), *_kv_rows(V, cache, T, "V"), k_type,
                                      _entries(slots, torch.int64, T, "slots"), _entries(positions, torch.int32, T, "positions"), T,

@@ -42,3 +42,19 @@ def test_an_adapter_of_any_size_is_loaded_by_one_launch(tmp_path):
     assert [f(n) for n in (0, 1, 256, 257)] == [1, 1, 1, 2]
     for n in (2 ** 32 - 256, 2 ** 32 - 255, 2 ** 32, 2 ** 33, 128 * 2 * (2 ** 31 - 256)):
         assert 0 < f(n) * 256 < 2 ** 32, n
+
+
+def test_sizes_of_more_than_32_bits_are_not_cut_to_them(b):
+    for bad in ((2 ** 32 + 2, 64, 64, 8), (2, 2 ** 32 + 64, 64, 8), (2, 64, 2 ** 32 + 64, 8), (2, 64, 64, 2 ** 32 + 8)):
+        with pytest.raises(ValueError):
+            b.LoraPool(*bad, device="cpu")
+    for bad in ((1, 2 ** 32 + 100000, 5), (1, 100000, 2 ** 32 + 5)):
+        with pytest.raises(ValueError):
+            b.abft_logprobs_workspace_bytes(*bad)
+
+    class Pool:
+        ref = ctypes.byref(b.abft_lora_t(0x1000, 0x1000, 0x1000, 0x1000, 3, 20, 100, 70, 2))
+    with pytest.raises(ValueError):
+        b.abft_lora_workspace_bytes(Pool, 2 ** 32 + 5)
+    with pytest.raises(ValueError):
+        b.abft_lora_load(Pool, 2 ** 32, None, None)

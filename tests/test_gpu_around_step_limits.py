@@ -66,3 +66,11 @@ def test_an_adapter_of_more_elements_than_a_launch_has_threads(b, K, N):  # noqa
         for n in range(0, N, 2 ** 22):      # (whole numbers below 2^24)
             want[n:n + 2 ** 22] += B[n:n + 2 ** 22].float() @ mid[i]
         assert torch.equal(y[i], want.to(torch.bfloat16))
+
+
+def test_a_vocabulary_of_more_than_32_bits_is_not_cut_to_them(b):  # noqa: F811
+    x = torch.zeros((1, 2 ** 32 + 5), dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((1,), 7.0, device="cuda")
+    with pytest.raises(ValueError):
+        b.abft_logprobs(x, lse=lse)
+    assert lse.item() == 7.0
