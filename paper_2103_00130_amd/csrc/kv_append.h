@@ -2,6 +2,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "kv_append_cut.h"
 #include "kv_cache.h"
 #include "values.h"
@@ -205,6 +207,12 @@ __device__ inline void append_run(const CacheParams& p, const Source& src, int8_
     constexpr int kSets = Source::kSets;
     const int places = (pieces + kSets - 1) / kSets, units = p.block / U * places;
     Eight<T> e, v[kSets][U];
+    // (v is indexed by numbers known as the source is read: a loop over sets is unrolled after arrays have been made registers, and their copies took 240 of them
+    // instead of 125 where 16 tokens are a unit: 2000 tokens of one request, 8 heads of 128 15.4 us for 11.6, 3000 in binary32 18.8 for 14.6)
+    auto for_sets = [&](const auto& f) __attribute__((always_inline)) {
+        f(std::integral_constant<int, 0>());
+        if constexpr (kSets > 1) f(std::integral_constant<int, 1>());
+    };
     // (every token of a unit is loaded, from rows that exist, so that the loads go out together)
     auto load = [&](int o, int c) __attribute__((always_inline)) {
         constexpr int kTogether = kSets == 1 || U < 4 ? U : 4;
@@ -235,10 +243,10 @@ __device__ inline void append_run(const CacheParams& p, const Source& src, int8_
             const int o = u / places * U;
             if (o + U <= first || o >= first + n) continue;
             load(o, u % places);
+            for_sets([&](auto s) __attribute__((always_inline)) {
 #pragma unroll
-            for (int s = 0; s < kSets; ++s)
-#pragma unroll
-                for (int j = 0; j < U; ++j) most = max_bits(most, v[s][j]);
+                for (int j = 0; j < U; ++j) most = max_bits(most, v[s.value][j]);
+            });
         }
     }
     // (as bits: those of an infinity or a NaN are above all others, where a maximum of floats would pass a NaN by)
@@ -295,13 +303,12 @@ __device__ inline void append_run(const CacheParams& p, const Source& src, int8_
             const int o = u / places * U;
             if (o + U <= first || o >= first + n) continue;
             if (units > 64) load(o, u % places);   // (with one unit to a lane it is there)
-#pragma unroll
-            for (int s = 0; s < kSets; ++s) {
-                const int d = src.column(u % places, s);
-                if (kSets > 1 && d >= p.dim) continue;
-                if (finite) store_unit<T, VALUES, true, U>(p, v[s], codes, o, d, first, n, r);
-                else store_unit<T, VALUES, false, U>(p, v[s], codes, o, d, first, n, r);
-            }
+            for_sets([&](auto s) __attribute__((always_inline)) {
+                const int d = src.column(u % places, s.value);
+                if (kSets > 1 && d >= p.dim) return;
+                if (finite) store_unit<T, VALUES, true, U>(p, v[s.value], codes, o, d, first, n, r);
+                else store_unit<T, VALUES, false, U>(p, v[s.value], codes, o, d, first, n, r);
+            });
         }
     }
 }
