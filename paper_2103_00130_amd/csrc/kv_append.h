@@ -178,12 +178,12 @@ __device__ inline void store_unit(const CacheParams& p, const Eight<T> (&v)[U], 
 }
 
 // The tokens of a run, as they are.  kSets: how many times 8 columns a lane has of a token where runs are long; column(c, set): where those of its
-// c-th place begin.
+// c-th place begin.  kTogether: tokens whose loads are under way together, at most, as what they are loaded as (Raw).
 template <typename T, bool WIDE>
 struct Rows {
     typedef T Kept;
     static constexpr bool kWide = WIDE;
-    static constexpr int kSets = 1;
+    static constexpr int kSets = 1, kTogether = 16;
     const T* x;
     int64_t stride;
     __device__ inline void load(Eight<T>& e, int token, int d, int dim) const { load_eight<T, WIDE>(e, x + (int64_t)token * stride, d, dim); }
@@ -215,7 +215,7 @@ __device__ inline void append_run(const CacheParams& p, const Source& src, int8_
     };
     // (every token of a unit is loaded, from rows that exist, so that the loads go out together)
     auto load = [&](int o, int c) __attribute__((always_inline)) {
-        constexpr int kTogether = kSets == 1 || U < 4 ? U : 4;
+        constexpr int kTogether = U < Source::kTogether ? U : Source::kTogether;
 #pragma unroll
         for (int j0 = 0; j0 < U; j0 += kTogether) {
             typename Source::Raw raw[kTogether];
@@ -316,58 +316,58 @@ __device__ inline void append_run(const CacheParams& p, const Source& src, int8_
 constexpr int kAppendWaves = 2 * kAppendHeads;
 
 // The runs that begin among the tokens of a window, by a workgroup: two heads of each (those of `group`), keys and values, dealt to its
-// wavefronts.  s_slot: kMaxAhead slots; slot_of(t, i) is token t's, i its place there; append(side, head, token, its place, block, first, n).
-// LEAVES: tokens of a run for whose place left_out holds stay out of it, and those behind them are appended as a run of their own, behind the one
+// wavefronts.  s_slot: kMaxAhead slots; slot_of(t, i, &out) is token t's, i its place there; append(side, head, token, its place, block, first, n).
+// LEAVES: a token for which slot_of sets `out` stays out of its run, and those behind it are appended as a run of their own, behind the one
 // before them: by the same wavefront, since a block's runs share its scale and the codes that it rescales.
-template <bool LEAVES, typename Slot, typename LeftOut, typename Append>
-__device__ inline void append_runs(const CacheParams& p, int64_t* s_slot, int group, const Slot& slot_of, const LeftOut& left_out, const Append& append) {
+constexpr int64_t kLeftOut = 1ll << 62;   // beside the slot of such a token (far above any of a cache)
+template <bool LEAVES, typename Slot, typename Append>
+__device__ inline void append_runs(const CacheParams& p, int64_t* s_slot, int group, const Slot& slot_of, const Append& append) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t t0 = (int64_t)blockIdx.x * p.window;
     // of the token before the window, the window, and what a run can reach
     const int ahead = p.window + p.block + 1;
     for (int i = threadIdx.x; i < ahead; i += kAppendWaves * 64) {
         const int64_t t = t0 - 1 + i;
-        const int64_t v = t >= 0 && t < p.n_tokens ? slot_of(t, i) : -1;
-        s_slot[i] = v >= 0 && v < p.limit ? v : -1;
+        bool out = false;
+        const int64_t v = t >= 0 && t < p.n_tokens ? slot_of(t, i, &out) : -1;
+        s_slot[i] = v < 0 || v >= p.limit ? -1 : LEAVES && out ? v | kLeftOut : v;
     }
     __syncthreads();
+    auto slot_at = [&](int i) { return LEAVES && s_slot[i] >= 0 ? s_slot[i] & ~kLeftOut : s_slot[i]; };
     // the tokens of the window that begin a run: those that do not continue the slot before them within its block
     bool begins = false;
     if (lane < p.window) {
-        const int64_t slot = s_slot[lane + 1];
-        begins = slot >= 0 && (((int)slot & (p.block - 1)) == 0 || s_slot[lane] != slot - 1);
+        const int64_t slot = slot_at(lane + 1);
+        begins = slot >= 0 && (((int)slot & (p.block - 1)) == 0 || slot_at(lane) != slot - 1);
     }
     unsigned long long left = __ballot(begins);
     const int side = wave & 1, head = group * kAppendHeads + (wave >> 1);
     if (head >= p.heads) return;
-    // the first number for which it does not hold (at most kMaxBlock)
-    auto count = [&](const auto& holds) __attribute__((always_inline)) {
-        int n = 0;
-#pragma unroll
-        for (int h = 0; h < kMaxBlock / 64; ++h) {
-            const unsigned long long b = __ballot(holds(h * 64 + lane));
-            if (n == h * 64) n += b == ~0ull ? 64 : __builtin_ctzll(~b);
-        }
-        return n;
-    };
     for (; left; left &= left - 1) {
         const int w = __builtin_ctzll(left);
-        const int64_t slot = s_slot[w + 1], block = slot >> p.shift;
+        const int64_t slot = slot_at(w + 1), block = slot >> p.shift;
         const int first = (int)slot & (p.block - 1);
-        // the run's length: how many slots count up from here without leaving the block
-        const int n = count([&](int j) { return j < p.block - first && s_slot[w + 1 + j] == slot + j; });
-        if constexpr (!LEAVES) {
-            append(side, head, t0 + w, w + 1, block, first, n);
-        } else {
-            for (int at = 0; at < n;) {
-                const int kept = count([&](int j) { return at + j < n && !left_out(w + 1 + at + j); });
-                if (kept > 0) append(side, head, t0 + w + at, w + 1 + at, block, first + at, kept);
-                at += kept + 1;
-                if (kept > 0 && at < n) {   // (what is behind reads the scale and the codes that were stored)
-                    __builtin_amdgcn_s_waitcnt(0);
-                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        for (int at = 0;;) {
+            // the run's length: how many slots count up from here without leaving the block, and whether they go on behind a token that is left out
+            int n = 0;
+            bool more = false;
+#pragma unroll
+            for (int h = 0; h < kMaxBlock / 64; ++h) {
+                const int j = at + h * 64 + lane;
+                const int64_t v = j < p.block - first ? s_slot[w + 1 + j] : -1;
+                const unsigned long long kept = __ballot(v == slot + j), out = LEAVES ? __ballot(v == (slot + j | kLeftOut)) : 0;
+                if (n == h * 64) {
+                    const int these = kept == ~0ull ? 64 : __builtin_ctzll(~kept);
+                    n += these;
+                    more = these < 64 && (out >> these & 1);
                 }
             }
+            if (!LEAVES || n > 0) append(side, head, t0 + w + at, w + 1 + at, block, first + at, n);
+            if (!LEAVES || !more) break;
+            at += n + 1;
+            // (what is behind reads the scale and the codes that were stored)
+            __builtin_amdgcn_s_waitcnt(0);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
         }
     }
 }

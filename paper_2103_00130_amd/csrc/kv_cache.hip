@@ -19,7 +19,7 @@ namespace {
 template <typename T, bool WIDE, int U>
 __global__ __launch_bounds__(kAppendWaves * 64) void kv_append_kernel(const CacheParams p) {
     __shared__ int64_t s_slot[kMaxAhead];
-    append_runs<false>(p, s_slot, blockIdx.y, [&](int64_t t, int) { return p.slots[t]; }, [](int) { return false; }, [&](int side, int head, int64_t t, int, int64_t block, int first, int n) {
+    append_runs<false>(p, s_slot, blockIdx.y, [&](int64_t t, int, bool*) { return p.slots[t]; }, [&](int side, int head, int64_t t, int, int64_t block, int first, int n) {
         const Side& s = p.side[side];
         const Rows<T, WIDE> src = {static_cast<const T*>(s.x) + t * s.token_stride + head * s.head_stride, s.token_stride};
         int8_t* const codes = s.codes + (block * p.heads + head) * p.block * p.cols;

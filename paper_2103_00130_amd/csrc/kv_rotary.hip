@@ -10,7 +10,8 @@
 // positions, then rows; 6000 tokens of a fused projection 33.8 us, 4.0 TB/s of 135 MB, 28.2 where rows come from the memory-side cache, 25.0 with queries
 // in place.  Queries alone take 17; keys are what waits longest: a run is a wavefront's, since it has one scale, and a lane turns 8 tokens of 16 columns.  A
 // lane that loaded each side of a pair for itself took twice as long for keys (37.7 against 21.5, with windows of 16; 13.8 with those of 64).  Columns that are no eights of
-// pairs (a rotation of 120 columns) cost nearly four times that, 100 us: partners, cosines and sines are loaded one by one.
+// pairs (a rotation of 120 columns) cost two and a half times that, 72 us (81 as neighbours): partners, cosines and sines are loaded one by one, of four tokens
+// together (of eight 100, and up to 340 registers: beyond 256 the compiler lost a constant that it put aside).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -108,7 +109,7 @@ template <typename T, bool NEIGHBOURS>
 struct Turned<T, kPieces, NEIGHBOURS> {
     typedef float Kept;
     static constexpr bool kWide = true;
-    static constexpr int kSets = 1;
+    static constexpr int kSets = 1, kTogether = 4;
     const T* x;
     int64_t stride;
     const float* table;
@@ -140,7 +141,7 @@ template <typename T, int READ, bool NEIGHBOURS>
 struct Turned {   // kPairs and kElements
     typedef float Kept;
     static constexpr bool WIDE = READ == kPairs, kWide = WIDE;
-    static constexpr int kSets = 2;   // of long runs a lane has both sides of 8 pairs
+    static constexpr int kSets = 2, kTogether = sizeof(T) == 4 ? 2 : 4;   // of long runs a lane has both sides of 8 pairs
     const T* x;
     int64_t stride;
     const float* table;
@@ -357,12 +358,12 @@ __global__ __launch_bounds__(kAppendWaves * 64) void kv_append_rotary_kernel(con
     // (runs go by the slots alone: two of one block have to be the same wavefront's, which a token without a row of the table does not change)
     append_runs<true>(
         c, s_slot, blockIdx.y,
-        [&](int64_t t, int i) {
+        [&](int64_t t, int i, bool* out) {
             const int position = p.positions[t];
-            s_position[i] = position < p.n_positions ? position : -1;
+            s_position[i] = position;
+            *out = position < 0 || position >= p.n_positions;
             return c.slots[t];
         },
-        [&](int i) { return s_position[i] < 0; },
         [&](int side, int head, int64_t t, int at, int64_t block, int first, int n) {
             const Side& s = c.side[side];
             const T* const x = static_cast<const T*>(s.x) + t * s.token_stride + head * s.head_stride;
