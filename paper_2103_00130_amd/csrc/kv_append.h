@@ -355,7 +355,7 @@ __device__ inline void append_runs(const CacheParams& p, int64_t* s_slot, int gr
             for (int h = 0; h < kMaxBlock / 64; ++h) {
                 const int j = at + h * 64 + lane;
                 const int64_t v = j < p.block - first ? s_slot[w + 1 + j] : -1;
-                const unsigned long long kept = __ballot(v == slot + j), out = LEAVES ? __ballot(v == (slot + j | kLeftOut)) : 0;
+                const unsigned long long kept = __ballot(v == slot + j), out = __ballot(LEAVES && v == (slot + j | kLeftOut));
                 if (n == h * 64) {
                     const int these = kept == ~0ull ? 64 : __builtin_ctzll(~kept);
                     n += these;
