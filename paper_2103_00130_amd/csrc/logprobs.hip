@@ -8,8 +8,9 @@
 // what does not reach a bar is dropped by one comparison for eight logits, the rest is gathered in LDS and sorted in 64 at a time, by lanes that
 // exchange keys without LDS.  The bar is what as many lanes reach as are wanted, which costs six steps across lanes, and then the list's last wanted entry.
 //
-// Measured: 2048 x 32000 binary32 with ranks and 5 alternatives 62 us, 4.2 TB/s (48.7 and 5.4 TB/s without alternatives and ranks; with 20 / 64
-// alternatives 69 / 77); the same in bfloat16 without alternatives 33 us, 4.1 TB/s: half the bytes, as many logits to go through.  1 x 131072 bfloat16 with 20 alternatives 10.5 us in 64 parts (6.4 and, for the join, 4.0; 5.9 without alternatives): two launches, and
+// Measured (a pass among others): 2048 x 32000 binary32 with ranks and 5 alternatives 62 us, 4.2 TB/s (48.5 and 5.4 TB/s without alternatives and ranks; with 20 / 64
+// alternatives 69 / 77); the same in bfloat16 without alternatives 33 us, 4.1 TB/s: half the bytes, as many logits to go through.  Alternatives cost 16-bit logits most,
+// since their sorts are as many: with 20 of them 63 us, 2.1 TB/s, 256 x 131072 41, 1.6 TB/s.  1 x 131072 bfloat16 with 20 alternatives 10.5 us in 64 parts (6.4 and, for the join, 4.0; 5.9 without alternatives): two launches, and
 // four sorts behind each other.  64 x 50001 13.1 (11 and 4.0).  The first form, whose wavefronts kept lists of their own sorted through
 // LDS, took 34, 24 and, for 2048 x 32000, 97.
 #include <hip/hip_runtime.h>

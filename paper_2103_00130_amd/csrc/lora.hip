@@ -9,7 +9,8 @@
 // Measured (4096 x 4096, bf16): one row of rank 16 6.8 us, both launches and two dependent trips to memory each (3.2 and 4.2); 64 rows through 36 adapters to
 // 6144 columns 9.4 (10.3 MB; 3.9 and 6.0, as many workgroups as rows have adapters, each with little to do); 4287 rows of nine prompts 46 (14.5 and 32, the
 // first at 2.4 TB/s, the second at 2.2 of base and Y; a copy of such rows, 16 of them and 128 bytes of each at a time, takes 17.7, rows end to end 15.7);
-// 4096 rows of rank 16 / 32 / 128 27 / 34 / 82.  Where 16 rows have several adapters the tile is gone through for each (with tiles of 32 rows 51 us for nine
+// 4096 rows of rank 16 / 32 / 128 26 / 33 / 80 (of rank 32 in float16 37); 2048 rows of rank 32 in binary32 44; 540 rows of rank 72 in binary32, 185 to 9239
+// columns, 38; 8 rows of rank 128 15; 4000 rows of rank 20, 1001 to 4099 columns (no row at a multiple of 16 bytes) 45.  Where 16 rows have several adapters the tile is gone through for each (with tiles of 32 rows 51 us for nine
 // prompts that begin anywhere, 43 for such that begin at multiples of 32; 4096 rows of 64 adapters in no order 120).
 #include <hip/hip_runtime.h>
 

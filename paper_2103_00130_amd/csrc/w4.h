@@ -14,7 +14,7 @@
 //    take chunks along K in turn and their sums meet in LDS in a fixed order.
 //
 // Measured: 1 x 4096 x 4096, bf16, groups of 128: 3.9 us (8.7 MB, 2.2 TB/s: launch, a trip to memory and the join, behind each other); 1 x 16384 x
-// 4096 9.2 us (3.8 TB/s); 16 x 16384 x 4096, f16, groups of 64 with bias: 11.6 us (38 MB, 3.3 TB/s; the rows of X that every workgroup
+// 4096 9.2 us (3.8 TB/s); 16 x 16384 x 4096, f16, groups of 64 with bias: 10.5 us (38 MB, 3.65 TB/s; the rows of X that every workgroup
 // fetches, and the vector work on codes and scales, beside the codes); 3 x 5001 x 1237, f32: 5.5 us (4.7 MB; rows of X at odd addresses, three parts each).
 #pragma once
 #include <hip/hip_runtime.h>
