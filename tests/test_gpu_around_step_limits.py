@@ -74,3 +74,57 @@ def test_a_vocabulary_of_more_than_32_bits_is_not_cut_to_them(b):  # noqa: F811
     with pytest.raises(ValueError):
         b.abft_logprobs(x, lse=lse)
     assert lse.item() == 7.0
+
+
+def test_logits_of_more_than_2_to_the_31_elements(b):  # noqa: F811
+    M, V, top = 70000, 33000, 3
+    x = torch.empty((M, V), dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(3))
+    targets = torch.arange(M, device="cuda") % V
+    results = lambda n: {"logprob": torch.empty(n, device="cuda"), "rank": torch.empty(n, dtype=torch.int32, device="cuda"), "entropy": torch.empty(n, device="cuda"),
+                         "top_logprob": torch.empty((n, top), device="cuda"), "top_index": torch.empty((n, top), dtype=torch.int64, device="cuda")}
+    whole = results(M)
+    b.abft_logprobs(x, targets, **whole)
+    for first in (0, 2 ** 31 // V - 600, 2 ** 32 // V // 2 - 10, M - 1100):      # (rows that are not cut either: the same bits)
+        rows, some = slice(first, first + 1100), results(1100)
+        b.abft_logprobs(x[rows].clone(), targets[rows], **some)
+        assert all(torch.equal(some[k], whole[k][rows]) for k in some), first
+
+
+@pytest.mark.parametrize("K,N", [(8_000_000, 16), (16, 8_000_000)])
+def test_rows_of_adapters_of_more_than_2_to_the_31_elements(b, K, N):  # noqa: F811
+    """Whole numbers, whose sums are exact however they are cut."""
+    M, rank, g = 300, 4, torch.Generator("cuda").manual_seed(4)
+    whole = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda").uniform_(-1.49, 1.49, generator=g).round_()
+    x, base, pool = whole(M, K), whole(M, N), b.LoraPool(2, K, N, rank)
+    for slot in range(2):
+        A, B = whole(rank, K), whole(N, rank)
+        A[:, 64:] *= (torch.rand(max(K - 64, 0), device="cuda", generator=g) < 1e-5).to(A.dtype)      # (sums below 2^8, which bfloat16 holds)
+        pool.load(slot, A, B)
+    ids = (torch.arange(M, device="cuda") % 3 - 1).int()
+    y = torch.empty_like(base)
+    b.abft_lora_gemv(x, pool, ids, y, base=base, workspace=b.LoraWorkspace(pool, M).tensor)
+    for first in (0, 260, M - 20):
+        rows = slice(first, first + 20)
+        some = base[rows].clone()
+        b.abft_lora_gemv(x[rows].clone(), pool, ids[rows].clone(), some, workspace=b.LoraWorkspace(pool, 20).tensor)
+        assert torch.equal(some, y[rows]) and not torch.equal(some, base[rows]), first
+
+
+def test_queries_of_more_than_2_to_the_31_elements(b):  # noqa: F811
+    T, q_heads, dim, block = 70000, 256, 128, 64
+    q = torch.empty((T, q_heads, dim), dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(5))
+    kv = torch.randn((T, 2, 1, dim), device="cuda").to(torch.bfloat16)
+    table, c = b.rotary_table(1000, dim), b.KvCache(T // block + 1, 1, dim, block)
+    at = torch.arange(T, device="cuda")
+    slots, pos = at, (at % 1000).int()
+    turned = torch.empty_like(q)
+    b.abft_kv_append_rotary(c, q, kv[:, 0], kv[:, 1], slots, pos, table, QR=turned)
+    for first in (0, 65536 - 64, T // block * block - 640):
+        rows, d = slice(first, first + 640), b.KvCache(10, 1, dim, block)
+        some = q[rows].clone()
+        b.abft_kv_append_rotary(d, some, kv[rows, 0], kv[rows, 1], at[:640], pos[rows], table)
+        assert torch.equal(some, turned[rows])
+        for one, two in zip(d.codes(), c.codes()):
+            assert torch.equal(one, two[first // block:first // block + 10])
+    b.abft_kv_append_rotary(c, q, kv[:, 0], kv[:, 1], slots, pos, table)      # in place
+    assert torch.equal(q, turned)
